@@ -186,7 +186,7 @@ def _run_own(s):
         loss, lse = sip.sip_xent_forward(s["hidden"], s["weight"], s["targets"], workspace=s["workspace"])
         if op == "score":
             return {"loss": loss, "lse": lse}
-        sip.sip_xent_backward(s["hidden"], s["weight"], s["targets"], lse, s["grad_loss"], s["scale"],
+        sip.sip_xent_backward(s["hidden"], s["weight"], s["targets"], loss, lse, s["grad_loss"], s["scale"],
                               grad_hidden=s["grad_hidden"], grad_weight=s["grad_weight"], workspace=s["workspace"])
         return {"loss": loss, "grad_hidden": s["grad_hidden"], "grad_weight": s["grad_weight"]}
     if op == "head":
@@ -210,17 +210,17 @@ def _plain_xent(s):
     rest = z.scatter(1, at, -math.inf)
     top = rest.amax(1, keepdim=True)
     gap = top + (rest - top).exp_().sum(1, keepdim=True).log() - zt
-    loss = gap.clamp(min=0.0) + (-gap.abs()).exp().log1p()
-    lse = zt + loss
+    every = gap.clamp(min=0.0) + (-gap.abs()).exp().log1p()
+    lse = zt + every
     zero = torch.zeros_like(lse)
-    loss = torch.where(valid[:, None], loss, zero)[:, 0]
+    loss = torch.where(valid[:, None], every, zero)[:, 0]
     if s["case"]["op"] == "score":
         return {"loss": loss, "lse": torch.where(valid[:, None], lse, zero)[:, 0]}
     g = valid.float() * s["scale"]
     if s["grad_loss"] is not None:
         g = g * s["grad_loss"]
     p = z.sub_(lse).exp_()
-    p.scatter_add_(1, at, torch.full_like(lse, -1.0))
+    p.scatter_(1, at, torch.expm1(-every))     # p_t - 1
     p.mul_(g[:, None])
     return {"loss": loss, "grad_hidden": (p @ w).bfloat16(), "grad_weight": (p.t() @ h).bfloat16()}
 
