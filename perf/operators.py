@@ -247,10 +247,11 @@ def _plain_clip(s):
 def _plain_quantise(s):
     w = s["weight"].float().unflatten(1, (-1, s["case"]["group"]))
     if s["zeros"] is None:
-        scale = w.abs().amax(2) / 7.0
+        scale = w.abs().amax(2)
+        scale = scale / torch.full_like(scale, 7.0)    # (torch multiplies by the reciprocal of a plain number)
     else:
         low = w.amin(2).clamp(max=0.0)
-        scale = (w.amax(2).clamp(min=0.0) - low) / 15.0
+        scale = (w.amax(2).clamp(min=0.0) - low) / torch.full_like(low, 15.0)
     scale = scale.to(s["scales"].dtype).float()
     scale = torch.where(scale == 0.0, torch.ones_like(scale), scale)
     zero = torch.full_like(scale, 8.0) if s["zeros"] is None else (-low / scale).round().clamp(0.0, 15.0)
