@@ -897,3 +897,6 @@ void sip_profile_kernel_events(void* stream_start, void* stream_stop, void* fini
 int sip_version(void) { return 100; }
 
 }  // extern "C"
+
+// The vocabulary head (include/sip_head.h).
+#include "sip_vocab.h"

@@ -1,0 +1,301 @@
+"""Cross entropy of given tokens under the head and its gradient, against the definitions in 64 bits."""
+import math
+
+import pytest
+import torch
+
+import paper_2506_22033_amd as sip
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+def make(N, V, D, seed=0, masked=0.0, lift=6.0, h_pad=0, w_pad=0):
+    g = torch.Generator().manual_seed(seed)
+    w = (torch.randn(V, D, generator=g) * (1.5 / math.sqrt(D))).bfloat16()
+    t = torch.randint(0, V, (N,), generator=g, dtype=torch.int32)
+    wt = w[t.long()].float()
+    h = torch.randn(N, D, generator=g) + lift * torch.rand(N, 1, generator=g) * wt / wt.square().sum(1, keepdim=True).clamp(min=1e-3)
+    t[torch.rand(N, generator=g) < masked] = -100
+    hidden = torch.full((N, D + h_pad), 77.0, dtype=torch.bfloat16)
+    hidden[:, :D] = h.bfloat16()
+    weight = torch.full((V, D + w_pad), -55.0, dtype=torch.bfloat16)
+    weight[:, :D] = w
+    return hidden.to(DEV)[:, :D], weight.to(DEV)[:, :D], t.to(DEV)
+
+
+def reference(hidden, weight, targets, logit_scale=1.0, grad_loss=None, scale=1.0):
+    """loss, lse, grad_hidden, grad_weight in 64 bits, and what bounds the errors: the scale of the logits' terms,
+    and of the two gradients' terms."""
+    V = weight.shape[0]
+    valid = (targets >= 0) & (targets < V)
+    rows = valid.nonzero()[:, 0]
+    h, w, t = hidden[rows].double(), weight.double(), targets[rows].long()
+    z = logit_scale * (h @ w.t())
+    lse = torch.logsumexp(z, 1) if rows.numel() else z.sum(1)
+    loss = lse - z.gather(1, t[:, None])[:, 0]
+    p = (z - lse[:, None]).exp()
+    p.scatter_(1, t[:, None], 0.0)
+    p.scatter_(1, t[:, None], -p.sum(1, keepdim=True))   # p_t - 1 is minus what the others have (nothing cancels)
+    if grad_loss is not None:
+        p = p * grad_loss[rows].double()[:, None]
+    f = scale * logit_scale
+    gh, gw = f * (p @ w), f * (p.t() @ h)
+    sh, sw = abs(f) * (p.abs() @ w.abs()), abs(f) * (p.abs().t() @ h.abs())
+    term = abs(logit_scale) * (h.abs() @ w.abs().t()).amax(1) if rows.numel() else z.sum(1)
+    N, D = hidden.shape
+    out = []
+    for x, shape in ((loss, (N,)), (lse, (N,)), (gh, (N, D)), (term, (N,)), (sh, (N, D))):
+        full = torch.zeros(shape, dtype=torch.float64, device=DEV)
+        full[rows] = x
+        out.append(full)
+    loss, lse, gh, term, sh = out
+    return loss, lse, gh, gw, term, sh, sw
+
+
+def check_loss(loss, lse, ref, D):
+    """A logit is a sum of D exact products in fp32: off by at most about sqrt(D) roundings (2^-24) of the sum of their
+    magnitudes (a random walk; four times that is allowed); loss and lse differ by twice that and by a few fp32
+    roundings of their own value."""
+    rl, rs, term = ref[0], ref[1], ref[4]
+    allow = 8 * 2.0 ** -24 * math.sqrt(D) * term
+    assert ((loss.double() - rl).abs() <= allow + 2.0 ** -20 * rl.abs() + 1e-30).all(), (loss.double() - rl).abs().max()
+    assert ((lse.double() - rs).abs() <= allow + 2.0 ** -20 * rs.abs() + 1e-30).all(), (lse.double() - rs).abs().max()
+
+
+def check_grad(got, want, terms, D, term):
+    """dz is rounded to bf16 (8 bits: 2^-8 of each term) and so is the result (2^-8 of it); the probabilities carry the
+    error of the logits (see check_loss).  What lies below fp32's range (2^-126 each, times the scales) is lost: 1e-30."""
+    p_err = 8 * 2.0 ** -24 * math.sqrt(D) * float(term.max()) + 2.0 ** -20
+    bound = 2.0 ** -8 * want.abs() + (2.0 ** -8 + p_err) * 1.01 * terms + 1e-30
+    err = (got.double() - want).abs()
+    assert (err <= bound).all(), (float((err - bound).max()), float(err.max()))
+    # the roundings are independent: together far less than the bound above
+    assert float(err.norm()) <= (2.0 ** -8 + 2 * p_err) * float(want.norm()) + 1e-30
+
+
+def run_all(hidden, weight, targets, logit_scale=1.0, grad_loss=None, scale=1.0):
+    loss, lse = sip.sip_xent_forward(hidden, weight, targets, logit_scale)
+    gh, gw = sip.sip_xent_backward(hidden, weight, targets, loss, lse, grad_loss, scale, logit_scale)
+    return loss, lse, gh, gw
+
+
+def check_all(hidden, weight, targets, logit_scale=1.0, grad_loss=None, scale=1.0):
+    got = run_all(hidden, weight, targets, logit_scale, grad_loss, scale)
+    ref = reference(hidden, weight, targets, logit_scale, grad_loss, scale)
+    D = hidden.shape[1]
+    check_loss(got[0], got[1], ref, D)
+    check_grad(got[2], ref[2], ref[5], D, ref[4])
+    check_grad(got[3], ref[3], ref[6], D, ref[4])
+    return got
+
+
+SHAPES = [(1, 1, 8), (1, 2, 8), (2, 31, 16), (1, 1000, 64), (5, 257, 24), (31, 256, 32), (33, 300, 40), (64, 1024, 64),
+          (65, 4097, 72), (127, 999, 136), (129, 513, 264), (257, 2049, 520), (300, 5000, 1032), (513, 1031, 96),
+          (1025, 700, 200), (2, 40000, 128), (70, 33000, 64)]
+
+
+@pytest.mark.parametrize("N,V,D", SHAPES)
+def test_loss_and_gradients(N, V, D):
+    check_all(*make(N, V, D, seed=N + V + D), scale=1.0 / N)
+
+
+@pytest.mark.parametrize("N,V,D,masked", [(1, 50, 16, 1.0), (40, 300, 64, 0.5), (300, 1000, 128, 0.9), (600, 777, 72, 0.1),
+                                          (700, 300, 64, 1.0)])
+def test_masked_tokens(N, V, D, masked):
+    """Masked rows leave loss, lse and grad_hidden at zero, whatever they hold."""
+    hidden, weight, targets = make(N, V, D, seed=3, masked=masked)
+    off = torch.tensor([-100, -1, V, 2 ** 31 - 1, -2 ** 31], dtype=torch.int32, device=DEV)
+    targets = torch.where(targets < 0, off[torch.arange(N, device=DEV) % 5], targets)
+    dirty = hidden.clone()
+    bad = torch.tensor([math.nan, math.inf, -math.inf], dtype=torch.bfloat16, device=DEV)
+    gone = (targets < 0) | (targets >= V)
+    dirty[gone] = bad[torch.arange(int(gone.sum()), device=DEV) % 3][:, None].expand(-1, D)
+    g = torch.randn(N, generator=torch.Generator().manual_seed(5)).to(DEV)
+    dirty_g = torch.where(gone, math.nan, g)
+    got = run_all(dirty, weight, targets, 1.0, dirty_g)
+    want = run_all(hidden, weight, targets, 1.0, g)
+    for a, b in zip(got, want):
+        assert torch.equal(a, b)
+    assert not got[0][gone].any() and not got[1][gone].any() and not got[2][gone].any()
+    clean = torch.where(gone[:, None], torch.zeros_like(hidden), hidden)
+    check_all(clean, weight, targets, 1.0, g)
+
+
+def test_every_row_masked_gives_zeros():
+    hidden, weight, targets = make(100, 200, 64)
+    got = run_all(hidden, weight, torch.full_like(targets, -1))
+    for x in got:
+        assert not x.any()
+
+
+@pytest.mark.parametrize("logit_scale,scale", [(1.25, 0.01), (0.5, -2.0), (2.0, 1e-4)])
+def test_scales_and_weights(logit_scale, scale):
+    hidden, weight, targets = make(200, 1500, 128, seed=8, masked=0.2)
+    g = torch.randn(200, generator=torch.Generator().manual_seed(1)).to(DEV)
+    g[::7] = 0.0
+    check_all(hidden, weight, targets, logit_scale, g, scale)
+
+
+def test_strides_of_every_matrix():
+    N, V, D = 150, 700, 104
+    hidden, weight, targets = make(N, V, D, seed=4, h_pad=24, w_pad=40)
+    loss, lse = sip.sip_xent_forward(hidden, weight, targets)
+    ref = reference(hidden, weight, targets)
+    check_loss(loss, lse, ref, D)
+    gh = torch.full((N, D + 16), 9.0, dtype=torch.bfloat16, device=DEV)
+    gw = torch.full((V, D + 8), 9.0, dtype=torch.bfloat16, device=DEV)
+    sip.sip_xent_backward(hidden, weight, targets, loss, lse, grad_hidden=gh[:, :D], grad_weight=gw[:, :D])
+    check_grad(gh[:, :D], ref[2], ref[5], D, ref[4])
+    check_grad(gw[:, :D], ref[3], ref[6], D, ref[4])
+    assert (gh[:, D:] == 9.0).all() and (gw[:, D:] == 9.0).all()
+
+
+def test_one_gradient_alone_is_the_same():
+    hidden, weight, targets = make(90, 800, 64, masked=0.3)
+    loss, lse, gh, gw = run_all(hidden, weight, targets)
+    a, none = sip.sip_xent_backward(hidden, weight, targets, loss, lse, want_weight=False)
+    assert none is None and torch.equal(a, gh)
+    none, b = sip.sip_xent_backward(hidden, weight, targets, loss, lse, want_hidden=False)
+    assert none is None and torch.equal(b, gw)
+
+
+def test_gradient_against_differences():
+    """Central differences of the loss in 64 bits, element by element of a small head."""
+    N, V, D, s = 4, 37, 16, 0.7
+    hidden, weight, targets = make(N, V, D, seed=11)
+    g = torch.tensor([1.0, -0.5, 2.0, 0.25], device=DEV)
+    _, _, gh, gw = run_all(hidden, weight, targets, s, g, 0.3)
+    h64, w64, t = hidden.double(), weight.double(), targets.long()
+
+    def f(h, w):
+        z = s * (h @ w.t())
+        return 0.3 * (g.double() * (torch.logsumexp(z, 1) - z.gather(1, t[:, None])[:, 0])).sum()
+
+    e = 1e-5
+    ref = reference(hidden, weight, targets, s, g, 0.3)
+    for x, got, terms in ((h64, gh, ref[5]), (w64, gw, ref[6])):
+        diff = torch.empty_like(x)
+        for i in range(x.shape[0]):
+            for j in range(x.shape[1]):
+                keep = x[i, j].clone()
+                x[i, j] = keep + e
+                up = f(h64, w64)
+                x[i, j] = keep - e
+                diff[i, j] = (up - f(h64, w64)) / (2 * e)
+                x[i, j] = keep
+        # 1e-8: the differences' own error (e^2 of a third derivative, 1e-16 / e of rounding)
+        assert ((got.double() - diff).abs() <= 2.0 ** -8 * diff.abs() + 2.0 ** -8 * terms + 1e-8).all()
+
+
+def test_nearly_certain_tokens_keep_their_accuracy():
+    """Logits of 0 and one of L at the target: loss = ln(1 + (V - 1) e^-L), and the gradient's factor -(1 - e^-loss)."""
+    V, D = 5000, 8
+    L = torch.tensor([2.0, 10.0, 20.0, 30.0], dtype=torch.float64)
+    hidden = torch.zeros(4, D, dtype=torch.bfloat16)
+    hidden[:, 0] = L.bfloat16()
+    weight = torch.zeros(V, D, dtype=torch.bfloat16)
+    weight[1234, 0] = 1.0
+    t = torch.full((4,), 1234, dtype=torch.int32, device=DEV)
+    loss, lse = sip.sip_xent_forward(hidden.to(DEV), weight.to(DEV), t)
+    want = torch.log1p((V - 1) * (-L).exp())
+    assert ((loss.cpu().double() - want).abs() <= 4e-6 * want).all()
+    gh, _ = sip.sip_xent_backward(hidden.to(DEV), weight.to(DEV), t, loss, lse)
+    assert ((gh[:, 0].cpu().double() - torch.expm1(-want)).abs() <= (2.0 ** -8 + 1e-5) * -torch.expm1(-want)).all()
+    assert not gh[:, 1:].any()
+
+
+def test_large_logits_do_not_overflow():
+    hidden, weight, targets = make(20, 400, 64, seed=2)
+    for s in (300.0, -300.0):
+        check_all(hidden, weight, targets, s)
+
+
+def test_infinite_and_nan_logits_stay_in_their_row():
+    hidden, weight, targets = make(70, 400, 64, seed=2)
+    loss, lse = sip.sip_xent_forward(hidden, weight, targets)
+    dirty = hidden.clone()
+    dirty[3] = math.nan
+    dirty[40, 5] = math.inf
+    l2, s2 = sip.sip_xent_forward(dirty, weight, targets)
+    keep = torch.ones(70, dtype=torch.bool, device=DEV)
+    keep[3] = keep[40] = False
+    assert torch.equal(l2[keep], loss[keep]) and torch.equal(s2[keep], lse[keep])
+    assert l2[3].isnan() and s2[3].isnan() and not s2[40].isfinite()
+
+
+def test_same_bits_on_every_call_and_on_another_stream():
+    hidden, weight, targets = make(333, 3001, 264, masked=0.2)
+    first = run_all(hidden, weight, targets)
+    side = torch.cuda.Stream()
+    for _ in range(3):
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            again = run_all(hidden, weight, targets)
+        side.synchronize()
+        for a, b in zip(first, again):
+            assert torch.equal(a, b)
+
+
+def test_workspace_and_outputs_stay_within_their_bounds():
+    N, V, D = 77, 1003, 72
+    hidden, weight, targets = make(N, V, D, masked=0.3)
+    need = sip.sip_xent_workspace_bytes(N, V, D, True)
+    buf = torch.full((need + 4096,), 0xA5, dtype=torch.uint8, device=DEV)
+    outs = [torch.full((n + 512,), 3.0, dtype=d, device=DEV) for n, d in
+            ((N, torch.float32), (N, torch.float32), (N * D, torch.bfloat16), (V * D, torch.bfloat16))]
+    loss, lse = outs[0][:N], outs[1][:N]
+    sip.sip_xent_forward(hidden, weight, targets, loss=loss, lse=lse, workspace=buf[:need])
+    sip.sip_xent_backward(hidden, weight, targets, loss, lse, grad_hidden=outs[2][:N * D].view(N, D),
+                          grad_weight=outs[3][:V * D].view(V, D), workspace=buf[:need])
+    want = run_all(hidden, weight, targets)
+    assert (buf[need:] == 0xA5).all()
+    for o, n, x in zip(outs, (N, N, N * D, V * D), want):
+        assert torch.equal(o[:n], x.reshape(-1)) and (o[n:] == 3.0).all()
+
+
+def test_recorded_in_a_graph():
+    hidden, weight, targets = make(50, 600, 64, masked=0.2)
+    ws = torch.empty(sip.sip_xent_workspace_bytes(50, 600, 64, True), dtype=torch.uint8, device=DEV)
+    loss, lse = torch.empty(50, device=DEV), torch.empty(50, device=DEV)
+    gh, gw = torch.empty_like(hidden), torch.empty_like(weight)
+
+    def step():
+        sip.sip_xent_forward(hidden, weight, targets, loss=loss, lse=lse, workspace=ws)
+        sip.sip_xent_backward(hidden, weight, targets, loss, lse, grad_hidden=gh, grad_weight=gw, workspace=ws)
+
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for seed in range(3):
+        h, w, t = make(50, 600, 64, seed=seed, masked=0.3)
+        hidden.copy_(h), weight.copy_(w), targets.copy_(t)
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [x.clone() for x in (loss, lse, gh, gw)]
+        for a, b in zip(got, run_all(hidden, weight, targets)):
+            assert torch.equal(a, b)
+
+
+def test_weights_beyond_four_gigabytes():
+    """Targets in the last rows of a weight of 2^32 bytes and more."""
+    V, D, N = 262300, 8192, 3
+    weight = torch.zeros(V, D, dtype=torch.bfloat16, device=DEV)
+    g = torch.Generator(device=DEV).manual_seed(1)
+    at = torch.tensor([0, 100000, 200000, V - 300, V - 1], device=DEV)
+    weight[at] = (torch.randn(5, D, generator=g, device=DEV) * 0.02).bfloat16()
+    hidden = torch.randn(N, D, generator=g, device=DEV).bfloat16()
+    targets = torch.tensor([V - 1, V - 300, 100000], dtype=torch.int32, device=DEV)
+    loss, lse, gh, gw = run_all(hidden, weight, targets)
+    z = hidden.double() @ weight[at].double().t()
+    want = torch.log(z.exp().sum(1) + (V - 5))
+    zt = z[torch.arange(3), torch.tensor([4, 3, 1])]
+    assert ((lse.double() - want).abs() <= 1e-5).all() and ((loss.double() - (want - zt)).abs() <= 1e-5).all()
+    p = (z - want[:, None]).exp()
+    p[torch.arange(3), torch.tensor([4, 3, 1])] -= 1.0
+    gw_want = p.t() @ hidden.double()
+    assert float((gw[at].double() - gw_want).norm()) <= 2.0 ** -8 * float(gw_want.norm())
+    gh_want = p @ weight[at].double()
+    assert float((gh.double() - gh_want).norm()) <= 2.0 ** -8 * float(gh_want.norm())
