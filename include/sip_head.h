@@ -96,7 +96,7 @@ sip_status sip_xent_backward(const void* hidden, int32_t N, int32_t D, int64_t h
 typedef struct {
   const void* grad;
   void* out;
-  int64_t count;                     /* elements, 0 .. 2^40                                          */
+  int64_t count;                     /* elements, 0 .. 2^40; of all tensors together up to 2^44      */
   sip_dtype dtype;
 } sip_grad;
 

@@ -1,11 +1,11 @@
 // A vocabulary head of 4-bit codes with group scales: the quantiser, and the product with hidden states.
 #pragma once
+#include <type_traits>
+
 #include "sip_gemm.h"
 
 namespace sip {
 
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 struct CodesArgs {
   const uint16_t* weight; long long weight_stride;     // quantiser: in
@@ -17,97 +17,586 @@ struct CodesArgs {
   const void* hidden; long long hidden_stride; int hidden_bf16;
   int B;
   void* logits; long long logits_stride; int logits_bf16;
+  char* states;                                        // workspace: see ManyLayout
 };
 
-__device__ inline float scale_at(const CodesArgs& p, long long i) {
-  return p.scales_bf16 ? __builtin_bit_cast(float, (uint32_t)static_cast<const uint16_t*>(p.scales)[i] << 16)
-                       : static_cast<const float*>(p.scales)[i];
-}
-
-// A thread quantises a group.
+// Eight weights a lane, a group in group / 8 neighbouring lanes: its bounds by exchange between them.  Reads 16 bytes a lane
+// and writes 4.  What a lane computes -- eight IEEE divisions above all -- takes less time than its share of the reads.
+template <int GROUP>
 __global__ __launch_bounds__(256) void quantize_kernel(CodesArgs p) {
-  const int groups = p.D / p.group;
-  const long long id = (long long)blockIdx.x * 256 + threadIdx.x;
-  if (id >= (long long)p.V * groups) return;
-  const int v = (int)(id / groups), g = (int)(id % groups);
-  const uint16_t* w = p.weight + v * p.weight_stride + g * p.group;
-  float lo = 0.0f, hi = 0.0f;
-  for (int e = 0; e < p.group; ++e) {
-    const float x = __builtin_bit_cast(float, (uint32_t)w[e] << 16);
-    lo = fminf(lo, x);
-    hi = fmaxf(hi, x);
-  }
-  float s = p.zeros ? (hi - lo) / 15.0f : fmaxf(hi, -lo) / 7.0f;
-  if (p.scales_bf16) s = (float)(__bf16)s;
-  if (s == 0.0f) s = 1.0f;
-  const float zero = p.zeros ? fminf(fmaxf(rintf(-lo / s), 0.0f), 15.0f) : 8.0f;
-  if (p.scales_bf16) static_cast<__bf16*>(p.scales)[id] = (__bf16)s;
-  else static_cast<float*>(p.scales)[id] = s;
-  if (p.zeros) p.zeros[id] = (uint8_t)zero;
-  uint8_t* c = p.codes + v * p.codes_stride + g * (p.group / 2);
-  for (int e = 0; e < p.group; e += 2) {
-    int q[2];
-    for (int h = 0; h < 2; ++h) {
-      const float x = __builtin_bit_cast(float, (uint32_t)w[e + h] << 16);
-      q[h] = (int)fminf(fmaxf(rintf(x / s) + zero, 0.0f), 15.0f);
+  const uint32_t per_row = (uint32_t)p.D / 8, total = (uint32_t)p.V * per_row;              // (below 2^31)
+  const uint32_t lanes = (total + 63) & ~63u, step = gridDim.x * 256u;
+  for (uint32_t id = blockIdx.x * 256 + threadIdx.x; id < lanes; id += step) {
+    const bool live = id < total;
+    const uint32_t v = live ? id / per_row : 0, c = live ? id - v * per_row : 0;
+    const u32x4 w = *reinterpret_cast<const u32x4*>(p.weight + v * p.weight_stride + c * 8);
+    float x[8], lo = 0.0f, hi = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      x[e] = __builtin_bit_cast(float, e & 1 ? w[e >> 1] & 0xffff0000u : w[e >> 1] << 16);
+      lo = fminf(lo, x[e]);
+      hi = fmaxf(hi, x[e]);
     }
-    c[e / 2] = (uint8_t)(q[0] | (q[1] << 4));
+#pragma unroll
+    for (int d = 1; d < GROUP / 8; d <<= 1) {
+      lo = fminf(lo, __shfl_xor(lo, d));
+      hi = fmaxf(hi, __shfl_xor(hi, d));
+    }
+    float s = p.zeros ? (hi - lo) / 15.0f : fmaxf(hi, -lo) / 7.0f;
+    if (p.scales_bf16) s = (float)(__bf16)s;
+    if (s == 0.0f) s = 1.0f;
+    const float zero = p.zeros ? fminf(fmaxf(rintf(-lo / s), 0.0f), 15.0f) : 8.0f;
+    uint32_t q = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) q |= (uint32_t)fminf(fmaxf(rintf(x[e] / s) + zero, 0.0f), 15.0f) << (4 * e);
+    if (live) {
+      *reinterpret_cast<uint32_t*>(p.codes + v * p.codes_stride + c * 4) = q;
+      if (c % (GROUP / 8) == 0) {
+        const long long at = (long long)v * (per_row / (GROUP / 8)) + c / (GROUP / 8);
+        if (p.scales_bf16) static_cast<__bf16*>(p.scales)[at] = (__bf16)s;
+        else static_cast<float*>(p.scales)[at] = s;
+        if (p.zeros) p.zeros[at] = (uint8_t)zero;
+      }
+    }
   }
 }
 
 // Eight codes of a dword as the bf16 values 16 + q (q in the mantissa's bits 3 to 6 over the exponent of 16), in the
 // order 0 4 1 5 2 6 3 7: no conversion, one shift and one and-or for a pair.
-__device__ inline u32x4 code_values(uint32_t c) {
-  constexpr uint32_t kMask = 0x00780078u, k16 = 0x41804180u;
-  u32x4 r;
-  r[0] = ((c << 3) & kMask) | k16;
-  r[1] = ((c >> 1) & kMask) | k16;
-  r[2] = ((c >> 5) & kMask) | k16;
-  r[3] = ((c >> 9) & kMask) | k16;
-  return r;
+// (The constants from registers that the compiler cannot see through: it then has an instruction for the and-or.)
+struct CodeValues {
+  uint32_t mask, k16;
+  __device__ CodeValues() {
+    asm("s_mov_b32 %0, 0x00780078" : "=s"(mask));
+    asm("v_mov_b32 %0, 0x41804180" : "=v"(k16));
+  }
+  __device__ u32x4 operator()(uint32_t c) const {
+    u32x4 r;
+    r[0] = ((c << 3) & mask) | k16;
+    r[1] = ((c >> 1) & mask) | k16;
+    r[2] = ((c >> 5) & mask) | k16;
+    r[3] = ((c >> 9) & mask) | k16;
+    return r;
+  }
+};
+
+// ---- few rows: the head is read once, and nothing else takes as long
+
+constexpr int kFewWaves = 8;
+#define SIP_GLOBAL __attribute__((address_space(1)))
+template <class T, int N> struct __attribute__((packed)) Packed { T w[N]; };
+
+// WORDS * 4 bytes from any address on, as the aligned words they lie in: a load of several words from an odd place takes twice the
+// time.  `odd`: whether there are such places (uniform); where not, the one more word that they need is not read.  (That word
+// holds a byte that is wanted, or it is the last one once more: nothing behind the array is touched.)
+template <int WORDS>
+struct Unaligned {
+  uint32_t w[WORDS], more, shift;
+
+  __device__ void load(const SIP_GLOBAL uint8_t* from, bool odd) {
+    const uint64_t at = (uint64_t)from;
+    shift = (uint32_t)(at & 3) * 8;
+    const auto* words = (const SIP_GLOBAL Packed<uint32_t, WORDS>*)(at & ~3ull);
+#pragma unroll
+    for (int i = 0; i < WORDS; ++i) w[i] = words->w[i];
+    more = 0;
+    if (odd) more = *((const SIP_GLOBAL uint32_t*)words + (shift ? WORDS : WORDS - 1));
+  }
+  __device__ void get(uint32_t (&out)[WORDS]) const {
+#pragma unroll
+    for (int i = 0; i < WORDS; ++i) out[i] = __builtin_amdgcn_alignbit(i + 1 < WORDS ? w[i + 1] : more, w[i], shift);
+  }
+};
+
+// Scales and zero points of N neighbouring groups, aligned to their element; whole words of them if there are any.
+__device__ const uint32_t kEights[8] = {0x08080808u, 0x08080808u, 0x08080808u, 0x08080808u,
+                                        0x08080808u, 0x08080808u, 0x08080808u, 0x08080808u};   // a head without zero points
+template <int N, int BYTES>
+struct Elements {                        // N of BYTES each
+  static constexpr bool kWhole = N * BYTES % 4 == 0;
+  static constexpr int kWords = kWhole ? N * BYTES / 4 : 1;
+  typedef std::conditional_t<BYTES == 1, uint8_t, uint16_t> Single;
+  // (singles as wide as they were read: widened before its time, a load under way would be waited for)
+  Unaligned<kWords> read;
+  Single single[N];
+  uint32_t words[kWords];
+
+  __device__ void load(const SIP_GLOBAL uint8_t* from, bool odd) {
+    if constexpr (kWhole) read.load(from, odd);
+    else
+#pragma unroll
+      for (int i = 0; i < N; ++i) single[i] = ((const SIP_GLOBAL Single*)from)[i];
+  }
+  __device__ uint32_t get(int i) const {         // after settle()
+    if constexpr (!kWhole) return single[i];
+    const uint32_t word = words[i * BYTES / 4];
+    return BYTES == 4 ? word : (word >> (i * BYTES % 4 * 8)) & (BYTES == 1 ? 0xffu : 0xffffu);
+  }
+  __device__ void settle() {
+    if constexpr (kWhole) read.get(words);
+  }
+};
+template <int N, bool SCALES_BF16>
+struct GroupScales {
+  Elements<N, SCALES_BF16 ? 2 : 4> s;
+  Elements<N, 1> z;
+
+  __device__ void settle() { s.settle(); z.settle(); }
+  __device__ float scale(int g) const {
+    if constexpr (SCALES_BF16) return __builtin_bit_cast(float, s.get(g) << 16);
+    else return __builtin_bit_cast(float, s.get(g));
+  }
+  __device__ float zero(int g) const { return (float)z.get(g); }
+};
+
+// How a wave of UNITS * 128 entries reads its codes.  Units in pairs: of a row's 128 bytes a lane takes 16 at 32 * quad and the 16
+// behind, so that a load touches whole lines (half lines are as many requests for half as much); a last unit without a
+// partner: 16 at 16 * quad.  Dwords are then exchanged between the quarters of the wave until the four of a product hold
+// entries of one group: between its halves (group 128), or as a 4 x 4 transposition; a unit alone needs less.
+template <int GROUP, int UNITS>
+struct UnitOrder {
+  static __device__ constexpr bool paired(int u) { return (u | 1) < UNITS; }
+  // byte of load u, from the row's first one in the wave's window on
+  static __device__ int byte_of(int u, int quad) { return paired(u) ? (u >> 1) * 128 + quad * 32 + (u & 1) * 16 : u * 64 + quad * 16; }
+  // entry at which the eight of dword j of load u begin, after order()
+  static __device__ int entry_of(int u, int j, int quad) {
+    if (paired(u))
+      return (u >> 1) * 256 + (u & 1) * 32 +
+             (GROUP == 128 ? (2 * (j >> 1) + (quad & 1)) * 64 + ((j & 1) + 2 * (quad >> 1)) * 8 : j * 64 + quad * 8);
+    return u * 128 + (GROUP == 128 ? 32 * quad + 8 * j
+                      : GROUP == 64 ? 64 * (j >> 1) + 32 * (quad & 1) + 8 * ((j & 1) + 2 * (quad >> 1)) : 32 * j + 8 * quad);
+  }
+  static __device__ u32x4 order(int u, u32x4 c) {
+    if (GROUP == 128 && !paired(u)) return c;
+    const u32x2 a = __builtin_amdgcn_permlane32_swap(c[0], c[2], false, false), b = __builtin_amdgcn_permlane32_swap(c[1], c[3], false, false);
+    if (GROUP == (paired(u) ? 128 : 64)) return u32x4{a[0], b[0], a[1], b[1]};
+    const u32x2 l = __builtin_amdgcn_permlane16_swap(a[0], b[0], false, false), h = __builtin_amdgcn_permlane16_swap(a[1], b[1], false, false);
+    return u32x4{l[0], l[1], h[0], h[1]};
+  }
+  // group of dword j of load u, counted in the window
+  static __device__ constexpr int group_of(int u, int j) {
+    return paired(u) ? ((u >> 1) * 256 + (u & 1) * 32 + j * 64) / GROUP : (u * 128 + j * 32) / GROUP;
+  }
+};
+
+// Row r of the hidden states as the products take them, eight entries from k on in the order of CodeValues; zeros if not
+// `wanted`.  A bf16 state is a row; an fp32 one is three, of 8 bits each: all 24.
+__device__ inline bf16x8 hidden_row(const CodesArgs& p, int r, int k, bool wanted) {
+  u32x4 out;
+  if (p.hidden_bf16) {
+    u32x4 w = {0, 0, 0, 0};
+    if (wanted) w = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(p.hidden) + r * p.hidden_stride + k);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) out[e] = e & 1 ? (w[e >> 1] >> 16) | (w[(e >> 1) + 2] & 0xffff0000u) : (w[e >> 1] & 0xffffu) | (w[(e >> 1) + 2] << 16);
+  } else {
+    const int b = r / 3, part = r - 3 * b;
+    const float* from = static_cast<const float*>(p.hidden) + b * p.hidden_stride + k;
+    uint32_t bits[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      float x = wanted ? from[e] : 0.0f;
+      for (int i = 0; i < 2; ++i)
+        if (i < part) x -= __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, x) & 0xffff0000u);
+      bits[e] = __builtin_bit_cast(uint32_t, x) >> 16;
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) out[e] = bits[e] | (bits[e + 4] << 16);
+  }
+  return __builtin_bit_cast(bf16x8, out);
+}
+__host__ __device__ inline int rows_of_state(bool hidden_bf16) { return hidden_bf16 ? 1 : 3; }
+
+// Tiles a turn: as many as leave room in the registers beside the states (16 registers a unit and row of tiles).
+constexpr int few_tiles(int group, bool scales_bf16, int units, int mt) {
+  const int bytes = units * 128 / group * (scales_bf16 ? 3 : 5), states = 16 * units * mt;
+  for (int nt = 4; nt > 1; nt /= 2)
+    if (states + nt * (4 * units + 2 * ((bytes + 3) / 4) + 8 * mt) <= 200) return nt;
+  return 1;
 }
 
-// A wave makes the logits of 16 rows and 16 vocabulary entries.  fp32 hidden states enter as three bf16 parts.
-__global__ __launch_bounds__(64) void head_logits_kernel(CodesArgs p) {
-  const int lane = threadIdx.x, v = blockIdx.y * 16 + (lane & 15), b = blockIdx.x * 16 + (lane & 15), q4 = lane >> 4;
-  const int groups = p.D / p.group;
-  const uint8_t* codes = p.codes + min(v, p.V - 1) * p.codes_stride;
-  const char* x_row = static_cast<const char*>(p.hidden) + min(b, p.B - 1) * p.hidden_stride * (p.hidden_bf16 ? 2 : 4);
-  f32x4 total{};
-  for (int g = 0; g < groups; ++g) {
-    const long long at = (long long)min(v, p.V - 1) * groups + g;
-    const float s = scale_at(p, at), zero = 16.0f + (p.zeros ? (float)p.zeros[at] : 8.0f);
-    f32x4 acc{}, sum{};
-    for (int k = g * p.group; k < (g + 1) * p.group; k += 32) {
-      const u32x4 cv = code_values(*reinterpret_cast<const uint32_t*>(codes + k / 2 + q4 * 4));
-      float x[8];
-      for (int e = 0; e < 8; ++e) {
-        const int at_e = k + q4 * 8 + (e >> 1) + 4 * (e & 1);
-        x[e] = p.hidden_bf16 ? __builtin_bit_cast(float, (uint32_t)reinterpret_cast<const uint16_t*>(x_row)[at_e] << 16)
-                             : reinterpret_cast<const float*>(x_row)[at_e];
+// Up to 16 * MT rows (hidden_row()), D from 128 on.  A workgroup a compute unit, which takes NT tiles of 16 vocabulary entries a turn; a
+// wave keeps its eighth of the hidden states -- up to UNITS units of 128 entries -- in registers for all turns, reads its
+// eighth of the tiles' codes, loading the next turn's into the registers it has just used, and the eight waves' sums meet
+// in LDS.  Codes are the only thing read in quantity, 8 * NT * UNITS KB ahead of their use on each compute unit.
+// A wave's window has UNITS units whatever its share; where that is more, it begins earlier if it would end behind the row,
+// and what is another wave's share meets zeros.  (All waves have the same loads, and a wait for one can be told by
+// how many came after it.)
+// Products: 16 + q against the states, from - (16 + zero) times the group's sum of the states on; the scale on the fp32
+// sum of a group.
+template <int GROUP, bool SCALES_BF16, int UNITS, int MT>
+__global__ __launch_bounds__(kFewWaves * 64) void head_few_kernel(CodesArgs p) {
+  constexpr int NT = few_tiles(GROUP, SCALES_BF16, UNITS, MT);
+  constexpr int kGroups = UNITS * 128 / GROUP;                          // of the window
+  typedef UnitOrder<GROUP, UNITS> Order;
+  __shared__ f32x4 sums[kFewWaves][kGroups][MT][4];                     // of the hidden states by group, as the accumulators lie
+  __shared__ f32x4 part[2][kFewWaves][NT * MT][64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), quad = lane >> 4;
+  const int units = (p.D + 127) / 128, groups = p.D / GROUP;
+  const int mine = wave * units / kFewWaves * 128, others = (wave + 1) * units / kFewWaves * 128;   // my share: [mine, others)
+  const int first = min(mine, p.D - UNITS * 128);                       // of the window
+  const bool last = others - mine == UNITS * 128;                        // whether the last unit is mine
+  const int turns = (p.V + 16 * NT - 1) / (16 * NT);
+
+  u32x4 codes[NT][UNITS];
+  GroupScales<kGroups, SCALES_BF16> scales[NT], next[NT];
+  const SIP_GLOBAL uint8_t* my_codes = (const SIP_GLOBAL uint8_t*)p.codes + first / 2;
+  const SIP_GLOBAL uint8_t* zeros = (const SIP_GLOBAL uint8_t*)(p.zeros ? p.zeros : reinterpret_cast<const uint8_t*>(kEights));
+  const uint32_t stride = (uint32_t)p.codes_stride, zeros_mask = p.zeros ? ~0u : 0u;
+  constexpr int kScaleBytes = SCALES_BF16 ? 2 : 4;
+  const SIP_GLOBAL uint8_t* scale_bytes = (const SIP_GLOBAL uint8_t*)p.scales;
+  const bool odd_scales = (((uint64_t)scale_bytes | (uint64_t)(groups * kScaleBytes) | (uint64_t)(first / GROUP * kScaleBytes)) & 3) != 0;
+  const bool odd_zeros = p.zeros && (((uint64_t)p.zeros | (uint64_t)groups | (uint64_t)(first / GROUP)) & 3) != 0;
+  int step = gridDim.x;
+  asm("" : "+s"(step));                                    // (read once: a load per use is what the compiler prefers)
+  auto row_of = [&](int t, int turn) { return (uint32_t)min((turn * NT + t) * 16 + (lane & 15), p.V - 1); };
+  auto load = [&](int t, int u, int turn) {
+    codes[t][u] = *(const SIP_GLOBAL u32x4*)(my_codes + (uint64_t)row_of(t, turn) * stride + Order::byte_of(u, quad));
+  };
+  auto load_scales = [&](int t, int turn) {
+    const uint32_t at = row_of(t, turn) * groups + first / GROUP;       // (below 2^28)
+    next[t].s.load(scale_bytes + at * (uint32_t)kScaleBytes, odd_scales);
+    next[t].z.load(zeros + (at & zeros_mask), odd_zeros);
+  };
+#pragma unroll
+  for (int t = 0; t < NT; ++t) load_scales(t, blockIdx.x);
+#pragma unroll
+  for (int u = 0; u < UNITS; ++u)
+#pragma unroll
+    for (int t = 0; t < NT; ++t) load(t, u, blockIdx.x);
+
+  const int each = rows_of_state(p.hidden_bf16), rows = p.B * each;
+  bf16x8 x[UNITS][4][MT];
+#pragma unroll
+  for (int m = 0; m < MT; ++m) {
+#pragma unroll
+    for (int u = 0; u < UNITS; ++u)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int k = first + Order::entry_of(u, j, quad);
+        x[u][j][m] = hidden_row(p, min(m * 16 + (lane & 15), rows - 1), k, k >= mine && k < others && k < p.D);
       }
-      u32x4 ones;
-      for (int e = 0; e < 4; ++e) ones[e] = 0x3f803f80u;
-      for (int part = 0; part < (p.hidden_bf16 ? 1 : 3); ++part) {
-        u32x4 xv;
-        for (int e = 0; e < 8; e += 2) {
-          const uint32_t h0 = __builtin_bit_cast(uint32_t, x[e]) & 0xffff0000u, h1 = __builtin_bit_cast(uint32_t, x[e + 1]) & 0xffff0000u;
-          xv[e / 2] = (h0 >> 16) | h1;
-          x[e] -= __builtin_bit_cast(float, h0);
-          x[e + 1] -= __builtin_bit_cast(float, h1);
+#pragma unroll
+    for (int g = 0; g < kGroups; ++g) {
+      const u32x4 ones = {0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
+      f32x4 sum = {};
+#pragma unroll
+      for (int u = 0; u < UNITS; ++u)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (Order::group_of(u, j) == g)
+            sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[u][j][m], __builtin_bit_cast(bf16x8, ones), sum, 0, 0, 0);
+      if ((lane & 15) == 0) sums[wave][g][m][quad] = sum;
+    }
+  }
+  // (a wave reads what it wrote itself)
+  const CodeValues code_values;
+  int side = 0;
+  // `more`: whether there is a next turn to load for.
+  auto take = [&](int turn, auto more) {
+    f32x4 total[NT][MT] = {};
+    // the next turn's scales ahead of its codes: loads arrive in the order of their issue, and the scales are wanted first
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      scales[t] = next[t];
+      scales[t].settle();
+      if constexpr (decltype(more)::value) load_scales(t, turn + step);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int u = 0; u < UNITS; u += Order::paired(u) ? 2 : 1) {
+      const int width = Order::paired(u) ? 2 : 1;
+      if (width == 1 && UNITS > 1 && !last) break;         // (a unit alone, another wave's)
+      // two tiles at once: a chain of products waits for its own sums
+#pragma unroll
+      for (int t0 = 0; t0 < NT; t0 += 2) {
+        constexpr int kPair = NT > 1 ? 2 : 1;
+        u32x4 c[kPair][2];
+#pragma unroll
+        for (int t = 0; t < kPair; ++t)
+#pragma unroll
+          for (int e = 0; e < width; ++e) c[t][e] = Order::order(u + e, codes[t0 + t][u + e]);
+        // a group's sums are scaled when the next group's products are under way; the sums of the states are read as far ahead
+        const int first_group = Order::group_of(u, 0), last_group = Order::group_of(u + width - 1, 3);
+        f32x4 acc[2][kPair][MT], sum[2][MT];
+#pragma unroll
+        for (int m = 0; m < MT; ++m) sum[0][m] = sums[wave][first_group][m][quad];
+#pragma unroll
+        for (int g = first_group; g <= last_group + 1; ++g) {
+          const int now = (g - first_group) & 1;
+          if (g < last_group) {
+#pragma unroll
+            for (int m = 0; m < MT; ++m) sum[now ^ 1][m] = sums[wave][g + 1][m][quad];
+          }
+          if (g <= last_group) {
+#pragma unroll
+            for (int t = 0; t < kPair; ++t) {
+              const float zero = -16.0f - scales[t0 + t].zero(g);
+#pragma unroll
+              for (int m = 0; m < MT; ++m) acc[now][t][m] = sum[now][m] * zero;
+#pragma unroll
+              for (int e = 0; e < width; ++e)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                  if (Order::group_of(u + e, j) != g) continue;
+                  const bf16x8 w = __builtin_bit_cast(bf16x8, code_values(c[t][e][j]));
+#pragma unroll
+                  for (int m = 0; m < MT; ++m)
+                    acc[now][t][m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[u + e][j][m], w, acc[now][t][m], 0, 0, 0);
+                }
+            }
+          }
+          __builtin_amdgcn_sched_barrier(0);
+          if (g > first_group) {
+#pragma unroll
+            for (int t = 0; t < kPair; ++t) {
+              const float s = scales[t0 + t].scale(g - 1);
+#pragma unroll
+              for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) total[t0 + t][m][r] = __builtin_fmaf(s, acc[now ^ 1][t][m][r], total[t0 + t][m][r]);
+            }
+          }
         }
-        const bf16x8 xb = __builtin_bit_cast(bf16x8, xv);
-        acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xb, __builtin_bit_cast(bf16x8, cv), acc, 0, 0, 0);
-        sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xb, __builtin_bit_cast(bf16x8, ones), sum, 0, 0, 0);
+        // Here and nowhere else: earlier they would need registers of their own, later they would be waited for.
+        __builtin_amdgcn_sched_barrier(0);
+        if constexpr (decltype(more)::value)
+#pragma unroll
+          for (int t = t0; t < t0 + 2 && t < NT; ++t) {
+#pragma unroll
+            for (int e = 0; e < width; ++e) load(t, u + e, turn + step);
+          }
+        __builtin_amdgcn_sched_barrier(0);
       }
     }
-    for (int r = 0; r < 4; ++r) total[r] = __builtin_fmaf(s, __builtin_fmaf(-zero, sum[r], acc[r]), total[r]);
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int m = 0; m < MT; ++m) part[side][wave][t * MT + m][lane] = total[t][m];
+    __builtin_amdgcn_s_waitcnt(0xC07F);                    // (LDS alone: what was loaded for the next turn stays under way)
+    __builtin_amdgcn_s_barrier();                          // (the other side's sums were read before this turn's)
+    // row r of entry v: quarter (r % 16) / 4, register r % 4
+    for (int o = threadIdx.x; o < NT * 16 * p.B; o += kFewWaves * 64) {
+      const int b = o / (NT * 16), e = o % (NT * 16);
+      float z = 0.0f;
+      for (int r = (b + 1) * each - 1; r >= b * each; --r)
+#pragma unroll
+        for (int w = 0; w < kFewWaves; ++w) z += part[side][w][(e >> 4) * MT + (r >> 4)][((r & 15) >> 2) * 16 + (e & 15)][r & 3];
+      const int v = turn * NT * 16 + e;
+      if (v < p.V) {
+        if (p.logits_bf16) static_cast<__bf16*>(p.logits)[b * p.logits_stride + v] = (__bf16)z;
+        else static_cast<float*>(p.logits)[b * p.logits_stride + v] = z;
+      }
+    }
+    side ^= 1;
+  };
+  // (else the compiler, which takes the loads up to here for still under way, waits for all of them in every turn)
+  __builtin_amdgcn_s_waitcnt(0x0F70);                      // vmcnt(0)
+  int turn = blockIdx.x;
+  for (; turn + step < turns; turn += step) take(turn, std::true_type());
+  take(turn, std::false_type());
+}
+
+// ---- more rows: tiles of the product, the hidden states through LDS
+
+// Rows of a block of MT * 16: as many whole states as fit it.
+constexpr int kManyWaves = 8, kManyTiles = 2, kManyEntries = kManyWaves * kManyTiles * 16;   // vocabulary entries of a workgroup
+__host__ __device__ inline int block_states(int mt, bool hidden_bf16) { return mt * 16 / rows_of_state(hidden_bf16); }
+__host__ __device__ inline int many_units(int D) { return (D + 255) / 256 * 2; }             // of 128 entries
+__host__ __device__ inline int many_groups(int D, int group) { return (D / group + 31) / 32 * 32; }
+
+// The states in the order of the products, by block: [unit][product of the unit][tile of rows][lane], 16 bytes a lane; and behind
+// them the sums of the states by group, in three bf16 parts, as rows of a product over groups: [32 groups][part][tile][lane].
+struct ManyLayout {
+  size_t sums, block;                                     // bytes of a block's states, and of all of it
+  __host__ __device__ ManyLayout(int D, int group, int mt) {
+    sums = (size_t)many_units(D) * 4 * mt * 1024;
+    block = sums + (size_t)many_groups(D, group) / 32 * 3 * mt * 1024;
   }
-  for (int r = 0; r < 4; ++r) {
-    const int row = blockIdx.x * 16 + 4 * q4 + r;
-    if (row < p.B && v < p.V) {
-      if (p.logits_bf16) static_cast<__bf16*>(p.logits)[row * p.logits_stride + v] = (__bf16)total[r];
-      else static_cast<float*>(p.logits)[row * p.logits_stride + v] = total[r];
+};
+
+// A wave takes a tile of 16 rows and a group.
+template <int GROUP>
+__global__ __launch_bounds__(256) void head_rows_kernel(CodesArgs p, int mt) {
+  const int lane = threadIdx.x & 63, quad = lane >> 4, g = blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (g >= many_groups(p.D, GROUP)) return;
+  const int block = blockIdx.y / mt, tile = blockIdx.y % mt, each = rows_of_state(p.hidden_bf16), states = block_states(mt, p.hidden_bf16);
+  const int r = tile * 16 + (lane & 15), state = block * states + r / each;
+  const bool live = r < states * each && state < p.B;
+  const ManyLayout layout(p.D, GROUP, mt);
+  char* out = p.states + block * layout.block;
+  float sum = 0.0f;
+  for (int c = g * (GROUP / 32); c < (g + 1) * (GROUP / 32); ++c) {
+    const int k = c * 32 + quad * 8;
+    const bf16x8 x = hidden_row(p, live ? state * each + r % each : 0, k, live && k < p.D);
+    if (c < many_units(p.D) * 4) *reinterpret_cast<bf16x8*>(out + ((size_t)c * mt + tile) * 1024 + lane * 16) = x;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sum += (float)x[e];
+  }
+  sum += __shfl_xor(sum, 16);
+  sum += __shfl_xor(sum, 32);
+  if (quad == 0) {
+    uint16_t* to = reinterpret_cast<uint16_t*>(out + layout.sums + ((size_t)(g >> 5) * 3 * mt + tile) * 1024 + (((g & 31) >> 3) * 16 + lane) * 16) + (g & 7);
+#pragma unroll
+    for (int part = 0; part < 3; ++part) {
+      const uint32_t top = __builtin_bit_cast(uint32_t, sum) & 0xffff0000u;
+      to[part * mt * 512] = (uint16_t)(top >> 16);
+      sum -= __builtin_bit_cast(float, top);
+    }
+  }
+}
+
+// 256 vocabulary entries by MT * 16 rows.  A wave has 32 of the entries and all rows.  It goes through a pair of units -- 256
+// entries of a state, a line of each row's codes -- at a time: states through LDS, codes and scales straight into registers,
+// all of the next pair's loaded while this one's products are made.
+//   sum_g s (sum_d (16 + q) x - (16 + zero) sum_d x)
+// The second part is a product over groups of its own, in 3 x 3 bf16 parts of which the six that matter are taken: with
+// 8 row tiles it saves 32 multiplications a group and tile of entries.  Matrix cores and vector units are about
+// equally busy with groups of 64.
+template <int GROUP, bool SCALES_BF16, int MT>
+__global__ __launch_bounds__(kManyWaves * 64) void head_many_kernel(CodesArgs p) {
+  constexpr int NT = kManyTiles, kGroups = 256 / GROUP, kPairBytes = 8 * MT * 1024, kLoads = kPairBytes / (kManyWaves * 1024);
+  constexpr int kPitch = kManyEntries + 4;
+  constexpr int kRing = 2 * kPairBytes, kOut = MT * 16 * kPitch * 4;
+  __shared__ __attribute__((aligned(1024))) char lds_bytes[kRing > kOut ? kRing : kOut];
+  SIP_LDS char* lds = (SIP_LDS char*)lds_bytes;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), quad = lane >> 4;
+  const int each = rows_of_state(p.hidden_bf16), states = block_states(MT, p.hidden_bf16), blocks = (p.B + states - 1) / states;
+  // the blocks of one tile of entries on one XCD, one after the other
+  const int tile = (int)(blockIdx.x >> 3) / blocks * 8 + (blockIdx.x & 7), block = (int)(blockIdx.x >> 3) % blocks;
+  if (tile * kManyEntries >= p.V) return;
+  const ManyLayout layout(p.D, GROUP, MT);
+  const char* from = p.states + block * layout.block;
+  const int pairs = many_units(p.D) / 2, groups = p.D / GROUP;
+  const uint32_t lds0 = (uint32_t)(uintptr_t)lds;
+  auto load_states = [&](int pair) {
+    const uint64_t at = reinterpret_cast<uint64_t>(from + (size_t)pair * kPairBytes);
+    const u32x4 buffer = {(uint32_t)at, (uint32_t)(at >> 32) & 0xffff, kPairBytes, 0x00020000};
+#pragma unroll
+    for (int l = 0; l < kLoads; ++l) {
+      const uint32_t piece = (l * kManyWaves + wave) * 1024;
+      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+                   :: "s"(lds0 + (uint32_t)(pair & 1) * kPairBytes + piece), "v"(piece + lane * 16), "s"(buffer) : "memory");
+    }
+  };
+  uint32_t row[NT];
+#pragma unroll
+  for (int t = 0; t < NT; ++t) row[t] = min(tile * kManyEntries + (wave * NT + t) * 16 + (lane & 15), p.V - 1);
+  const SIP_GLOBAL uint8_t* zeros = (const SIP_GLOBAL uint8_t*)(p.zeros ? p.zeros : reinterpret_cast<const uint8_t*>(kEights));
+  const uint32_t stride = (uint32_t)p.codes_stride;
+  u32x4 codes[NT][2], next_codes[NT][2];
+  auto load_codes = [&](int pair) {
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int e = 0; e < 2; ++e)
+        next_codes[t][e] = *(const SIP_GLOBAL u32x4*)((const SIP_GLOBAL uint8_t*)p.codes + (uint64_t)row[t] * stride +
+                                                      min(pair * 128 + quad * 32 + e * 16, p.D / 2 - 16));
+  };
+  auto scale_at = [&](int t, int g) -> float {
+    const uint32_t at = row[t] * groups + min(g, groups - 1);
+    if constexpr (SCALES_BF16) return __builtin_bit_cast(float, (uint32_t)((const SIP_GLOBAL uint16_t*)p.scales)[at] << 16);
+    else return ((const SIP_GLOBAL float*)p.scales)[at];
+  };
+  float scales[NT][kGroups], next_scales[NT][kGroups];
+  auto load_scales = [&](int pair) {
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int g = 0; g < kGroups; ++g) next_scales[t][g] = scale_at(t, pair * kGroups + g);
+  };
+  load_states(0);
+  load_scales(0);
+  load_codes(0);
+
+  f32x4 total[NT][MT] = {};
+  for (int g0 = 0; g0 < groups; g0 += 32) {
+    bf16x8 w[NT][3];
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int g = g0 + quad * 8 + e;
+        const uint32_t at = row[t] * groups + min(g, groups - 1);
+        float f = scale_at(t, g) * (-16.0f - (float)zeros[p.zeros ? at : 0]);
+#pragma unroll
+        for (int part = 0; part < 3; ++part) {
+          const uint32_t top = __builtin_bit_cast(uint32_t, f) & 0xffff0000u;
+          w[t][part][e] = __builtin_bit_cast(__bf16, (uint16_t)(top >> 16));
+          f -= __builtin_bit_cast(float, top);
+        }
+      }
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+      bf16x8 x[3];
+#pragma unroll
+      for (int part = 0; part < 3; ++part)
+        x[part] = *reinterpret_cast<const bf16x8*>(from + layout.sums + ((size_t)(g0 / 32 * 3 + part) * MT + m) * 1024 + lane * 16);
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int sum = 2; sum >= 0; --sum)
+#pragma unroll
+          for (int part = 0; part <= sum; ++part)
+            total[t][m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[part], w[t][sum - part], total[t][m], 0, 0, 0);
+    }
+  }
+  const CodeValues code_values;
+  f32x4 acc[NT][MT];
+  for (int pair = 0; pair < pairs; ++pair) {
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+#pragma unroll
+      for (int e = 0; e < 2; ++e) codes[t][e] = UnitOrder<32, 2>::order(e, next_codes[t][e]);
+#pragma unroll
+      for (int g = 0; g < kGroups; ++g) scales[t][g] = next_scales[t][g];
+    }
+    // this pair's states have arrived, and everybody has read the last one's
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    if (pair + 1 < pairs) {
+      load_states(pair + 1);
+      load_scales(pair + 1);
+      load_codes(pair + 1);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int c = 0; c < 8; ++c) {                          // product of the pair: dword c / 2 of load c % 2
+      const bool starts = c % (GROUP / 32) == 0, ends = (c + 1) % (GROUP / 32) == 0;
+      bf16x8 w[NT];
+#pragma unroll
+      for (int t = 0; t < NT; ++t) w[t] = __builtin_bit_cast(bf16x8, code_values(codes[t][c & 1][c >> 1]));
+#pragma unroll
+      for (int m = 0; m < MT; ++m) {
+        const bf16x8 x = *(const SIP_LDS bf16x8*)(uintptr_t)(lds0 + (uint32_t)(pair & 1) * kPairBytes + (c * MT + m) * 1024 + lane * 16);
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+          acc[t][m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, w[t], starts ? f32x4{} : acc[t][m], 0, 0, 0);
+      }
+      if (ends)
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+          for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) total[t][m][r] = __builtin_fmaf(scales[t][c / (GROUP / 32)], acc[t][m][r], total[t][m][r]);
+    }
+  }
+  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+  SIP_LDS float* out = (SIP_LDS float*)lds;
+#pragma unroll
+  for (int t = 0; t < NT; ++t)
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) out[(m * 16 + quad * 4 + r) * kPitch + (wave * NT + t) * 16 + (lane & 15)] = total[t][m][r];
+  __syncthreads();
+  const int v = tile * kManyEntries + (threadIdx.x & (kManyEntries - 1));
+  for (int b = threadIdx.x / kManyEntries; b < states && block * states + b < p.B; b += kManyWaves * 64 / kManyEntries) {
+    float z = 0.0f;
+    for (int r = (b + 1) * each - 1; r >= b * each; --r) z += out[r * kPitch + (threadIdx.x & (kManyEntries - 1))];
+    if (v < p.V) {
+      const long long at = (block * states + b) * p.logits_stride + v;
+      if (p.logits_bf16) static_cast<__bf16*>(p.logits)[at] = (__bf16)z;
+      else static_cast<float*>(p.logits)[at] = z;
     }
   }
 }

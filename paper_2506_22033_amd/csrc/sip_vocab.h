@@ -1,6 +1,7 @@
 // Host side of the entry points declared in include/sip_head.h: argument checks, workspace carving, launches.
 #pragma once
 #include <algorithm>
+#include <initializer_list>
 
 #include "../../include/sip_head.h"
 #include "sip_clip.h"
@@ -15,19 +16,49 @@ inline bool workspace_ok(const void* p, size_t have, size_t need) {
   return p && (reinterpret_cast<uintptr_t>(p) & 255u) == 0 && have >= need;
 }
 
+// Tiles of the cross entropy's products, by how many tokens there are; the wide ones where they fill the chip.
+typedef sip::GemmShape<256, 256, 128, 64, 3, 2> Wide;
+typedef sip::GemmShape<256, 128, 128, 64, 3, 3> Half;
+typedef sip::GemmShape<256, 64, 64, 64, 4, 3> Quarter;
+typedef sip::GemmShape<128, 32, 32, 32, 4, 4> Narrow;
+typedef sip::GemmShape<128, 128, 64, 64, 2, 2> Small;
+enum XentShape { kWide, kHalf, kQuarter, kNarrow, kSmall };
+
+inline int tiles(long long n, int tile) { return (int)((n + tile - 1) / tile); }
+constexpr int kChip = 256;                             // workgroups of a compute unit each
+
+// What a product of a x b with sums over k costs in Wide or Small tiles, the sums dealt out in `splits` parts: rounds of
+// workgroups -- one a compute unit, or two --, each with a start and an end worth 512 k; two Small tiles take nine tenths of
+// the time of a Wide one, which does twice as much (300 tokens, V = 151643, D = 2048: 52 and 56 us a round).
+double tiles_cost(XentShape s, long long a, long long b, int k, int splits) {
+  const int side = s == kWide ? 256 : 128, at_once = s == kWide ? kChip : 2 * kChip;
+  return (double)tiles(tiles(a, side) * (long long)tiles(b, side) * splits, at_once) * (tiles(k, splits) + 512) * (s == kWide ? 1.0 : 0.9);
+}
+XentShape cheaper(long long a, long long b, int k) {
+  return tiles_cost(kWide, a, b, k, 1) <= tiles_cost(kSmall, a, b, k, 1) ? kWide : kSmall;
+}
+// The logits of `tokens` against a rows of the head: the narrowest tile that holds all tokens, or the cheaper one.
+XentShape shape_for(int a, int tokens, int D) {
+  return tokens <= 32 ? kNarrow : tokens <= 64 ? kQuarter : tokens <= 128 ? kHalf : cheaper(a, tokens, D);
+}
+int shape_a(XentShape s) { return s == kNarrow || s == kSmall ? 128 : 256; }
+int shape_b(XentShape s) { return s == kWide ? 256 : s == kQuarter ? 64 : s == kNarrow ? 32 : 128; }
+int shape_wave_a(XentShape s) { return s == kWide || s == kHalf ? 128 : s == kNarrow ? 32 : 64; }
+
 // How a cross entropy of this shape is cut, and where its parts lie in the workspace.
 struct XentPlan {
-  int parts;                    // tiles' partial sums of a token
+  XentShape score;              // tiles of the logits
+  int parts;                    // waves' partial sums of a token
   int piece;                    // vocabulary entries whose dz is held at once
-  size_t count, rows, target_z, part, dense, dz, sum, bytes;
+  XentShape score_piece, hidden, weight;
+  sip::Parts hidden_parts, weight_parts;   // (without their room)
+  size_t count, rows, target_z, part, dense, dz, hidden_sum, weight_sum, bytes;
 };
 
 XentPlan xent_plan(int32_t N, int32_t V, int32_t D, bool backward) {
   XentPlan p{};
-  p.parts = (V + sip::kTileA - 1) / sip::kTileA * (sip::kTileA / 32);
-  const long long most = std::max<long long>(256, ((1ll << 28) / N) / 256 * 256);   // dz: half a gigabyte at most, or 256 columns
-  const long long pieces = (V + most - 1) / most;
-  p.piece = (int)(((V + pieces - 1) / pieces + 255) / 256 * 256);
+  p.score = shape_for(V, N, D);
+  p.parts = tiles(V, shape_a(p.score)) * (shape_a(p.score) / shape_wave_a(p.score));
   size_t at = 0;
   auto take = [&](size_t n) { const size_t here = at; at += head_align(n); return here; };
   p.count = take(4);
@@ -38,14 +69,53 @@ XentPlan xent_plan(int32_t N, int32_t V, int32_t D, bool backward) {
   p.part = take((size_t)N * p.parts * 8);
   p.bytes = at;
   if (backward) {
+    const long long most = std::max<long long>(256, ((1ll << 28) / N) / 256 * 256);   // dz: half a gigabyte at most, or 256 columns
+    const int pieces = tiles(V, (int)std::min<long long>(most, 1 << 20));
+    p.piece = tiles(tiles(V, pieces), 256) * 256;
+    const int left = std::min(p.piece, V);
+    p.score_piece = shape_for(left, N, D);
+    // A product with few tiles and a long sum has that dealt out in so many parts that it takes the least time.
+    auto deal = [](auto&& shapes, int k, auto&& cost_of, XentShape& shape, int& count) {
+      double best = 0.0;
+      for (XentShape s : shapes)
+        for (int n = 1; n <= 128 && (n == 1 || k / n >= 256); ++n) {
+          const double cost = cost_of(s, n) + (n > 1 ? 256.0 : 0.0);                // (the join)
+          if (best == 0.0 || cost < best) { best = cost; shape = s; count = n; }
+        }
+    };
+    const std::initializer_list<XentShape> square = {kWide, kSmall};
+    int parts = 1;
+    if (N <= 128)
+      deal(std::initializer_list<XentShape>{shape_for(left, N, D)}, left, [&](XentShape s, int n) {
+        return (double)tiles((long long)tiles(D, shape_a(s)) * n, kChip) * (tiles(left, n) + 512);
+      }, p.hidden, parts);
+    else
+      deal(square, left, [&](XentShape s, int n) { return tiles_cost(s, D, N, left, n); }, p.hidden, parts);
+    p.hidden_parts = {nullptr, tiles(D, shape_a(p.hidden)) * tiles(N, shape_b(p.hidden)), parts, tiles(tiles(left, parts), 64) * 64};
+    deal(square, N, [&](XentShape s, int n) { return tiles_cost(s, D, left, N, n); }, p.weight, parts);
+    p.weight_parts = {nullptr, tiles(D, shape_a(p.weight)) * tiles(left, shape_b(p.weight)), parts, tiles(tiles(N, parts), 64) * 64};
+    auto room = [](const sip::Parts& q, XentShape s) { return (size_t)q.count * q.tiles * shape_a(s) * shape_b(s) * 4; };
     at = both;
     p.dense = take((size_t)N * D * 2);
     p.dz = take((size_t)N * p.piece * 2);
-    p.sum = take((size_t)N * D * 4);
+    p.hidden_sum = take(p.hidden_parts.count == 1 && p.piece >= V ? 0 : room(p.hidden_parts, p.hidden));
+    p.weight_sum = take(p.weight_parts.count == 1 ? 0 : room(p.weight_parts, p.weight));
     p.bytes = std::max(p.bytes, at);
   }
   return p;
 }
+
+// f(S{}) with the tile's type, one of those named.
+template <XentShape> struct ShapeType;
+template <> struct ShapeType<kWide> { typedef Wide type; };
+template <> struct ShapeType<kHalf> { typedef Half type; };
+template <> struct ShapeType<kQuarter> { typedef Quarter type; };
+template <> struct ShapeType<kNarrow> { typedef Narrow type; };
+template <> struct ShapeType<kSmall> { typedef Small type; };
+template <XentShape... AMONG, class F>
+void with_shape(XentShape s, F f) { (void)((s == AMONG && (f(typename ShapeType<AMONG>::type{}), true)) || ...); }
+// Workgroups for n tiles of which each XCD takes an eighth (sip_xent.h, tile_of).
+inline int tile_grid(long long n) { return tiles(n, 8) * 8; }
 
 bool xent_shape_ok(int32_t N, int32_t V, int32_t D) {
   return N > 0 && V > 0 && D > 0 && N <= SIP_MAX_TOKENS && V <= SIP_MAX_V && D <= SIP_MAX_D && D % 8 == 0;
@@ -79,12 +149,66 @@ sip::XentArgs xent_args(const void* hidden, int32_t N, int32_t D, int64_t hidden
   a.dense = reinterpret_cast<uint16_t*>(ws + pl.dense);
   a.dz = reinterpret_cast<uint16_t*>(ws + pl.dz);
   a.piece = pl.piece;
-  a.sum = reinterpret_cast<float*>(ws + pl.sum);
+  a.hidden_parts = pl.hidden_parts; a.hidden_parts.sum = reinterpret_cast<float*>(ws + pl.hidden_sum);
+  a.weight_parts = pl.weight_parts; a.weight_parts.sum = reinterpret_cast<float*>(ws + pl.weight_sum);
   return a;
 }
 
 inline sip_status launched() { return hipGetLastError() == hipSuccess ? SIP_OK : SIP_ERR_HIP; }
-inline int tiles(int n, int tile) { return (n + tile - 1) / tile; }
+
+template <int N> using Int = std::integral_constant<int, N>;
+
+// Launches head_few_kernel where the hidden states fit the registers of a workgroup: 16 rows (an fp32 state is three) and D
+// <= 8192, or 32 and 4096, D from 128 on.  False: they do not.
+template <int GROUP, bool SCALES_BF16>
+bool few_rows_of(const sip::CodesArgs& a, hipStream_t stream) {
+  const int units = tiles(tiles(a.D, 128), sip::kFewWaves);              // of a wave
+  // the kernel of the fewest UNITS that hold them
+  auto launch = [&](auto mt, auto... counts) {
+    bool done = false;
+    auto one = [&](auto n) {
+      constexpr int kUnits = decltype(n)::value, kMt = decltype(mt)::value;
+      if (done || units > kUnits) return;
+      constexpr int kTiles = sip::few_tiles(GROUP, SCALES_BF16, kUnits, kMt);
+      hipLaunchKernelGGL((sip::head_few_kernel<GROUP, SCALES_BF16, kUnits, kMt>), dim3(std::min(kChip, tiles(a.V, 16 * kTiles))),
+                         dim3(sip::kFewWaves * 64), 0, stream, a);
+      done = true;
+    };
+    (one(counts), ...);
+    return done;
+  };
+  const int rows = std::min(a.B, 64) * sip::rows_of_state(a.hidden_bf16);
+  if (a.D < 128 || rows > 32) return false;
+  if (rows > 16) return launch(Int<2>(), Int<1>(), Int<2>(), Int<3>(), Int<4>());
+  return launch(Int<1>(), Int<1>(), Int<2>(), Int<3>(), Int<4>(), Int<5>(), Int<6>(), Int<7>(), Int<8>());
+}
+template <int GROUP>
+bool few_rows_of(const sip::CodesArgs& a, hipStream_t stream) {
+  return a.scales_bf16 ? few_rows_of<GROUP, true>(a, stream) : few_rows_of<GROUP, false>(a, stream);
+}
+bool few_rows(const sip::CodesArgs& a, hipStream_t stream) {
+  return a.group == 32 ? few_rows_of<32>(a, stream) : a.group == 64 ? few_rows_of<64>(a, stream) : few_rows_of<128>(a, stream);
+}
+
+// head_many_kernel: blocks of 64 rows where one holds them all, else of 128.
+int many_tiles(int32_t B, bool hidden_bf16) { return B <= sip::block_states(4, hidden_bf16) ? 4 : 8; }
+size_t many_bytes(int32_t B, int32_t D, int32_t group, bool hidden_bf16) {
+  const int mt = many_tiles(B, hidden_bf16);
+  return tiles(B, sip::block_states(mt, hidden_bf16)) * sip::ManyLayout(D, group, mt).block;
+}
+template <int GROUP>
+void many_rows_of(const sip::CodesArgs& a, hipStream_t stream) {
+  const int mt = many_tiles(a.B, a.hidden_bf16), blocks = tiles(a.B, sip::block_states(mt, a.hidden_bf16));
+  hipLaunchKernelGGL(sip::head_rows_kernel<GROUP>, dim3(tiles(sip::many_groups(a.D, GROUP), 4), blocks * mt), dim3(256), 0, stream, a, mt);
+  const dim3 grid(tiles(tiles(a.V, sip::kManyEntries), 8) * 8 * blocks), threads(sip::kManyWaves * 64);
+  if (a.scales_bf16) {
+    if (mt == 4) hipLaunchKernelGGL((sip::head_many_kernel<GROUP, true, 4>), grid, threads, 0, stream, a);
+    else hipLaunchKernelGGL((sip::head_many_kernel<GROUP, true, 8>), grid, threads, 0, stream, a);
+  } else {
+    if (mt == 4) hipLaunchKernelGGL((sip::head_many_kernel<GROUP, false, 4>), grid, threads, 0, stream, a);
+    else hipLaunchKernelGGL((sip::head_many_kernel<GROUP, false, 8>), grid, threads, 0, stream, a);
+  }
+}
 
 }  // namespace
 
@@ -106,8 +230,11 @@ sip_status sip_xent_forward(const void* hidden, int32_t N, int32_t D, int64_t hi
   sip::XentArgs a = xent_args(hidden, N, D, hidden_stride, weight, V, weight_stride, targets, logit_scale, pl, workspace);
   a.loss = loss; a.lse = lse;
   hipLaunchKernelGGL(sip::xent_rows_kernel, dim3(1), dim3(1024), 0, stream, a);
-  hipLaunchKernelGGL(sip::xent_forward_kernel, dim3(tiles(V, sip::kTileA), tiles(N, sip::kTileB)), dim3(sip::kGemmThreads), 0,
-                     stream, a);
+  with_shape<kWide, kHalf, kQuarter, kNarrow, kSmall>(pl.score, [&](auto shape) {
+    typedef decltype(shape) S;
+    hipLaunchKernelGGL(sip::xent_forward_kernel<S>, dim3(tile_grid((long long)tiles(V, S::kA) * tiles(N, S::kB))),
+                       dim3(S::kThreads), 0, stream, a);
+  });
   hipLaunchKernelGGL(sip::xent_loss_kernel, dim3(tiles(N, 4)), dim3(256), 0, stream, a);
   return launched();
 }
@@ -136,57 +263,77 @@ sip_status sip_xent_backward(const void* hidden, int32_t N, int32_t D, int64_t h
   for (int v0 = 0; v0 < V; v0 += pl.piece) {
     a.v0 = v0;
     const int left = std::min(pl.piece, V - v0);
-    hipLaunchKernelGGL(sip::xent_dz_kernel, dim3(tiles(left, sip::kTileA), tiles(N, sip::kTileB)), dim3(sip::kGemmThreads), 0,
-                       stream, a);
+    with_shape<kWide, kHalf, kQuarter, kNarrow, kSmall>(pl.score_piece, [&](auto shape) {
+      typedef decltype(shape) S;
+      hipLaunchKernelGGL(sip::xent_dz_kernel<S>, dim3(tile_grid((long long)tiles(left, S::kA) * tiles(N, S::kB))),
+                         dim3(S::kThreads), 0, stream, a);
+    });
     if (grad_hidden)
-      hipLaunchKernelGGL(sip::xent_grad_hidden_kernel, dim3(tiles(D, sip::kTileA), tiles(N, sip::kTileB)),
-                         dim3(sip::kGemmThreads), 0, stream, a);
+      with_shape<kWide, kHalf, kQuarter, kNarrow, kSmall>(pl.hidden, [&](auto shape) {
+        typedef decltype(shape) S;
+        hipLaunchKernelGGL(sip::xent_grad_hidden_kernel<S>, dim3(tile_grid(pl.hidden_parts.tiles), pl.hidden_parts.count), dim3(S::kThreads), 0,
+                           stream, a);
+        if (pl.hidden_parts.count > 1 && v0 + pl.piece >= V)
+          hipLaunchKernelGGL((sip::xent_join_kernel<S, true>), dim3(pl.hidden_parts.tiles, S::kTA * S::kTB), dim3(S::kThreads), 0, stream, a);
+      });
     if (grad_weight)
-      hipLaunchKernelGGL(sip::xent_grad_weight_kernel, dim3(tiles(D, sip::kTileA), tiles(left, sip::kTileB)),
-                         dim3(sip::kGemmThreads), 0, stream, a);
+      with_shape<kWide, kSmall>(pl.weight, [&](auto shape) {
+        typedef decltype(shape) S;
+        const int n_tiles = tiles(D, S::kA) * tiles(left, S::kB);
+        hipLaunchKernelGGL(sip::xent_grad_weight_kernel<S>, dim3(tile_grid(n_tiles), pl.weight_parts.count), dim3(S::kThreads), 0, stream, a);
+        if (pl.weight_parts.count > 1)
+          hipLaunchKernelGGL((sip::xent_join_kernel<S, false>), dim3(n_tiles, S::kTA * S::kTB), dim3(S::kThreads), 0, stream, a);
+      });
   }
   return launched();
 }
 
 size_t sip_grad_clip_workspace_bytes(int32_t n_tensors) {
   if (n_tensors < 0 || n_tensors > SIP_MAX_TENSORS) return 0;
-  const int launches = std::max(1, tiles(n_tensors, sip::kClipTable));
-  return 256 + head_align((size_t)launches * sip::kClipGroups * sizeof(double));
+  return head_align((size_t)std::max(1, tiles(n_tensors, sip::kClipTable)) * sip::kClipGroups * sizeof(double));
 }
 
 sip_status sip_grad_clip(const sip_grad* tensors, int32_t n_tensors, float max_norm, float eps, float* norm,
                          void* workspace, size_t workspace_bytes, void* hip_stream) {
   if (n_tensors < 0 || (n_tensors > 0 && !tensors) || !norm || !(max_norm >= 0.0f) || !(eps >= 0.0f)) return SIP_ERR_INVALID_ARG;
   if (n_tensors > SIP_MAX_TENSORS) return SIP_ERR_UNSUPPORTED;
+  int64_t bytes = 0;
   for (int j = 0; j < n_tensors; ++j) {
     const sip_grad& t = tensors[j];
     if (t.count < 0 || (t.dtype != SIP_F32 && t.dtype != SIP_BF16)) return SIP_ERR_INVALID_ARG;
     if (t.count > 0 && (!t.grad || !t.out)) return SIP_ERR_INVALID_ARG;
-    if (t.count > (1ll << 40)) return SIP_ERR_UNSUPPORTED;
+    if (t.count > (1ll << 40) || (bytes += t.count * 4) > (1ll << 46)) return SIP_ERR_UNSUPPORTED;
     const uintptr_t mask = t.dtype == SIP_F32 ? 3 : 1;
     if (((reinterpret_cast<uintptr_t>(t.grad) | reinterpret_cast<uintptr_t>(t.out)) & mask) != 0) return SIP_ERR_INVALID_ARG;
   }
   if (!workspace_ok(workspace, workspace_bytes, sip_grad_clip_workspace_bytes(n_tensors))) return SIP_ERR_WORKSPACE;
   hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-  float* factor = static_cast<float*>(workspace);
-  double* part = reinterpret_cast<double*>(static_cast<char*>(workspace) + 256);
+  double* part = static_cast<double*>(workspace);
   const int launches = std::max(1, tiles(n_tensors, sip::kClipTable));
   auto table = [&](int l) {
     sip::ClipTable t{};
-    for (int j = l * sip::kClipTable; j < std::min(n_tensors, (l + 1) * sip::kClipTable); ++j, ++t.n) {
-      t.grad[t.n] = tensors[j].grad;
-      t.out[t.n] = tensors[j].out;
+    for (int j = l * sip::kClipTable; j < std::min(n_tensors, (l + 1) * sip::kClipTable); ++j) {
+      if (tensors[j].count == 0) continue;
+      t.grad[t.n] = static_cast<const char*>(tensors[j].grad);
+      t.out[t.n] = static_cast<char*>(tensors[j].out);
       t.count[t.n] = tensors[j].count | (tensors[j].dtype == SIP_BF16 ? sip::kClipBf16 : 0);
+      t.end[t.n] = (t.n ? t.end[t.n - 1] : 0) + (uint32_t)((sip::clip_bytes(t.count[t.n]) + sip::kClipBytes - 1) / sip::kClipBytes);
+      ++t.n;
     }
     return t;
   };
-  for (int l = 0; l < launches; ++l)
-    hipLaunchKernelGGL(sip::clip_squares_kernel, dim3(sip::kClipGroups), dim3(sip::kClipThreads), 0, stream, table(l),
-                       part + (size_t)l * sip::kClipGroups);
-  hipLaunchKernelGGL(sip::clip_norm_kernel, dim3(1), dim3(1024), 0, stream, part, launches * sip::kClipGroups, max_norm, eps, norm,
-                     factor);
-  for (int l = 0; l < launches; ++l)
-    hipLaunchKernelGGL(sip::clip_scale_kernel, dim3(sip::kClipGroups), dim3(sip::kClipThreads), 0, stream, table(l), factor);
+  auto groups = [](const sip::ClipTable& t) { return t.n ? (int)std::min<uint32_t>(t.end[t.n - 1], sip::kClipGroups) : 1; };
+  int parts = 0;
+  for (int l = 0; l < launches; ++l) {
+    const sip::ClipTable t = table(l);
+    hipLaunchKernelGGL(sip::clip_squares_kernel, dim3(groups(t)), dim3(sip::kClipThreads), 0, stream, t, part + parts);
+    parts += groups(t);
+  }
+  for (int l = launches - 1; l >= 0; --l) {
+    const sip::ClipTable t = table(l);
+    hipLaunchKernelGGL(sip::clip_scale_kernel, dim3(groups(t)), dim3(sip::kClipThreads), 0, stream, t, part, parts, max_norm, eps,
+                       l == 0 ? norm : nullptr);
+  }
   return launched();
 }
 
@@ -217,16 +364,18 @@ sip_status sip_head_quantize(const void* weight, int32_t V, int32_t D, int64_t w
   a.scales = scales; a.scales_bf16 = scales_dtype == SIP_BF16;
   a.zeros = zeros;
   a.V = V; a.D = D; a.group = group;
-  const long long groups = (long long)V * (D / group);
-  hipLaunchKernelGGL(sip::quantize_kernel, dim3((unsigned)((groups + 255) / 256)), dim3(256), 0,
-                     static_cast<hipStream_t>(hip_stream), a);
+  const dim3 grid(std::min(tiles((long long)V * (D / 8), 256), kChip * 64));
+  hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+  if (group == 32) hipLaunchKernelGGL(sip::quantize_kernel<32>, grid, dim3(256), 0, stream, a);
+  else if (group == 64) hipLaunchKernelGGL(sip::quantize_kernel<64>, grid, dim3(256), 0, stream, a);
+  else hipLaunchKernelGGL(sip::quantize_kernel<128>, grid, dim3(256), 0, stream, a);
   return launched();
 }
 
 size_t sip_head_workspace_bytes(int32_t B, int32_t V, int32_t D, int32_t group) {
   if (B <= 0 || V <= 0 || D <= 0 || B > SIP_MAX_B || V > SIP_MAX_V || D > SIP_MAX_D) return 0;
   if ((group != 32 && group != 64 && group != 128) || D % group != 0) return 0;
-  return 256;
+  return head_align(std::max(many_bytes(B, D, group, true), many_bytes(B, D, group, false)));
 }
 
 sip_status sip_head_logits(const void* hidden, int32_t B, int32_t D, int64_t hidden_stride, sip_dtype hidden_dtype,
@@ -252,8 +401,12 @@ sip_status sip_head_logits(const void* hidden, int32_t B, int32_t D, int64_t hid
   a.hidden = hidden; a.hidden_stride = hidden_stride; a.hidden_bf16 = hidden_dtype == SIP_BF16;
   a.B = B;
   a.logits = logits; a.logits_stride = logits_stride; a.logits_bf16 = logits_dtype == SIP_BF16;
-  hipLaunchKernelGGL(sip::head_logits_kernel, dim3(tiles(B, 16), tiles(V, 16)), dim3(64), 0,
-                     static_cast<hipStream_t>(hip_stream), a);
+  a.states = static_cast<char*>(workspace);
+  hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+  if (few_rows(a, stream)) return launched();
+  if (group == 32) many_rows_of<32>(a, stream);
+  else if (group == 64) many_rows_of<64>(a, stream);
+  else many_rows_of<128>(a, stream);
   return launched();
 }
 

@@ -12,9 +12,16 @@ __device__ inline uint32_t bf16_bits(float x) {          // round to nearest eve
   const __bf16 b = (__bf16)x;
   return __builtin_bit_cast(uint16_t, b);
 }
-__device__ inline uint2 bf16_pack(float a, float b, float c, float d) {
-  return make_uint2(bf16_bits(a) | (bf16_bits(b) << 16), bf16_bits(c) | (bf16_bits(d) << 16));
+__device__ inline u32x2 bf16_pack(f32x4 x) {
+  return u32x2{bf16_bits(x[0]) | (bf16_bits(x[1]) << 16), bf16_bits(x[2]) | (bf16_bits(x[3]) << 16)};
 }
+
+// A product whose long sum is dealt out: part i has the `split` k from i * split on, and its sums lie behind those of the parts
+// before it, [tiles] of them, tile by tile in the order of the accumulators: a lane's four neighbours, a wave's lanes in a row.
+struct Parts {
+  float* sum;
+  int tiles, count, split;
+};
 
 struct XentArgs {
   const uint16_t* hidden; long long hidden_stride;
@@ -31,33 +38,46 @@ struct XentArgs {
   int* count;                             // rows that take part
   int* rows;                              // [N] their indices, ascending
   float* target_z;                        // [N] z of the target, by place in the list
-  float2* part;                           // [N][parts] maximum and sum of a tile's logits without the target
+  float2* part;                           // [N][parts] maximum and sum of a wave's logits without the target
   int parts;
   uint16_t* dense;                        // [N][D] the rows that take part, one after the other
   uint16_t* dz; int piece;                // [N][piece] gradient of a piece's logits
-  float* sum;                             // [N][D] of grad_hidden over the pieces
+  Parts hidden_parts, weight_parts;
   int v0;                                 // the piece's first vocabulary entry
 };
 
-// One workgroup lists the rows.  What is read is N integers once: latency of a launch.
+// One workgroup lists the rows, eight targets a thread a turn.  What is read is N integers once: latency.
 __global__ __launch_bounds__(1024) void xent_rows_kernel(XentArgs p) {
-  __shared__ int wave_n[16];
-  __shared__ int base;
+  __shared__ int wave_n[2][16];
   const int t = threadIdx.x, lane = t & 63, w = t >> 6;
-  if (t == 0) base = 0;
-  for (int i0 = 0; i0 < p.N; i0 += 1024) {
-    const int i = i0 + t;
-    const bool live = i < p.N && (unsigned)p.targets[i] < (unsigned)p.V;
-    const unsigned long long m = __ballot(live);
-    if (lane == 0) wave_n[w] = __popcll(m);
+  int base = 0, side = 0;
+  for (int first = 0; first < p.N; first += 8192, side ^= 1) {
+    const int i0 = first + t * 8;
+    uint32_t live = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (i0 + e < p.N && (unsigned)p.targets[i0 + e] < (unsigned)p.V) live |= 1u << e;
+    const int mine = __popc(live);
+    int before = mine;                                   // of the wave's lanes up to mine
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const int other = __shfl_up(before, d);
+      if (lane >= d) before += other;
+    }
+    if (lane == 63) wave_n[side][w] = before;
     __syncthreads();
-    int before = base;
-    for (int j = 0; j < w; ++j) before += wave_n[j];
-    if (live) p.rows[before + __popcll(m & ((1ull << lane) - 1))] = i;
-    else if (i < p.N && p.loss) p.loss[i] = p.lse[i] = 0.0f;
-    __syncthreads();
-    if (t == 1023) base = before + wave_n[15];
-    __syncthreads();
+    int at = base + before - mine;
+#pragma unroll
+    for (int j = 0; j < 16; ++j) {
+      const int n = wave_n[side][j];
+      if (j < w) at += n;
+      base += n;
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      if (live >> e & 1) p.rows[at++] = i0 + e;
+      else if (i0 + e < p.N && p.loss) p.loss[i0 + e] = p.lse[i0 + e] = 0.0f;
+    }
   }
   if (t == 0) *p.count = base;
 }
@@ -76,33 +96,106 @@ __global__ __launch_bounds__(256) void xent_gather_kernel(XentArgs p) {
   }
 }
 
-// A tile of logits, reduced to its maximum and sum of exponentials per token.
-__global__ __launch_bounds__(kGemmThreads) void xent_forward_kernel(XentArgs p) {
-  const int n = *p.count, a0 = blockIdx.x * kTileA, b0 = blockIdx.y * kTileB;
-  if (b0 >= n) return;
-  f32x16 acc{};
-  gemm_tile<kRows, kRows>(acc, Operand{p.weight, p.weight_stride, p.V, nullptr}, Operand{p.hidden, p.hidden_stride, n, p.rows},
-                          a0, b0, 0, p.D);
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  const int v_first = a0 + 32 * (w & 1), i = b0 + 32 * (w >> 1) + (lane & 31);
-  const bool live = i < n;
-  const int target = live ? p.targets[p.rows[i]] : -1;
-  float m = -INFINITY, s = 0.0f;
-  bool nan = false;
-  for (int r = 0; r < 16; ++r) {
-    const int v = v_first + acc_a(r, lane);
-    acc[r] *= p.logit_scale;
-    if (v == target && live) p.target_z[i] = acc[r];
-    if (v >= p.V || v == target) acc[r] = -INFINITY;
-    nan |= acc[r] != acc[r];
-    m = fmaxf(m, acc[r]);
+// Which tile a workgroup takes of tiles_a x tiles_b.  The eight XCDs, to which workgroups go in turn, take a run of
+// tiles each; within it eight tiles along a go with one along b before the next, so that the 32 of an XCD that are under
+// way share their rows of either operand in its L2.  False: none is left.
+__device__ inline bool tile_of(int id, int tiles_a, int tiles_b, int& ta, int& tb) {
+  constexpr int kGroup = 8;
+  const int total = tiles_a * tiles_b, run = (total + 7) / 8;
+  const int local = id >> 3, s = (id & 7) * run + local;
+  if (local >= run || s >= total) return false;
+  const int first = s / (kGroup * tiles_b) * kGroup, width = min(kGroup, tiles_a - first), r = s - first * tiles_b;
+  ta = first + r % width;
+  tb = r / width;
+  return true;
+}
+__host__ __device__ inline int div_up(int a, int b) { return (a + b - 1) / b; }
+
+// Where the blocks of a wave begin in the tile.
+template <class S> __device__ inline int wave_a() { return (int)(threadIdx.x >> 6) % (S::kA / S::kWaveA) * S::kWaveA; }
+template <class S> __device__ inline int wave_b() { return (int)(threadIdx.x >> 6) / (S::kA / S::kWaveA) * S::kWaveB; }
+
+// The tile's values value(i, j) -- the lane's four of block (i, j) -- as bf16, row by row through LDS, to where row(b) says
+// (nullptr: nowhere), columns [a0, a_end).  A lane holds four neighbours of one row: eight bytes, whose 16-byte group goes
+// to place group ^ row, so that 16 rows meet every bank once; rows leave in 16-byte groups.
+template <class S, class Value, class Row>
+__device__ inline void store_tile(SIP_LDS char* lds, int a0, int a_end, Value value, Row row) {
+  constexpr int kPitch = S::kA * 2, kGroups = S::kA / 8, kMask = 15;
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int j = 0; j < S::kTB; ++j) {
+    const int b = wave_b<S>() + 16 * j + (lane & 15);
+#pragma unroll
+    for (int i = 0; i < S::kTA; ++i) {
+      const int a = wave_a<S>() + 16 * i + acc_a(lane);
+      *reinterpret_cast<SIP_LDS u32x2*>(lds + b * kPitch + (((a >> 3) ^ (b & kMask)) << 4) + ((a & 4) << 1)) = bf16_pack(value(i, j));
+    }
   }
-  m = fmaxf(m, __shfl_xor(m, 32));
-  const float base = m == -INFINITY ? 0.0f : m;
-  for (int r = 0; r < 16; ++r) s += __builtin_amdgcn_exp2f((acc[r] - base) * kLog2e);
-  if (nan) s = NAN;
-  s += __shfl_xor(s, 32);
-  if (live && lane < 32) p.part[(long long)i * p.parts + (v_first >> 5)] = make_float2(m, s);
+  __syncthreads();
+#pragma unroll 4
+  for (int g = threadIdx.x; g < S::kB * kGroups; g += S::kThreads) {
+    const int b = g / kGroups, c = g % kGroups;
+    uint16_t* to = row(b);
+    if (to && a0 + c * 8 < a_end)
+      *reinterpret_cast<u32x4*>(to + a0 + c * 8) = *reinterpret_cast<SIP_LDS u32x4*>(lds + b * kPitch + ((c ^ (b & kMask)) << 4));
+  }
+}
+
+// A tile of logits, reduced to its maximum and sum of exponentials per token and wave.
+template <class S>
+__global__ __launch_bounds__(S::kThreads) void xent_forward_kernel(XentArgs p) {
+  __shared__ __attribute__((aligned(1024))) char lds[S::kLds];
+  const int n = *p.count;
+  int ta, tb;
+  if (!tile_of(blockIdx.x, div_up(p.V, S::kA), div_up(n, S::kB), ta, tb)) return;
+  const int a0 = ta * S::kA, b0 = tb * S::kB;
+  typename S::Acc acc = {};
+  Gemm<S, kRows, kRows>::tile(acc, Operand{p.weight, p.weight_stride, p.V, nullptr}, Operand{p.hidden, p.hidden_stride, n, p.rows},
+                             a0, b0, 0, p.D, (SIP_LDS char*)lds);
+  // Maxima and sums as the logits are made: acc, times f for a base of 2.
+  const int lane = threadIdx.x & 63, v0 = a0 + wave_a<S>();
+  const float f = p.logit_scale * kLog2e;
+#pragma unroll
+  for (int j = 0; j < S::kTB; ++j) {
+    const int i = b0 + wave_b<S>() + 16 * j + (lane & 15);
+    const bool live = i < n;
+    const int target = live ? p.targets[p.rows[i]] : -1;
+    // the target's own logit is kept apart, and so is what lies past the vocabulary: -inf, whatever the scale's sign
+    if (__any(target >= v0 && target < v0 + S::kWaveA) || v0 + S::kWaveA > p.V) {
+#pragma unroll
+      for (int t = 0; t < S::kTA; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int v = v0 + 16 * t + acc_a(lane) + r;
+          if (v == target) p.target_z[i] = acc[t][j][r] * p.logit_scale;
+          if (v >= p.V || v == target) acc[t][j][r] = f < 0.0f ? INFINITY : -INFINITY;
+        }
+    }
+    float m = -INFINITY, s = 0.0f;
+    if (f < 0.0f) {
+#pragma unroll
+      for (int t = 0; t < S::kTA; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) m = fmaxf(m, -acc[t][j][r]);
+      m *= -f;
+    } else {
+#pragma unroll
+      for (int t = 0; t < S::kTA; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) m = fmaxf(m, acc[t][j][r]);
+      m *= f;
+    }
+    m = fmaxf(m, __shfl_xor(m, 16));
+    m = fmaxf(m, __shfl_xor(m, 32));
+    const float base = m == -INFINITY ? 0.0f : m;
+#pragma unroll
+    for (int t = 0; t < S::kTA; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) s += __builtin_amdgcn_exp2f(__builtin_fmaf(acc[t][j][r], f, -base));
+    s += __shfl_xor(s, 16);
+    s += __shfl_xor(s, 32);
+    if (live && lane < 16) p.part[(long long)i * p.parts + v0 / S::kWaveA] = make_float2(m, s);
+  }
 }
 
 // A wave joins a token's parts.
@@ -114,18 +207,18 @@ __global__ __launch_bounds__(256) void xent_loss_kernel(XentArgs p) {
   for (int j = lane; j < p.parts; j += 64) {
     const float2 q = part[j];
     const float top = fmaxf(m, q.x), base = top == -INFINITY ? 0.0f : top;
-    s = s * __builtin_amdgcn_exp2f((m - base) * kLog2e) + q.y * __builtin_amdgcn_exp2f((q.x - base) * kLog2e);
+    s = s * __builtin_amdgcn_exp2f(m - base) + q.y * __builtin_amdgcn_exp2f(q.x - base);
     m = top;
   }
   for (int d = 32; d; d >>= 1) {
     const float mo = __shfl_xor(m, d), so = __shfl_xor(s, d);
     const float top = fmaxf(m, mo), base = top == -INFINITY ? 0.0f : top;
-    s = s * __builtin_amdgcn_exp2f((m - base) * kLog2e) + so * __builtin_amdgcn_exp2f((mo - base) * kLog2e);
+    s = s * __builtin_amdgcn_exp2f(m - base) + so * __builtin_amdgcn_exp2f(mo - base);
     m = top;
   }
   if (lane == 0) {
     const float zt = p.target_z[i];
-    const float gap = m + logf(s) - zt;                  // ln of the others' mass over the target's
+    const float gap = __builtin_fmaf(m, 1.0f / kLog2e, logf(s) - zt);                 // ln of the others' mass over the target's
     const float loss = fmaxf(gap, 0.0f) + log1pf(expf(-fabsf(gap)));
     const int row = p.rows[i];
     p.loss[row] = gap != gap ? gap : loss;
@@ -133,72 +226,121 @@ __global__ __launch_bounds__(256) void xent_loss_kernel(XentArgs p) {
   }
 }
 
-// dz of a tile of the piece's logits.
-__global__ __launch_bounds__(kGemmThreads) void xent_dz_kernel(XentArgs p) {
-  const int n = *p.count, a0 = blockIdx.x * kTileA, b0 = blockIdx.y * kTileB;
-  if (b0 >= n) return;
-  f32x16 acc{};
-  gemm_tile<kRows, kRows>(acc, Operand{p.weight + p.v0 * p.weight_stride, p.weight_stride, p.V - p.v0, nullptr},
-                          Operand{p.dense, p.D, n, nullptr}, a0, b0, 0, p.D);
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  const int v_first = a0 + 32 * (w & 1), i = b0 + 32 * (w >> 1) + (lane & 31);
-  if (i >= n) return;
-  const int row = p.rows[i], target = p.targets[row] - p.v0;
-  const float lse = p.lse_in[row], g = p.grad_loss ? p.grad_loss[row] : 1.0f;
-  const float at_target = expm1f(-p.loss_in[row]);
-  for (int r = 0; r < 16; r += 4) {
-    float d[4];
-    for (int e = 0; e < 4; ++e) {
-      const int v = v_first + acc_a(r + e, lane);
-      d[e] = v >= p.V - p.v0 ? 0.0f : g * (v == target ? at_target : __builtin_amdgcn_exp2f((acc[r + e] * p.logit_scale - lse) * kLog2e));
-    }
-    *reinterpret_cast<uint2*>(p.dz + (long long)i * p.piece + v_first + acc_a(r, lane)) = bf16_pack(d[0], d[1], d[2], d[3]);
-  }
-}
-
-// grad_hidden of a piece, added to what the pieces before it gave.
-__global__ __launch_bounds__(kGemmThreads) void xent_grad_hidden_kernel(XentArgs p) {
-  const int n = *p.count, a0 = blockIdx.x * kTileA, b0 = blockIdx.y * kTileB;
-  if (b0 >= n) return;
-  const int kv = min(p.piece, p.V - p.v0);
-  f32x16 acc{};
-  gemm_tile<kCols, kRows>(acc, Operand{p.weight + p.v0 * p.weight_stride, p.weight_stride, p.D, nullptr},
-                          Operand{p.dz, p.piece, n, nullptr}, a0, b0, 0, kv);
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  const int d_first = a0 + 32 * (w & 1), i = b0 + 32 * (w >> 1) + (lane & 31);
-  if (i >= n) return;
-  const bool last = p.v0 + p.piece >= p.V;
-  for (int r = 0; r < 16; r += 4) {
-    const int d = d_first + acc_a(r, lane);
-    if (d >= p.D) continue;
-    float4* sum = reinterpret_cast<float4*>(p.sum + (long long)i * p.D + d);
-    float4 s = make_float4(acc[r], acc[r + 1], acc[r + 2], acc[r + 3]);
-    if (p.v0) { const float4 o = *sum; s.x += o.x; s.y += o.y; s.z += o.z; s.w += o.w; }
-    if (last) {
-      const float f = p.out_scale;
-      *reinterpret_cast<uint2*>(p.grad_hidden + p.rows[i] * p.gh_stride + d) = bf16_pack(s.x * f, s.y * f, s.z * f, s.w * f);
-    } else {
-      *sum = s;
+// dz of a tile of the piece's logits.  Columns past the vocabulary are zeros: what multiplies dz reads groups of eight.
+template <class S>
+__global__ __launch_bounds__(S::kThreads) void xent_dz_kernel(XentArgs p) {
+  __shared__ __attribute__((aligned(1024))) char lds[S::kLds];
+  const int n = *p.count, left = min(p.piece, p.V - p.v0);
+  int ta, tb;
+  if (!tile_of(blockIdx.x, div_up(left, S::kA), div_up(n, S::kB), ta, tb)) return;
+  const int a0 = ta * S::kA, b0 = tb * S::kB;
+  typename S::Acc acc = {};
+  Gemm<S, kRows, kRows>::tile(acc, Operand{p.weight + p.v0 * p.weight_stride, p.weight_stride, left, nullptr},
+                             Operand{p.dense, p.D, n, nullptr}, a0, b0, 0, p.D, (SIP_LDS char*)lds);
+  const int lane = threadIdx.x & 63, v0 = a0 + wave_a<S>();
+  const float f = p.logit_scale * kLog2e;
+#pragma unroll
+  for (int j = 0; j < S::kTB; ++j) {
+    const int i = b0 + wave_b<S>() + 16 * j + (lane & 15);
+    const bool live = i < n;
+    const int row = live ? p.rows[i] : 0;
+    const int target = live ? p.targets[row] - p.v0 : -1;
+    const float lse = live ? p.lse_in[row] * kLog2e : 0.0f, g = !live ? 0.0f : p.grad_loss ? p.grad_loss[row] : 1.0f;
+#pragma unroll
+    for (int t = 0; t < S::kTA; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) acc[t][j][r] = g * __builtin_amdgcn_exp2f(__builtin_fmaf(acc[t][j][r], f, -lse));
+    if (__any(target >= v0 && target < v0 + S::kWaveA) || v0 + S::kWaveA > left) {
+      const float at_target = live ? g * expm1f(-p.loss_in[row]) : 0.0f;
+#pragma unroll
+      for (int t = 0; t < S::kTA; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int v = v0 + 16 * t + acc_a(lane) + r;
+          if (v >= left || v == target) acc[t][j][r] = v >= left ? 0.0f : at_target;
+        }
     }
   }
+  store_tile<S>((SIP_LDS char*)lds, a0, p.piece, [&](int i, int j) { return acc[i][j]; },
+                [&](int b) { return b0 + b < n ? p.dz + (long long)(b0 + b) * p.piece : nullptr; });
 }
 
-// grad_weight of a piece's rows.
-__global__ __launch_bounds__(kGemmThreads) void xent_grad_weight_kernel(XentArgs p) {
-  const int n = *p.count, a0 = blockIdx.x * kTileA, b0 = blockIdx.y * kTileB;
-  const int left = p.V - p.v0;
-  f32x16 acc{};
-  gemm_tile<kCols, kCols>(acc, Operand{p.dense, p.D, p.D, nullptr}, Operand{p.dz, p.piece, p.piece, nullptr}, a0, b0, 0, n);
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  const int d_first = a0 + 32 * (w & 1), v = b0 + 32 * (w >> 1) + (lane & 31);
-  if (v >= left) return;
+template <class S>
+__device__ inline f32x4* sum_tile(const Parts& parts, int part, int tile) {
+  return reinterpret_cast<f32x4*>(parts.sum) + ((long long)part * parts.tiles + tile) * (S::kA * S::kB / 4) + threadIdx.x;
+}
+
+template <class S>
+__device__ inline void store_grad_hidden(const XentArgs& p, SIP_LDS char* lds, const typename S::Acc& acc, int a0, int b0, int n) {
   const float f = p.out_scale;
-  for (int r = 0; r < 16; r += 4) {
-    const int d = d_first + acc_a(r, lane);
-    if (d < p.D)
-      *reinterpret_cast<uint2*>(p.grad_weight + (p.v0 + (long long)v) * p.gw_stride + d) =
-          bf16_pack(acc[r] * f, acc[r + 1] * f, acc[r + 2] * f, acc[r + 3] * f);
+  store_tile<S>(lds, a0, p.D, [&](int i, int j) { return acc[i][j] * f; },
+                [&](int b) { return b0 + b < n ? p.grad_hidden + p.rows[b0 + b] * p.gh_stride : nullptr; });
+}
+
+// grad_hidden of a piece, a part of whose entries blockIdx.y names, added to what the pieces before it gave.  The last
+// piece's kernel stores the result itself where nothing else has a part in it.
+template <class S>
+__global__ __launch_bounds__(S::kThreads) void xent_grad_hidden_kernel(XentArgs p) {
+  __shared__ __attribute__((aligned(1024))) char lds[S::kLds];
+  const int n = *p.count, tiles_a = div_up(p.D, S::kA);
+  int ta, tb;
+  if (!tile_of(blockIdx.x, tiles_a, div_up(n, S::kB), ta, tb)) return;
+  const int a0 = ta * S::kA, b0 = tb * S::kB, left = min(p.piece, p.V - p.v0);
+  const int k_begin = min(left, (int)blockIdx.y * p.hidden_parts.split), k_end = min(left, k_begin + p.hidden_parts.split);
+  typename S::Acc acc = {};
+  Gemm<S, kCols, kRows>::tile(acc, Operand{p.weight + p.v0 * p.weight_stride, p.weight_stride, p.D, nullptr},
+                             Operand{p.dz, p.piece, n, nullptr}, a0, b0, k_begin, k_end, (SIP_LDS char*)lds);
+  f32x4* sum = sum_tile<S>(p.hidden_parts, blockIdx.y, tb * tiles_a + ta);
+  const bool last = gridDim.y == 1 && p.v0 + p.piece >= p.V;
+#pragma unroll
+  for (int i = 0; i < S::kTA; ++i)
+#pragma unroll
+    for (int j = 0; j < S::kTB; ++j, sum += S::kThreads) {
+      if (p.v0) acc[i][j] += *sum;
+      if (!last) *sum = acc[i][j];
+    }
+  if (last) store_grad_hidden<S>(p, (SIP_LDS char*)lds, acc, a0, b0, n);
+}
+
+// The parts of grad_hidden (or of grad_weight's rows of a piece), added up in their order: workgroup (x, y) joins block y of each
+// wave's in tile x.
+template <class S, bool HIDDEN>
+__global__ __launch_bounds__(S::kThreads) void xent_join_kernel(XentArgs p) {
+  const Parts& parts = HIDDEN ? p.hidden_parts : p.weight_parts;
+  const int tiles_a = div_up(p.D, S::kA), ta = blockIdx.x % tiles_a, tb = blockIdx.x / tiles_a, lane = threadIdx.x & 63;
+  const int i = blockIdx.y / S::kTB, j = blockIdx.y % S::kTB;
+  const int a = ta * S::kA + wave_a<S>() + 16 * i + acc_a(lane), b = tb * S::kB + wave_b<S>() + 16 * j + (lane & 15);
+  if (a >= p.D || b >= (HIDDEN ? *p.count : min(p.piece, p.V - p.v0))) return;
+  const f32x4* sum = sum_tile<S>(parts, 0, blockIdx.x) + blockIdx.y * S::kThreads;
+  f32x4 total = {};
+  for (int k = 0; k < parts.count; ++k, sum += (long long)parts.tiles * (S::kA * S::kB / 4)) total += *sum;
+  uint16_t* to = HIDDEN ? p.grad_hidden + p.rows[b] * p.gh_stride : p.grad_weight + (p.v0 + (long long)b) * p.gw_stride;
+  *reinterpret_cast<u32x2*>(to + a) = bf16_pack(total * p.out_scale);
+}
+
+// grad_weight of a piece's rows, or the part of its sums over the tokens that blockIdx.y names.
+template <class S>
+__global__ __launch_bounds__(S::kThreads) void xent_grad_weight_kernel(XentArgs p) {
+  __shared__ __attribute__((aligned(1024))) char lds[S::kLds];
+  const int n = *p.count, left = min(p.piece, p.V - p.v0), tiles_a = div_up(p.D, S::kA);
+  int ta, tb;
+  if (!tile_of(blockIdx.x, tiles_a, div_up(left, S::kB), ta, tb)) return;
+  const int a0 = ta * S::kA, b0 = tb * S::kB;
+  const int k_begin = min(n, (int)blockIdx.y * p.weight_parts.split), k_end = min(n, k_begin + p.weight_parts.split);
+  typename S::Acc acc = {};
+  Gemm<S, kCols, kCols>::tile(acc, Operand{p.dense, p.D, p.D, nullptr}, Operand{p.dz, p.piece, left, nullptr}, a0, b0, k_begin, k_end,
+                              (SIP_LDS char*)lds);
+  if (gridDim.y > 1) {
+    f32x4* sum = sum_tile<S>(p.weight_parts, blockIdx.y, tb * tiles_a + ta);
+#pragma unroll
+    for (int i = 0; i < S::kTA; ++i)
+#pragma unroll
+      for (int j = 0; j < S::kTB; ++j, sum += S::kThreads) *sum = acc[i][j];
+    return;
   }
+  const float f = p.out_scale;
+  store_tile<S>((SIP_LDS char*)lds, a0, p.D, [&](int i, int j) { return acc[i][j] * f; },
+                [&](int b) { return b0 + b < left ? p.grad_weight + (p.v0 + b0 + (long long)b) * p.gw_stride : nullptr; });
 }
 
 }  // namespace sip
