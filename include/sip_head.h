@@ -37,9 +37,9 @@ extern "C" {
  * logit_scale is 1, or the reciprocal of the temperature that the tokens were sampled with.  A row
  * whose target lies outside [0, V) -- a masked token -- costs nothing: loss and lse are 0, and
  * whatever its hidden state holds (NaN included) goes nowhere.  Logits are made a tile at a time from
- * bf16 operands with fp32 sums and never written; maxima and sums of exponentials are fp32.  The loss
- * is formed as ln(1 + sum_{v != target} exp(z_v - z_target)), so that it keeps its relative accuracy
- * for a token that is nearly certain.
+ * bf16 operands with fp32 sums and never written; maxima and sums of exponentials are fp32, the
+ * target's own logit is summed in fp64.  The loss is formed as ln(1 + sum_{v != target} exp(z_v -
+ * z_target)), so that it keeps its relative accuracy for a token that is nearly certain.
  *
  *  hidden   [N, hidden_stride] bf16, N * hidden_stride up to 2^30.
  *  weight   [V, weight_stride] bf16.
@@ -66,9 +66,10 @@ sip_status sip_xent_forward(const void* hidden, int32_t N, int32_t D, int64_t hi
  *  grad_loss    [N] fp32, NULL = all ones.
  *  grad_hidden  [N, grad_hidden_stride] bf16, NULL = not wanted; rows of masked tokens are zero.
  *  grad_weight  [V, grad_weight_stride] bf16, NULL = not wanted.  Both are overwritten.
- * The logits are made again, a piece of the vocabulary at a time; dz of a piece is held as bf16 (without
- * scale * logit_scale, which the fp32 sums are multiplied with), sums over the vocabulary and over
- * the tokens are fp32 across pieces, and the gradients are rounded once.
+ * The logits are made again, a piece of the vocabulary at a time; dz of a piece is held as bf16, in
+ * calls of up to 64 tokens as the sum of two bf16 (without scale * logit_scale, which the fp32 sums
+ * are multiplied with), sums over the vocabulary and over the tokens are fp32 across pieces, and the
+ * gradients are rounded once.
  */
 sip_status sip_xent_backward(const void* hidden, int32_t N, int32_t D, int64_t hidden_stride, const void* weight,
                              int32_t V, int64_t weight_stride, const int32_t* targets, float logit_scale,

@@ -16,34 +16,51 @@ inline bool workspace_ok(const void* p, size_t have, size_t need) {
   return p && (reinterpret_cast<uintptr_t>(p) & 255u) == 0 && have >= need;
 }
 
-// Tiles of the cross entropy's products, by how many tokens there are; the wide ones where they fill the chip.
+// Tiles of the cross entropy's products.
 typedef sip::GemmShape<256, 256, 128, 64, 3, 2> Wide;
-typedef sip::GemmShape<256, 128, 128, 64, 3, 3> Half;
 typedef sip::GemmShape<256, 64, 64, 64, 4, 3> Quarter;
 typedef sip::GemmShape<128, 32, 32, 32, 4, 4> Narrow;
 typedef sip::GemmShape<128, 128, 64, 64, 2, 2> Small;
-enum XentShape { kWide, kHalf, kQuarter, kNarrow, kSmall };
+typedef sip::GemmShape<64, 32, 16, 32, 4, 4> Tiny;
+enum XentShape { kWide, kQuarter, kNarrow, kSmall, kTiny };
+constexpr int kShapeA[] = {256, 256, 128, 128, 64}, kShapeB[] = {256, 64, 32, 128, 32}, kShapeWaveA[] = {128, 64, 32, 64, 16};
 
 inline int tiles(long long n, int tile) { return (int)((n + tile - 1) / tile); }
 constexpr int kChip = 256;                             // workgroups of a compute unit each
 
-// What a product of a x b with sums over k costs in Wide or Small tiles, the sums dealt out in `splits` parts: rounds of
-// workgroups -- one a compute unit, or two --, each with a start and an end worth 512 k; two Small tiles take nine tenths of
-// the time of a Wide one, which does twice as much (300 tokens, V = 151643, D = 2048: 52 and 56 us a round).
-double tiles_cost(XentShape s, long long a, long long b, int k, int splits) {
-  const int side = s == kWide ? 256 : 128, at_once = s == kWide ? kChip : 2 * kChip;
-  return (double)tiles(tiles(a, side) * (long long)tiles(b, side) * splits, at_once) * (tiles(k, splits) + 512) * (s == kWide ? 1.0 : 0.9);
+// What a product of a x b with sums over k, dealt out in `parts`, is expected to take in us, from products of one round (a unit of 64 k, one
+// workgroup on its compute unit; each further one at once; how many LDS has room for) and of many rounds of one unit (a
+// round's start and end), by tile: D = 8192, 2048 x 32 to 4096 x 256, and 262144 x 2000 of D = 64.
+double tiles_cost(XentShape s, long long a, long long b, long long k, int parts) {
+  constexpr double kUnitUs[] = {1.13, 0.68, 0.25, 0.92, 0.18}, kFurther[] = {0.0, 0.0, 0.20, 0.23, 0.08}, kEnds[] = {7.0, 5.1, 3.0, 5.2, 2.8};
+  constexpr int kAtOnce[] = {1, 1, 2, 2, 3};
+  const long long each = tiles((long long)tiles(a, kShapeA[s]) * tiles(b, kShapeB[s]) * parts, kChip);     // of a compute unit
+  const long long rounds = each / kAtOnce[s], rest = each % kAtOnce[s];
+  const double units = tiles(tiles(k, parts), 64);
+  const double us = rounds * (units * (kUnitUs[s] + kFurther[s] * (kAtOnce[s] - 1)) + kEnds[s]) +
+                    (rest ? units * (kUnitUs[s] + kFurther[s] * (rest - 1)) + kEnds[s] : 0.0);
+  // the head's rows come from memory once (5.2 TB/s, 4.5 in the smallest tiles), and from cache for every further row of tiles (17)
+  const double read = 2e-6 * a * k / (s == kTiny ? 4.5 : 5.2) + 2e-6 * a * k / 17.0 * (tiles(b, kShapeB[s]) - 1);
+  return std::max(us, read) + 0.4 * std::min(us, read);   // (the one hides the other in part)
 }
-XentShape cheaper(long long a, long long b, int k) {
-  return tiles_cost(kWide, a, b, k, 1) <= tiles_cost(kSmall, a, b, k, 1) ? kWide : kSmall;
+// The tile that is expected to take the least time, and into how many parts it pays to deal the sums (at most `most`).
+struct Cheapest { XentShape shape; int parts; };
+Cheapest cheapest(std::initializer_list<XentShape> among, long long a, long long b, long long k, int most = 1) {
+  Cheapest c{*among.begin(), 1};
+  double best = -1.0;
+  for (XentShape s : among)
+    for (int n = 1; n <= most && (n == 1 || k / n >= 256); ++n) {
+      const double cost = tiles_cost(s, a, b, k, n) + (n > 1 ? 6.0 + 4e-6 * n * a * b : 0.0);              // (the join)
+      if (best < 0.0 || cost < best) { best = cost; c = {s, n}; }
+    }
+  return c;
 }
-// The logits of `tokens` against a rows of the head: the narrowest tile that holds all tokens, or the cheaper one.
-XentShape shape_for(int a, int tokens, int D) {
-  return tokens <= 32 ? kNarrow : tokens <= 64 ? kQuarter : tokens <= 128 ? kHalf : cheaper(a, tokens, D);
-}
-int shape_a(XentShape s) { return s == kNarrow || s == kSmall ? 128 : 256; }
-int shape_b(XentShape s) { return s == kWide ? 256 : s == kQuarter ? 64 : s == kNarrow ? 32 : 128; }
-int shape_wave_a(XentShape s) { return s == kWide || s == kHalf ? 128 : s == kNarrow ? 32 : 64; }
+XentShape score_shape(int a, int tokens, int D) { return cheapest({kWide, kQuarter, kNarrow, kSmall, kTiny}, a, tokens, D).shape; }
+
+// Up to here a token's dz is held in two bf16 parts, as two rows: dz's rounding is an error of its own in every gradient, and
+// where few tokens make it up it may all go one way.  These calls are bound by reading the head and writing its gradient:
+// V = 128256, D = 4096 take 850 us instead of 762 for 64 tokens, 735 instead of 717 for one.
+constexpr int kTwoPartRows = 64;
 
 // How a cross entropy of this shape is cut, and where its parts lie in the workspace.
 struct XentPlan {
@@ -51,21 +68,21 @@ struct XentPlan {
   int parts;                    // waves' partial sums of a token
   int piece;                    // vocabulary entries whose dz is held at once
   XentShape score_piece, hidden, weight;
+  int rows_each;                // rows of dz that a token has
   sip::Parts hidden_parts, weight_parts;   // (without their room)
-  size_t count, rows, target_z, part, dense, dz, hidden_sum, weight_sum, bytes;
+  size_t count, rows, part, dense, dz, hidden_sum, weight_sum, bytes;
 };
 
 XentPlan xent_plan(int32_t N, int32_t V, int32_t D, bool backward) {
   XentPlan p{};
-  p.score = shape_for(V, N, D);
-  p.parts = tiles(V, shape_a(p.score)) * (shape_a(p.score) / shape_wave_a(p.score));
+  p.score = score_shape(V, N, D);
+  p.parts = tiles(V, kShapeA[p.score]) * (kShapeA[p.score] / kShapeWaveA[p.score]);
   size_t at = 0;
   auto take = [&](size_t n) { const size_t here = at; at += head_align(n); return here; };
   p.count = take(4);
   p.rows = take((size_t)N * 4);
   // the two directions' own parts share the room behind
   const size_t both = at;
-  p.target_z = take((size_t)N * 4);
   p.part = take((size_t)N * p.parts * 8);
   p.bytes = at;
   if (backward) {
@@ -73,32 +90,19 @@ XentPlan xent_plan(int32_t N, int32_t V, int32_t D, bool backward) {
     const int pieces = tiles(V, (int)std::min<long long>(most, 1 << 20));
     p.piece = tiles(tiles(V, pieces), 256) * 256;
     const int left = std::min(p.piece, V);
-    p.score_piece = shape_for(left, N, D);
-    // A product with few tiles and a long sum has that dealt out in so many parts that it takes the least time.
-    auto deal = [](auto&& shapes, int k, auto&& cost_of, XentShape& shape, int& count) {
-      double best = 0.0;
-      for (XentShape s : shapes)
-        for (int n = 1; n <= 128 && (n == 1 || k / n >= 256); ++n) {
-          const double cost = cost_of(s, n) + (n > 1 ? 256.0 : 0.0);                // (the join)
-          if (best == 0.0 || cost < best) { best = cost; shape = s; count = n; }
-        }
-    };
-    const std::initializer_list<XentShape> square = {kWide, kSmall};
-    int parts = 1;
-    if (N <= 128)
-      deal(std::initializer_list<XentShape>{shape_for(left, N, D)}, left, [&](XentShape s, int n) {
-        return (double)tiles((long long)tiles(D, shape_a(s)) * n, kChip) * (tiles(left, n) + 512);
-      }, p.hidden, parts);
-    else
-      deal(square, left, [&](XentShape s, int n) { return tiles_cost(s, D, N, left, n); }, p.hidden, parts);
-    p.hidden_parts = {nullptr, tiles(D, shape_a(p.hidden)) * tiles(N, shape_b(p.hidden)), parts, tiles(tiles(left, parts), 64) * 64};
-    deal(square, N, [&](XentShape s, int n) { return tiles_cost(s, D, left, N, n); }, p.weight, parts);
-    p.weight_parts = {nullptr, tiles(D, shape_a(p.weight)) * tiles(left, shape_b(p.weight)), parts, tiles(tiles(N, parts), 64) * 64};
-    auto room = [](const sip::Parts& q, XentShape s) { return (size_t)q.count * q.tiles * shape_a(s) * shape_b(s) * 4; };
+    p.rows_each = N <= kTwoPartRows ? 2 : 1;
+    p.score_piece = p.rows_each == 2 ? cheapest({kQuarter, kNarrow, kSmall, kTiny}, left, N, D).shape : score_shape(left, N, D);
+    const long long dz_rows = (long long)N * p.rows_each;
+    const Cheapest h = cheapest({kWide, kNarrow, kSmall}, D, dz_rows, left, 128), w = cheapest({kWide, kSmall}, D, left, dz_rows, 128);
+    p.hidden = h.shape;
+    p.weight = w.shape;
+    p.hidden_parts = {nullptr, tiles(D, kShapeA[h.shape]) * tiles(dz_rows, kShapeB[h.shape]), h.parts, tiles(tiles(left, h.parts), 64) * 64};
+    p.weight_parts = {nullptr, tiles(D, kShapeA[w.shape]) * tiles(left, kShapeB[w.shape]), w.parts, tiles(tiles(dz_rows, w.parts), 64) * 64};
+    auto room = [](const sip::Parts& q, XentShape s) { return (size_t)q.count * q.tiles * kShapeA[s] * kShapeB[s] * 4; };
     at = both;
-    p.dense = take((size_t)N * D * 2);
-    p.dz = take((size_t)N * p.piece * 2);
-    p.hidden_sum = take(p.hidden_parts.count == 1 && p.piece >= V ? 0 : room(p.hidden_parts, p.hidden));
+    p.dense = take((size_t)dz_rows * D * 2);
+    p.dz = take((size_t)dz_rows * p.piece * 2);
+    p.hidden_sum = take(p.hidden_parts.count == 1 && p.piece >= V && p.rows_each == 1 ? 0 : room(p.hidden_parts, p.hidden));
     p.weight_sum = take(p.weight_parts.count == 1 ? 0 : room(p.weight_parts, p.weight));
     p.bytes = std::max(p.bytes, at);
   }
@@ -108,10 +112,10 @@ XentPlan xent_plan(int32_t N, int32_t V, int32_t D, bool backward) {
 // f(S{}) with the tile's type, one of those named.
 template <XentShape> struct ShapeType;
 template <> struct ShapeType<kWide> { typedef Wide type; };
-template <> struct ShapeType<kHalf> { typedef Half type; };
 template <> struct ShapeType<kQuarter> { typedef Quarter type; };
 template <> struct ShapeType<kNarrow> { typedef Narrow type; };
 template <> struct ShapeType<kSmall> { typedef Small type; };
+template <> struct ShapeType<kTiny> { typedef Tiny type; };
 template <XentShape... AMONG, class F>
 void with_shape(XentShape s, F f) { (void)((s == AMONG && (f(typename ShapeType<AMONG>::type{}), true)) || ...); }
 // Workgroups for n tiles of which each XCD takes an eighth (sip_xent.h, tile_of).
@@ -143,12 +147,12 @@ sip::XentArgs xent_args(const void* hidden, int32_t N, int32_t D, int64_t hidden
   a.logit_scale = logit_scale;
   a.count = reinterpret_cast<int*>(ws + pl.count);
   a.rows = reinterpret_cast<int*>(ws + pl.rows);
-  a.target_z = reinterpret_cast<float*>(ws + pl.target_z);
   a.part = reinterpret_cast<float2*>(ws + pl.part);
   a.parts = pl.parts;
   a.dense = reinterpret_cast<uint16_t*>(ws + pl.dense);
   a.dz = reinterpret_cast<uint16_t*>(ws + pl.dz);
   a.piece = pl.piece;
+  a.rows_each = pl.rows_each;
   a.hidden_parts = pl.hidden_parts; a.hidden_parts.sum = reinterpret_cast<float*>(ws + pl.hidden_sum);
   a.weight_parts = pl.weight_parts; a.weight_parts.sum = reinterpret_cast<float*>(ws + pl.weight_sum);
   return a;
@@ -230,12 +234,12 @@ sip_status sip_xent_forward(const void* hidden, int32_t N, int32_t D, int64_t hi
   sip::XentArgs a = xent_args(hidden, N, D, hidden_stride, weight, V, weight_stride, targets, logit_scale, pl, workspace);
   a.loss = loss; a.lse = lse;
   hipLaunchKernelGGL(sip::xent_rows_kernel, dim3(1), dim3(1024), 0, stream, a);
-  with_shape<kWide, kHalf, kQuarter, kNarrow, kSmall>(pl.score, [&](auto shape) {
+  with_shape<kWide, kQuarter, kNarrow, kSmall, kTiny>(pl.score, [&](auto shape) {
     typedef decltype(shape) S;
     hipLaunchKernelGGL(sip::xent_forward_kernel<S>, dim3(tile_grid((long long)tiles(V, S::kA) * tiles(N, S::kB))),
                        dim3(S::kThreads), 0, stream, a);
   });
-  hipLaunchKernelGGL(sip::xent_loss_kernel, dim3(tiles(N, 4)), dim3(256), 0, stream, a);
+  hipLaunchKernelGGL(sip::xent_loss_kernel, dim3(N), dim3(256), 0, stream, a);
   return launched();
 }
 
@@ -263,17 +267,19 @@ sip_status sip_xent_backward(const void* hidden, int32_t N, int32_t D, int64_t h
   for (int v0 = 0; v0 < V; v0 += pl.piece) {
     a.v0 = v0;
     const int left = std::min(pl.piece, V - v0);
-    with_shape<kWide, kHalf, kQuarter, kNarrow, kSmall>(pl.score_piece, [&](auto shape) {
+    auto make_dz = [&](auto shape, auto two_parts) {
       typedef decltype(shape) S;
-      hipLaunchKernelGGL(sip::xent_dz_kernel<S>, dim3(tile_grid((long long)tiles(left, S::kA) * tiles(N, S::kB))),
+      hipLaunchKernelGGL((sip::xent_dz_kernel<S, decltype(two_parts)::value>), dim3(tile_grid((long long)tiles(left, S::kA) * tiles(N, S::kB))),
                          dim3(S::kThreads), 0, stream, a);
-    });
+    };
+    if (pl.rows_each == 2) with_shape<kQuarter, kNarrow, kSmall, kTiny>(pl.score_piece, [&](auto shape) { make_dz(shape, std::true_type()); });
+    else with_shape<kWide, kQuarter, kNarrow, kSmall, kTiny>(pl.score_piece, [&](auto shape) { make_dz(shape, std::false_type()); });
     if (grad_hidden)
-      with_shape<kWide, kHalf, kQuarter, kNarrow, kSmall>(pl.hidden, [&](auto shape) {
+      with_shape<kWide, kNarrow, kSmall>(pl.hidden, [&](auto shape) {
         typedef decltype(shape) S;
         hipLaunchKernelGGL(sip::xent_grad_hidden_kernel<S>, dim3(tile_grid(pl.hidden_parts.tiles), pl.hidden_parts.count), dim3(S::kThreads), 0,
                            stream, a);
-        if (pl.hidden_parts.count > 1 && v0 + pl.piece >= V)
+        if ((pl.hidden_parts.count > 1 || pl.rows_each > 1) && v0 + pl.piece >= V)
           hipLaunchKernelGGL((sip::xent_join_kernel<S, true>), dim3(pl.hidden_parts.tiles, S::kTA * S::kTB), dim3(S::kThreads), 0, stream, a);
       });
     if (grad_weight)

@@ -299,3 +299,22 @@ def test_weights_beyond_four_gigabytes():
     assert float((gw[at].double() - gw_want).norm()) <= 2.0 ** -8 * float(gw_want.norm())
     gh_want = p @ weight[at].double()
     assert float((gh.double() - gh_want).norm()) <= 2.0 ** -8 * float(gh_want.norm())
+
+
+@pytest.mark.parametrize("N,V,D", [(1, 20000, 256), (1, 40, 2048), (3, 4097, 520), (20, 9000, 1000), (64, 3001, 136)])
+def test_few_tokens_lose_no_more_than_the_result_s_rounding(N, V, D):
+    """Up to 64 tokens dz is held in two bf16 parts (2^-8 of 2^-8 of a term is lost).  What remains: the result's own
+    rounding, 2^-8; the probabilities' error (see check_loss); sums in fp32, a random walk of 2^-24 of the terms."""
+    hidden, weight, targets = make(N, V, D, seed=21 + N)
+    _, _, gh, gw = run_all(hidden, weight, targets, 0.8, None, 0.5)
+    ref = reference(hidden, weight, targets, 0.8, None, 0.5)
+    p_err = 8 * 2.0 ** -24 * math.sqrt(D) * float(ref[4].max()) + 2.0 ** -20
+    for got, want, terms, count in ((gh, ref[2], ref[5], V), (gw, ref[3], ref[6], N)):
+        bound = 2.0 ** -8 * want.abs() + (2.0 ** -16 + p_err + 4 * 2.0 ** -24 * math.sqrt(count)) * 1.01 * terms + 1e-30
+        assert ((got.double() - want).abs() <= bound).all()
+
+
+@pytest.mark.parametrize("N,V,D", [(4096, 300, 64), (6000, 129, 24), (300, 30000, 16), (65536, 5000, 16), (40000, 7000, 72)])
+def test_sums_dealt_out_and_vocabularies_in_pieces(N, V, D):
+    """Long sums over few outputs are dealt out and joined; many tokens cut the vocabulary into pieces."""
+    check_all(*make(N, V, D, seed=N, masked=0.05), scale=1.0 / N)
