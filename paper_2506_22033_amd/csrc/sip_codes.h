@@ -22,6 +22,7 @@ struct CodesArgs {
 
 // Eight weights a lane, a group in group / 8 neighbouring lanes: its bounds by exchange between them.  Reads 16 bytes a lane
 // and writes 4.  What a lane computes -- eight IEEE divisions above all -- takes less time than its share of the reads.
+// Bound by memory: V = 256000, D = 4096, groups of 128 0.75 ms, 3.5 TB/s read and written (a plain copy moves 4.9).
 template <int GROUP>
 __global__ __launch_bounds__(256) void quantize_kernel(CodesArgs p) {
   const uint32_t per_row = (uint32_t)p.D / 8, total = (uint32_t)p.V * per_row;              // (below 2^31)
@@ -223,6 +224,9 @@ constexpr int few_tiles(int group, bool scales_bf16, int units, int mt) {
 // how many came after it.)
 // Products: 16 + q against the states, from - (16 + zero) times the group's sum of the states on; the scale on the fp32
 // sum of a group.
+// Bound by reading the head: one row, V = 128256, D = 4096, groups of 128 51 us, 5.3 TB/s.  With groups of 32, fp32 scales and
+// 7 fp32 states (two rows of tiles), V = 151643, D = 2080, 106 us, 2.0 TB/s: a tile a turn is all that registers hold then, and
+// scales, sums by group and the codes' conversion take the vector units longer than the reads take.
 template <int GROUP, bool SCALES_BF16, int UNITS, int MT>
 __global__ __launch_bounds__(kFewWaves * 64) void head_few_kernel(CodesArgs p) {
   constexpr int NT = few_tiles(GROUP, SCALES_BF16, UNITS, MT);
@@ -399,7 +403,6 @@ __global__ __launch_bounds__(kFewWaves * 64) void head_few_kernel(CodesArgs p) {
 // ---- more rows: tiles of the product, the hidden states through LDS
 
 // Rows of a block of MT * 16: as many whole states as fit it.
-constexpr int kManyWaves = 8, kManyTiles = 2, kManyEntries = kManyWaves * kManyTiles * 16;   // vocabulary entries of a workgroup
 __host__ __device__ inline int block_states(int mt, bool hidden_bf16) { return mt * 16 / rows_of_state(hidden_bf16); }
 __host__ __device__ inline int many_units(int D) { return (D + 255) / 256 * 2; }             // of 128 entries
 __host__ __device__ inline int many_groups(int D, int group) { return (D / group + 31) / 32 * 32; }
@@ -445,17 +448,21 @@ __global__ __launch_bounds__(256) void head_rows_kernel(CodesArgs p, int mt) {
   }
 }
 
-// 256 vocabulary entries by MT * 16 rows.  A wave has 32 of the entries and all rows.  It goes through a pair of units -- 256
-// entries of a state, a line of each row's codes -- at a time: states through LDS, codes and scales straight into registers,
-// all of the next pair's loaded while this one's products are made.
+// WAVES * NT * 16 vocabulary entries by MT * 16 rows: 256 entries, or 64 where tiles of 256 would leave compute units without
+// one (31 fp32 states, V = 5164, D = 5568: 62 us instead of 116).  A wave has NT * 16 of the entries and all rows, so that a
+// code becomes a bf16 value once.  It goes through a pair of units -- 256 entries of a state, a line of each row's codes -- at a
+// time: states through LDS, codes and scales straight into registers, all of the next pair's loaded while this one's products
+// are made.
 //   sum_g s (sum_d (16 + q) x - (16 + zero) sum_d x)
 // The second part is a product over groups of its own, in 3 x 3 bf16 parts of which the six that matter are taken: with
-// 8 row tiles it saves 32 multiplications a group and tile of entries.  Matrix cores and vector units are about
-// equally busy with groups of 64.
-template <int GROUP, bool SCALES_BF16, int MT>
-__global__ __launch_bounds__(kManyWaves * 64) void head_many_kernel(CodesArgs p) {
-  constexpr int NT = kManyTiles, kGroups = 256 / GROUP, kPairBytes = 8 * MT * 1024, kLoads = kPairBytes / (kManyWaves * 1024);
-  constexpr int kPitch = kManyEntries + 4;
+// 8 row tiles it saves 32 multiplications a group and tile of entries.
+// 256 rows, V = 152064, D = 4096, fp32 logits, groups of 128, 64, 32: 381, 447, 605 us, 837, 714, 527 TFLOP/s.  In groups of 64
+// matrix cores are busy for 30 % of it and vector units for 40 (half of that the scales' multiplications), which two waves of a
+// SIMD do not hide behind each other altogether; reads further ahead or four waves of half the entries changed nothing.
+template <int GROUP, bool SCALES_BF16, int MT, int WAVES, int NT>
+__global__ __launch_bounds__(WAVES * 64) void head_many_kernel(CodesArgs p) {
+  constexpr int kEntries = WAVES * NT * 16, kGroups = 256 / GROUP, kPairBytes = 8 * MT * 1024, kLoads = kPairBytes / (WAVES * 1024);
+  constexpr int kPitch = kEntries + 4, kScaleBytes = SCALES_BF16 ? 2 : 4;
   constexpr int kRing = 2 * kPairBytes, kOut = MT * 16 * kPitch * 4;
   __shared__ __attribute__((aligned(1024))) char lds_bytes[kRing > kOut ? kRing : kOut];
   SIP_LDS char* lds = (SIP_LDS char*)lds_bytes;
@@ -463,7 +470,7 @@ __global__ __launch_bounds__(kManyWaves * 64) void head_many_kernel(CodesArgs p)
   const int each = rows_of_state(p.hidden_bf16), states = block_states(MT, p.hidden_bf16), blocks = (p.B + states - 1) / states;
   // the blocks of one tile of entries on one XCD, one after the other
   const int tile = (int)(blockIdx.x >> 3) / blocks * 8 + (blockIdx.x & 7), block = (int)(blockIdx.x >> 3) % blocks;
-  if (tile * kManyEntries >= p.V) return;
+  if (tile * kEntries >= p.V) return;
   const ManyLayout layout(p.D, GROUP, MT);
   const char* from = p.states + block * layout.block;
   const int pairs = many_units(p.D) / 2, groups = p.D / GROUP;
@@ -473,17 +480,17 @@ __global__ __launch_bounds__(kManyWaves * 64) void head_many_kernel(CodesArgs p)
     const u32x4 buffer = {(uint32_t)at, (uint32_t)(at >> 32) & 0xffff, kPairBytes, 0x00020000};
 #pragma unroll
     for (int l = 0; l < kLoads; ++l) {
-      const uint32_t piece = (l * kManyWaves + wave) * 1024;
+      const uint32_t piece = (l * WAVES + wave) * 1024;
       asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
                    :: "s"(lds0 + (uint32_t)(pair & 1) * kPairBytes + piece), "v"(piece + lane * 16), "s"(buffer) : "memory");
     }
   };
   uint32_t row[NT];
 #pragma unroll
-  for (int t = 0; t < NT; ++t) row[t] = min(tile * kManyEntries + (wave * NT + t) * 16 + (lane & 15), p.V - 1);
+  for (int t = 0; t < NT; ++t) row[t] = min(tile * kEntries + (wave * NT + t) * 16 + (lane & 15), p.V - 1);
   const SIP_GLOBAL uint8_t* zeros = (const SIP_GLOBAL uint8_t*)(p.zeros ? p.zeros : reinterpret_cast<const uint8_t*>(kEights));
   const uint32_t stride = (uint32_t)p.codes_stride;
-  u32x4 codes[NT][2], next_codes[NT][2];
+  u32x4 next_codes[NT][2];
   auto load_codes = [&](int pair) {
 #pragma unroll
     for (int t = 0; t < NT; ++t)
@@ -497,12 +504,17 @@ __global__ __launch_bounds__(kManyWaves * 64) void head_many_kernel(CodesArgs p)
     if constexpr (SCALES_BF16) return __builtin_bit_cast(float, (uint32_t)((const SIP_GLOBAL uint16_t*)p.scales)[at] << 16);
     else return ((const SIP_GLOBAL float*)p.scales)[at];
   };
-  float scales[NT][kGroups], next_scales[NT][kGroups];
+  float scales[NT][kGroups];
+  uint32_t next_scales[NT][kGroups];                       // as they are loaded: to shift them there would wait for them
   auto load_scales = [&](int pair) {
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
-      for (int g = 0; g < kGroups; ++g) next_scales[t][g] = scale_at(t, pair * kGroups + g);
+      for (int g = 0; g < kGroups; ++g) {
+        const uint32_t at = row[t] * groups + min(pair * kGroups + g, groups - 1);
+        if constexpr (SCALES_BF16) next_scales[t][g] = ((const SIP_GLOBAL uint16_t*)p.scales)[at];
+        else next_scales[t][g] = ((const SIP_GLOBAL uint32_t*)p.scales)[at];
+      }
   };
   load_states(0);
   load_scales(0);
@@ -512,12 +524,27 @@ __global__ __launch_bounds__(kManyWaves * 64) void head_many_kernel(CodesArgs p)
   for (int g0 = 0; g0 < groups; g0 += 32) {
     bf16x8 w[NT][3];
 #pragma unroll
-    for (int t = 0; t < NT; ++t)
+    for (int t = 0; t < NT; ++t) {
+      float scale[8], zero[8];
+      if (groups % 8 == 0) {                               // eight at once
+        const uint32_t at = row[t] * groups + min(g0 + quad * 8, groups - 8);
+        GroupScales<8, SCALES_BF16> eight;
+        eight.s.load((const SIP_GLOBAL uint8_t*)p.scales + (uint64_t)at * kScaleBytes, ((uint64_t)p.scales & 3) != 0);
+        eight.z.load(zeros + (p.zeros ? at : 0), ((uint64_t)zeros & 3) != 0);
+        eight.settle();
+#pragma unroll
+        for (int e = 0; e < 8; ++e) { scale[e] = eight.scale(e); zero[e] = eight.zero(e); }
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const int g = g0 + quad * 8 + e;
+          scale[e] = scale_at(t, g);
+          zero[e] = (float)zeros[p.zeros ? row[t] * groups + min(g, groups - 1) : 0];
+        }
+      }
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const int g = g0 + quad * 8 + e;
-        const uint32_t at = row[t] * groups + min(g, groups - 1);
-        float f = scale_at(t, g) * (-16.0f - (float)zeros[p.zeros ? at : 0]);
+        float f = scale[e] * (-16.0f - zero[e]);
 #pragma unroll
         for (int part = 0; part < 3; ++part) {
           const uint32_t top = __builtin_bit_cast(uint32_t, f) & 0xffff0000u;
@@ -525,6 +552,7 @@ __global__ __launch_bounds__(kManyWaves * 64) void head_many_kernel(CodesArgs p)
           f -= __builtin_bit_cast(float, top);
         }
       }
+    }
 #pragma unroll
     for (int m = 0; m < MT; ++m) {
       bf16x8 x[3];
@@ -540,18 +568,41 @@ __global__ __launch_bounds__(kManyWaves * 64) void head_many_kernel(CodesArgs p)
             total[t][m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[part], w[t][sum - part], total[t][m], 0, 0, 0);
     }
   }
+  // A step: the products of a tile of rows and a group, and with them the multiplications of the step before and the reads of
+  // the one behind.
+  constexpr int kEach = GROUP / 32, kSteps = MT * kGroups;
   const CodeValues code_values;
-  f32x4 acc[NT][MT];
   for (int pair = 0; pair < pairs; ++pair) {
+    bf16x8 w[NT][8];                                       // product c of the pair: dword c / 2 of load c % 2
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
 #pragma unroll
-      for (int e = 0; e < 2; ++e) codes[t][e] = UnitOrder<32, 2>::order(e, next_codes[t][e]);
+      for (int e = 0; e < 2; ++e) {
+        const u32x4 codes = UnitOrder<32, 2>::order(e, next_codes[t][e]);
 #pragma unroll
-      for (int g = 0; g < kGroups; ++g) scales[t][g] = next_scales[t][g];
+        for (int j = 0; j < 4; ++j) w[t][2 * j + e] = __builtin_bit_cast(bf16x8, code_values(codes[j]));
+      }
+#pragma unroll
+      for (int g = 0; g < kGroups; ++g) scales[t][g] = __builtin_bit_cast(float, SCALES_BF16 ? next_scales[t][g] << 16 : next_scales[t][g]);
     }
     // this pair's states have arrived, and everybody has read the last one's
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    const uint32_t states_at = lds0 + (uint32_t)(pair & 1) * kPairBytes + lane * 16;
+    bf16x8 x[2][kEach];
+    f32x4 acc[2][NT];
+    auto read = [&](int step) {
+#pragma unroll
+      for (int j = 0; j < kEach; ++j)
+        x[step & 1][j] = *(const SIP_LDS bf16x8*)(uintptr_t)(states_at + ((step % kGroups * kEach + j) * MT + step / kGroups) * 1024);
+    };
+    auto scale = [&](int step) {
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          total[t][step / kGroups][r] = __builtin_fmaf(scales[t][step % kGroups], acc[step & 1][t][r], total[t][step / kGroups][r]);
+    };
+    read(0);
     if (pair + 1 < pairs) {
       load_states(pair + 1);
       load_scales(pair + 1);
@@ -559,26 +610,23 @@ __global__ __launch_bounds__(kManyWaves * 64) void head_many_kernel(CodesArgs p)
     }
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int c = 0; c < 8; ++c) {                          // product of the pair: dword c / 2 of load c % 2
-      const bool starts = c % (GROUP / 32) == 0, ends = (c + 1) % (GROUP / 32) == 0;
-      bf16x8 w[NT];
+    for (int step = 0; step < kSteps; ++step) {
+      if (step + 1 < kSteps) read(step + 1);
 #pragma unroll
-      for (int t = 0; t < NT; ++t) w[t] = __builtin_bit_cast(bf16x8, code_values(codes[t][c & 1][c >> 1]));
-#pragma unroll
-      for (int m = 0; m < MT; ++m) {
-        const bf16x8 x = *(const SIP_LDS bf16x8*)(uintptr_t)(lds0 + (uint32_t)(pair & 1) * kPairBytes + (c * MT + m) * 1024 + lane * 16);
+      for (int j = 0; j < kEach; ++j)
 #pragma unroll
         for (int t = 0; t < NT; ++t)
-          acc[t][m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, w[t], starts ? f32x4{} : acc[t][m], 0, 0, 0);
+          acc[step & 1][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[step & 1][j], w[t][step % kGroups * kEach + j], j == 0 ? f32x4{} : acc[step & 1][t], 0, 0, 0);
+      if (step > 0) scale(step - 1);
+      __builtin_amdgcn_sched_group_barrier(0x100, kEach, 0);
+#pragma unroll
+      for (int n = 0; n < kEach * NT; ++n) {               // in turn: a product, and multiplications while it runs
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x002, 4 / kEach, 0);
       }
-      if (ends)
-#pragma unroll
-        for (int t = 0; t < NT; ++t)
-#pragma unroll
-          for (int m = 0; m < MT; ++m)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) total[t][m][r] = __builtin_fmaf(scales[t][c / (GROUP / 32)], acc[t][m][r], total[t][m][r]);
+      __builtin_amdgcn_sched_barrier(0);
     }
+    scale(kSteps - 1);
   }
   asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
   SIP_LDS float* out = (SIP_LDS float*)lds;
@@ -589,10 +637,10 @@ __global__ __launch_bounds__(kManyWaves * 64) void head_many_kernel(CodesArgs p)
 #pragma unroll
       for (int r = 0; r < 4; ++r) out[(m * 16 + quad * 4 + r) * kPitch + (wave * NT + t) * 16 + (lane & 15)] = total[t][m][r];
   __syncthreads();
-  const int v = tile * kManyEntries + (threadIdx.x & (kManyEntries - 1));
-  for (int b = threadIdx.x / kManyEntries; b < states && block * states + b < p.B; b += kManyWaves * 64 / kManyEntries) {
+  const int v = tile * kEntries + (threadIdx.x & (kEntries - 1));
+  for (int b = threadIdx.x / kEntries; b < states && block * states + b < p.B; b += WAVES * 64 / kEntries) {
     float z = 0.0f;
-    for (int r = (b + 1) * each - 1; r >= b * each; --r) z += out[r * kPitch + (threadIdx.x & (kManyEntries - 1))];
+    for (int r = (b + 1) * each - 1; r >= b * each; --r) z += out[r * kPitch + (threadIdx.x & (kEntries - 1))];
     if (v < p.V) {
       const long long at = (block * states + b) * p.logits_stride + v;
       if (p.logits_bf16) static_cast<__bf16*>(p.logits)[at] = (__bf16)z;

@@ -194,7 +194,7 @@ bool few_rows(const sip::CodesArgs& a, hipStream_t stream) {
   return a.group == 32 ? few_rows_of<32>(a, stream) : a.group == 64 ? few_rows_of<64>(a, stream) : few_rows_of<128>(a, stream);
 }
 
-// head_many_kernel: blocks of 64 rows where one holds them all, else of 128.
+// head_many_kernel: blocks of 64 rows where one holds them all, else of 128; entries as its comment says.
 int many_tiles(int32_t B, bool hidden_bf16) { return B <= sip::block_states(4, hidden_bf16) ? 4 : 8; }
 size_t many_bytes(int32_t B, int32_t D, int32_t group, bool hidden_bf16) {
   const int mt = many_tiles(B, hidden_bf16);
@@ -204,14 +204,15 @@ template <int GROUP>
 void many_rows_of(const sip::CodesArgs& a, hipStream_t stream) {
   const int mt = many_tiles(a.B, a.hidden_bf16), blocks = tiles(a.B, sip::block_states(mt, a.hidden_bf16));
   hipLaunchKernelGGL(sip::head_rows_kernel<GROUP>, dim3(tiles(sip::many_groups(a.D, GROUP), 4), blocks * mt), dim3(256), 0, stream, a, mt);
-  const dim3 grid(tiles(tiles(a.V, sip::kManyEntries), 8) * 8 * blocks), threads(sip::kManyWaves * 64);
-  if (a.scales_bf16) {
-    if (mt == 4) hipLaunchKernelGGL((sip::head_many_kernel<GROUP, true, 4>), grid, threads, 0, stream, a);
-    else hipLaunchKernelGGL((sip::head_many_kernel<GROUP, true, 8>), grid, threads, 0, stream, a);
-  } else {
-    if (mt == 4) hipLaunchKernelGGL((sip::head_many_kernel<GROUP, false, 4>), grid, threads, 0, stream, a);
-    else hipLaunchKernelGGL((sip::head_many_kernel<GROUP, false, 8>), grid, threads, 0, stream, a);
-  }
+  auto launch = [&](auto row_tiles, auto waves, auto nt) {
+    constexpr int kMt = decltype(row_tiles)::value, kWaves = decltype(waves)::value, kNt = decltype(nt)::value;
+    const dim3 grid(tiles(tiles(a.V, kWaves * kNt * 16), 8) * 8 * blocks), threads(kWaves * 64);
+    if (a.scales_bf16) hipLaunchKernelGGL((sip::head_many_kernel<GROUP, true, kMt, kWaves, kNt>), grid, threads, 0, stream, a);
+    else hipLaunchKernelGGL((sip::head_many_kernel<GROUP, false, kMt, kWaves, kNt>), grid, threads, 0, stream, a);
+  };
+  const bool narrow = (long long)tiles(a.V, 256) * blocks < kChip;
+  if (mt == 4) narrow ? launch(Int<4>(), Int<4>(), Int<1>()) : launch(Int<4>(), Int<8>(), Int<2>());
+  else narrow ? launch(Int<8>(), Int<4>(), Int<1>()) : launch(Int<8>(), Int<8>(), Int<2>());
 }
 
 }  // namespace
