@@ -232,3 +232,37 @@ def test_what_the_binding_refuses():
         sip.sip_head_quantize(torch.zeros(4, 48, dtype=BF16, device=DEV), 32)
     with pytest.raises(TypeError):
         sip.sip_head_quantize(torch.zeros(4, 64, device=DEV), 32)
+
+
+@pytest.mark.parametrize("B,V,D,group", [(40, 66000, 512, 64), (40, 65537, 96, 32), (200, 33001, 2048, 32), (300, 23000, 640, 128),
+                                         (150, 33300, 1088, 64)])
+@pytest.mark.parametrize("hidden", [BF16, F32])
+def test_many_rows_over_many_tiles(B, V, D, group, hidden):
+    for scales in (BF16, F32):
+        check(*make(B, V, D, group, True, hidden, scales, seed=B), F32)
+
+
+@pytest.mark.parametrize("B,V,D,group", [(2, 301, 512, 32), (40, 301, 512, 32), (70, 66000, 256, 32), (40, 130, 2048, 64), (40, 130, 160, 32)])
+def test_scales_and_zeros_at_any_element(B, V, D, group):
+    """Bases that are aligned to an element only give the bits that aligned ones do."""
+    for dtype in (BF16, F32):
+        x, codes, s, z = make(B, V, D, group, True, scales=dtype, seed=6)
+        want = check(x, codes, s, z, F32)
+        for by in (1, 2, 3):
+            s_room = torch.full((s.numel() + 8,), math.nan, dtype=dtype, device=DEV)
+            z_room = torch.full((z.numel() + 8,), 255, dtype=torch.uint8, device=DEV)
+            s_there = s_room[by:by + s.numel()].view_as(s).copy_(s)
+            z_there = z_room[by:by + z.numel()].view_as(z).copy_(z)
+            assert torch.equal(sip.sip_head_logits(x, codes, s_there, z_there), want)
+
+
+@pytest.mark.parametrize("exponent", [-100, -62, -50, 50, 62, 100])
+def test_quantizer_far_from_one(exponent):
+    """Quotients by scales at either end of fp32's range and around 2^+-60 are the division's, bit for bit."""
+    g = torch.Generator(device=DEV).manual_seed(9)
+    w = torch.ldexp(torch.randn(400, 512, generator=g, device=DEV), torch.tensor(exponent, device=DEV)).bfloat16()
+    for group in (32, 64, 128):
+        for zeros in (False, True):
+            for scales in (BF16, F32):
+                for a, b in zip(sip.sip_head_quantize(w, group, use_zeros=zeros, scales_dtype=scales), quantized(w, group, zeros, scales)):
+                    assert (a is None and b is None) or torch.equal(a, b)
