@@ -69,7 +69,7 @@ struct XentPlan {
   int piece;                    // vocabulary entries whose dz is held at once
   XentShape score_piece, hidden, weight;
   int rows_each;                // rows of dz that a token has
-  sip::Parts hidden_parts, weight_parts;   // (without their room)
+  sip::Parts hidden_parts, weight_parts;   // for all N rows (without their room)
   size_t count, rows, part, dense, dz, hidden_sum, weight_sum, bytes;
 };
 
@@ -96,8 +96,8 @@ XentPlan xent_plan(int32_t N, int32_t V, int32_t D, bool backward) {
     const Cheapest h = cheapest({kWide, kNarrow, kSmall}, D, dz_rows, left, 128), w = cheapest({kWide, kSmall}, D, left, dz_rows, 128);
     p.hidden = h.shape;
     p.weight = w.shape;
-    p.hidden_parts = {nullptr, tiles(D, kShapeA[h.shape]) * tiles(dz_rows, kShapeB[h.shape]), h.parts, tiles(tiles(left, h.parts), 64) * 64};
-    p.weight_parts = {nullptr, tiles(D, kShapeA[w.shape]) * tiles(left, kShapeB[w.shape]), w.parts, tiles(tiles(dz_rows, w.parts), 64) * 64};
+    p.hidden_parts = {nullptr, tiles(D, kShapeA[h.shape]) * tiles(dz_rows, kShapeB[h.shape]), h.parts, 0};
+    p.weight_parts = {nullptr, tiles(D, kShapeA[w.shape]) * tiles(left, kShapeB[w.shape]), w.parts, 0};
     auto room = [](const sip::Parts& q, XentShape s) { return (size_t)q.count * q.tiles * kShapeA[s] * kShapeB[s] * 4; };
     at = both;
     p.dense = take((size_t)dz_rows * D * 2);

@@ -16,7 +16,7 @@ __device__ inline u32x2 bf16_pack(f32x4 x) {
   return u32x2{bf16_bits(x[0]) | (bf16_bits(x[1]) << 16), bf16_bits(x[2]) | (bf16_bits(x[3]) << 16)};
 }
 
-// A product whose long sum is dealt out: part i has the `split` k from i * split on, and its sums lie behind those of the parts
+// A product whose long sum is dealt out: part i has the `split` k (dealt()) from i * split on, and its sums lie behind those of the parts
 // before it, [tiles] of them, tile by tile in the order of the accumulators: a lane's four neighbours, a wave's lanes in a row.
 struct Parts {
   float* sum;
@@ -100,16 +100,22 @@ __global__ __launch_bounds__(256) void xent_gather_kernel(XentArgs p) {
 
 // Which tile a workgroup takes of tiles_a x tiles_b.  The eight XCDs, to which workgroups go in turn, take a run of
 // tiles each; within it eight tiles along a go with one along b before the next, so that the 32 of an XCD that are under
-// way share their rows of either operand in its L2.  False: none is left.
-__device__ inline bool tile_of(int id, int tiles_a, int tiles_b, int& ta, int& tb) {
+// way share their rows of either operand in its L2.  Of `parts` such sets, one after the other, `part` is the one.  False: none is left.
+__device__ inline bool tile_of(int id, int tiles_a, int tiles_b, int parts, int& ta, int& tb, int& part) {
   constexpr int kGroup = 8;
-  const int total = tiles_a * tiles_b, run = (total + 7) / 8;
-  const int local = id >> 3, s = (id & 7) * run + local;
-  if (local >= run || s >= total) return false;
+  const int total = tiles_a * tiles_b * parts, run = (total + 7) / 8;
+  const int local = id >> 3, at = (id & 7) * run + local;
+  if (local >= run || at >= total) return false;
+  part = at / (tiles_a * tiles_b);
+  const int s = at - part * (tiles_a * tiles_b);
   const int first = s / (kGroup * tiles_b) * kGroup, width = min(kGroup, tiles_a - first), r = s - first * tiles_b;
   ta = first + r % width;
   tb = r / width;
   return true;
+}
+__device__ inline bool tile_of(int id, int tiles_a, int tiles_b, int& ta, int& tb) {
+  int part;
+  return tile_of(id, tiles_a, tiles_b, 1, ta, tb, part);
 }
 __host__ __device__ inline int div_up(int a, int b) { return (a + b - 1) / b; }
 
@@ -301,6 +307,18 @@ __global__ __launch_bounds__(S::kThreads) void xent_dz_kernel(XentArgs p) {
   }
 }
 
+// How a launch for up to parts.tiles tiles of parts.count parts deals out `tiles` (1 .. parts.tiles) of `k` terms each: the
+// workgroups and the room of rows that are masked go to those that are not.  2048 tokens of which 922 take part, V = 128256, D =
+// 2048, forward and backward: 1916 us instead of 2165.
+__device__ inline Parts dealt(const Parts& parts, int tiles, int k) {
+  Parts p = parts;
+  if (parts.count > 1) {
+    p.tiles = tiles;
+    p.count = max(parts.count, min(parts.tiles * parts.count / tiles, k / 256));
+  }
+  p.split = div_up(div_up(k, p.count), 64) * 64;
+  return p;
+}
 template <class S>
 __device__ inline f32x4* sum_tile(const Parts& parts, int part, int tile) {
   return reinterpret_cast<f32x4*>(parts.sum) + ((long long)part * parts.tiles + tile) * (S::kA * S::kB / 4) + threadIdx.x;
@@ -313,20 +331,22 @@ __device__ inline void store_grad_hidden(const XentArgs& p, SIP_LDS char* lds, c
                 [&](int b) { return b0 + b < n ? p.grad_hidden + p.rows[b0 + b] * p.gh_stride : nullptr; });
 }
 
-// grad_hidden of a piece, a part of whose entries blockIdx.y names, added to what the pieces before it gave.  The last
+// grad_hidden of a piece, or a part of its sums over the entries, added to what the pieces before it gave.  The last
 // piece's kernel stores the result itself where nothing else has a part in it.
 template <class S>
 __global__ __launch_bounds__(S::kThreads) void xent_grad_hidden_kernel(XentArgs p) {
   __shared__ __attribute__((aligned(1024))) char lds[S::kLds];
-  const int n = *p.count * p.rows_each, tiles_a = div_up(p.D, S::kA);
-  int ta, tb;
-  if (!tile_of(blockIdx.x, tiles_a, div_up(n, S::kB), ta, tb)) return;
+  const int n = *p.count * p.rows_each, tiles_a = div_up(p.D, S::kA), tiles = tiles_a * div_up(n, S::kB);
+  if (tiles == 0) return;
+  const Parts parts = dealt(p.hidden_parts, tiles, min(p.piece, p.V));
+  int ta, tb, part;
+  if (!tile_of(blockIdx.y * gridDim.x + blockIdx.x, tiles_a, div_up(n, S::kB), parts.count, ta, tb, part)) return;
   const int a0 = ta * S::kA, b0 = tb * S::kB, left = min(p.piece, p.V - p.v0);
-  const int k_begin = min(left, (int)blockIdx.y * p.hidden_parts.split), k_end = min(left, k_begin + p.hidden_parts.split);
+  const int k_begin = min(left, part * parts.split), k_end = min(left, k_begin + parts.split);
   typename S::Acc acc = {};
   Gemm<S, kCols, kRows>::tile(acc, Operand{p.weight + p.v0 * p.weight_stride, p.weight_stride, p.D, nullptr},
                              Operand{p.dz, p.piece, n, nullptr}, a0, b0, k_begin, k_end, (SIP_LDS char*)lds);
-  f32x4* sum = sum_tile<S>(p.hidden_parts, blockIdx.y, tb * tiles_a + ta);
+  f32x4* sum = sum_tile<S>(parts, part, tb * tiles_a + ta);
   const bool last = gridDim.y == 1 && p.rows_each == 1 && p.v0 + p.piece >= p.V;
 #pragma unroll
   for (int i = 0; i < S::kTA; ++i)
@@ -342,11 +362,11 @@ __global__ __launch_bounds__(S::kThreads) void xent_grad_hidden_kernel(XentArgs 
 // wave's in tile x.
 template <class S, bool HIDDEN>
 __global__ __launch_bounds__(S::kThreads) void xent_join_kernel(XentArgs p) {
-  const Parts& parts = HIDDEN ? p.hidden_parts : p.weight_parts;
   const int tiles_a = div_up(p.D, S::kA), ta = blockIdx.x % tiles_a, tb = blockIdx.x / tiles_a, lane = threadIdx.x & 63;
   const int i = blockIdx.y / S::kTB, j = blockIdx.y % S::kTB;
   const int a = ta * S::kA + wave_a<S>() + 16 * i + acc_a(lane), b = tb * S::kB + wave_b<S>() + 16 * j + (lane & 15);
   if (a >= p.D || b >= (HIDDEN ? *p.count : min(p.piece, p.V - p.v0))) return;
+  const Parts parts = HIDDEN ? dealt(p.hidden_parts, tiles_a * div_up(*p.count * p.rows_each, S::kB), min(p.piece, p.V)) : p.weight_parts;
   f32x4 total = {};
   for (int row = HIDDEN ? p.rows_each - 1 : 0; row >= 0; --row) {
     // where row b + row * count lies: its tile, its wave and block, its lane
@@ -359,20 +379,20 @@ __global__ __launch_bounds__(S::kThreads) void xent_join_kernel(XentArgs p) {
   *reinterpret_cast<u32x2*>(to + a) = bf16_pack(total * p.out_scale);
 }
 
-// grad_weight of a piece's rows, or the part of its sums over the tokens that blockIdx.y names.
+// grad_weight of a piece's rows, or a part of its sums over the tokens.
 template <class S>
 __global__ __launch_bounds__(S::kThreads) void xent_grad_weight_kernel(XentArgs p) {
   __shared__ __attribute__((aligned(1024))) char lds[S::kLds];
   const int n = *p.count * p.rows_each, left = min(p.piece, p.V - p.v0), tiles_a = div_up(p.D, S::kA);
-  int ta, tb;
-  if (!tile_of(blockIdx.x, tiles_a, div_up(left, S::kB), ta, tb)) return;
+  int ta, tb, part;
+  if (!tile_of(blockIdx.y * gridDim.x + blockIdx.x, tiles_a, div_up(left, S::kB), p.weight_parts.count, ta, tb, part)) return;
   const int a0 = ta * S::kA, b0 = tb * S::kB;
-  const int k_begin = min(n, (int)blockIdx.y * p.weight_parts.split), k_end = min(n, k_begin + p.weight_parts.split);
+  const int split = div_up(div_up(n, p.weight_parts.count), 64) * 64, k_begin = min(n, part * split), k_end = min(n, k_begin + split);
   typename S::Acc acc = {};
   Gemm<S, kCols, kCols>::tile(acc, Operand{p.dense, p.D, p.D, nullptr}, Operand{p.dz, p.piece, left, nullptr}, a0, b0, k_begin, k_end,
                               (SIP_LDS char*)lds);
   if (gridDim.y > 1) {
-    f32x4* sum = sum_tile<S>(p.weight_parts, blockIdx.y, tb * tiles_a + ta);
+    f32x4* sum = sum_tile<S>(p.weight_parts, part, tb * tiles_a + ta);
 #pragma unroll
     for (int i = 0; i < S::kTA; ++i)
 #pragma unroll

@@ -318,3 +318,9 @@ def test_few_tokens_lose_no_more_than_the_result_s_rounding(N, V, D):
 def test_sums_dealt_out_and_vocabularies_in_pieces(N, V, D):
     """Long sums over few outputs are dealt out and joined; many tokens cut the vocabulary into pieces."""
     check_all(*make(N, V, D, seed=N, masked=0.05), scale=1.0 / N)
+
+
+@pytest.mark.parametrize("N,V,D,masked", [(2000, 5000, 64, 0.5), (2000, 5000, 64, 0.97), (500, 30000, 256, 0.6), (60, 30000, 512, 0.7),
+                                          (1500, 40000, 520, 0.55), (30000, 12000, 72, 0.8)])
+def test_sums_dealt_out_among_masked_tokens(N, V, D, masked):
+    check_all(*make(N, V, D, seed=N, masked=masked), scale=1.0 / N)
