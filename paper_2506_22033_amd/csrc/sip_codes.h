@@ -40,8 +40,9 @@ __device__ inline s16x2 group_max(s16x2 x) {
 // Quotients: with r = fl(1 / s), t the product w r corrected once by its remainder, fl(t + r (w - t s)) is w / s correctly rounded
 // (Markstein, 1990), six operations instead of an IEEE division's dozen; for s in the middle of fp32's range, where
 // nothing that matters underflows.
-// Bound by memory: V = 256000, D = 4096, groups of 128 644 us, 4.1 TB/s read and written (a plain copy moves 4.9).  With IEEE
-// divisions, and bounds in fp32 by shuffles, vector units were busy all the time: 751 us.
+// Bound by vector instructions, 180 for a lane's eight weights, close to memory's rate: V = 256000, D = 4096, groups of 128 594 to
+// 644 us, 4.1 to 4.4 TB/s read and written (a plain copy moves 4.9).  With IEEE divisions, and bounds in fp32 by shuffles, it
+// was 220 instructions and 751 us.
 template <int GROUP>
 __global__ __launch_bounds__(256) void quantize_kernel(CodesArgs p) {
   const uint32_t per_row = (uint32_t)p.D / 8, total = (uint32_t)p.V * per_row;              // (below 2^31)
