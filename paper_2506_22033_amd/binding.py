@@ -4,6 +4,7 @@ path runs in the library's kernels.  There is no fallback: without the compiled 
 (or without a GPU) the calls raise."""
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 from typing import Dict, Optional, Tuple
@@ -272,6 +273,20 @@ def sip_state_bytes(slots: int, L_max: int) -> int:
 
 def _nbytes(t: torch.Tensor) -> int:
     return t.numel() * t.element_size()
+
+
+def _on(stream: Optional[torch.cuda.Stream]):
+    """The context in which a call with ``stream=`` allocates, or runs an operation of torch's."""
+    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
+
+
+def _empty(stream: Optional[torch.cuda.Stream], *size, dtype, device) -> torch.Tensor:
+    """torch.empty() for a call on ``stream``: memory of that stream's, which torch hands out again only to what runs behind
+    the call.  (Memory of the current stream's would be handed out while the call still uses it.)"""
+    if stream is None:
+        return torch.empty(*size, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(*size, dtype=dtype, device=device)
 
 
 # (the handle itself: the Stream object that torch.cuda.current_stream() builds around it takes 1.9 us, twice in a

@@ -1,5 +1,8 @@
 """ctypes binding of the vocabulary head's entry points (include/sip_head.h), with torch tensors standing in for device
-pointers.  Argument marshalling only; there is no fallback."""
+pointers.  Argument marshalling only; there is no fallback.
+
+A call runs on ``stream`` (default: torch's current stream).  The outputs and the scratch memory that it allocates because they
+were not supplied belong to that stream, as under ``torch.cuda.stream(stream)``."""
 from __future__ import annotations
 
 import ctypes
@@ -8,7 +11,7 @@ from typing import Optional, Sequence, Tuple
 import torch
 
 from . import binding
-from .binding import SIP_BF16, SIP_F32, SIP_OK, SipError, _nbytes, _ptr, _stream_handle
+from .binding import SIP_BF16, SIP_F32, SIP_OK, SipError, _empty, _nbytes, _on, _ptr, _stream_handle
 
 SIP_MAX_D = 16384
 SIP_MAX_TOKENS = 65536
@@ -78,8 +81,8 @@ def _stride(t: torch.Tensor) -> int:
     return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
 
 
-def _scratch(workspace: Optional[torch.Tensor], need: int, dev) -> torch.Tensor:
-    return workspace if workspace is not None else torch.empty(max(need, 256), dtype=torch.uint8, device=dev)
+def _scratch(workspace: Optional[torch.Tensor], need: int, dev, stream) -> torch.Tensor:
+    return workspace if workspace is not None else _empty(stream, max(need, 256), dtype=torch.uint8, device=dev)
 
 
 # ---- cross entropy
@@ -107,12 +110,12 @@ def sip_xent_forward(hidden: torch.Tensor, weight: torch.Tensor, targets: torch.
     lib = _load()
     N, V, D = _xent_operands(hidden, weight, targets)
     dev = hidden.device
-    loss = torch.empty(N, dtype=torch.float32, device=dev) if loss is None else _vector(loss, "loss", torch.float32, N)
-    lse = torch.empty(N, dtype=torch.float32, device=dev) if lse is None else _vector(lse, "lse", torch.float32, N)
+    loss = _empty(stream, N, dtype=torch.float32, device=dev) if loss is None else _vector(loss, "loss", torch.float32, N)
+    lse = _empty(stream, N, dtype=torch.float32, device=dev) if lse is None else _vector(lse, "lse", torch.float32, N)
     _same_device(hidden, loss, lse, workspace)
     if N == 0:
         return loss, lse
-    ws = _scratch(workspace, 0 if workspace is not None else lib.sip_xent_workspace_bytes(N, V, D, 0), dev)
+    ws = _scratch(workspace, 0 if workspace is not None else lib.sip_xent_workspace_bytes(N, V, D, 0), dev, stream)
     _check(lib.sip_xent_forward(_ptr(hidden), N, D, _stride(hidden), _ptr(weight), V, _stride(weight), _ptr(targets),
                                 logit_scale, _ptr(loss), _ptr(lse), _ptr(ws), _nbytes(ws), _stream_handle(dev, stream)))
     return loss, lse
@@ -135,15 +138,18 @@ def sip_xent_backward(hidden: torch.Tensor, weight: torch.Tensor, targets: torch
         _vector(grad_loss, "grad_loss", torch.float32, N)
     gh = gw = None
     if want_hidden:
-        gh = (torch.empty(N, D, dtype=torch.bfloat16, device=dev) if grad_hidden is None
+        gh = (_empty(stream, N, D, dtype=torch.bfloat16, device=dev) if grad_hidden is None
               else _matrix(grad_hidden, "grad_hidden", (torch.bfloat16,), (N, D)))
     if want_weight:
-        gw = (torch.empty(V, D, dtype=torch.bfloat16, device=dev) if grad_weight is None
+        gw = (_empty(stream, V, D, dtype=torch.bfloat16, device=dev) if grad_weight is None
               else _matrix(grad_weight, "grad_weight", (torch.bfloat16,), (V, D)))
     _same_device(hidden, loss, lse, grad_loss, gh, gw, workspace)
     if N == 0:
-        return gh, None if gw is None else gw.zero_()
-    ws = _scratch(workspace, 0 if workspace is not None else lib.sip_xent_workspace_bytes(N, V, D, 1), dev)
+        if gw is not None:
+            with _on(stream):
+                gw.zero_()
+        return gh, gw
+    ws = _scratch(workspace, 0 if workspace is not None else lib.sip_xent_workspace_bytes(N, V, D, 1), dev, stream)
     _check(lib.sip_xent_backward(_ptr(hidden), N, D, _stride(hidden), _ptr(weight), V, _stride(weight), _ptr(targets),
                                  logit_scale, _ptr(loss), _ptr(lse), _ptr(grad_loss), scale, _ptr(gh),
                                  0 if gh is None else _stride(gh), _ptr(gw), 0 if gw is None else _stride(gw), _ptr(ws),
@@ -183,8 +189,8 @@ def sip_grad_clip(grads, max_norm: float, *, eps: float = 1e-6, norm: Optional[t
     their 2-norm before that, one float32 on the device."""
     lib = _load()
     t = grads if isinstance(grads, GradTable) else GradTable(grads)
-    norm = torch.empty((), dtype=torch.float32, device=t.device) if norm is None else _vector(norm, "norm", torch.float32, 1)
-    ws = _scratch(workspace, 0 if workspace is not None else lib.sip_grad_clip_workspace_bytes(t.n), t.device)
+    norm = _empty(stream, (), dtype=torch.float32, device=t.device) if norm is None else _vector(norm, "norm", torch.float32, 1)
+    ws = _scratch(workspace, 0 if workspace is not None else lib.sip_grad_clip_workspace_bytes(t.n), t.device, stream)
     _check(lib.sip_grad_clip(t.table, t.n, max_norm, eps, _ptr(norm), _ptr(ws), _nbytes(ws), _stream_handle(t.device, stream)))
     return norm
 
@@ -216,11 +222,11 @@ def sip_head_quantize(weight: torch.Tensor, group: int = 128, *, use_zeros: bool
         raise TypeError(f"the width {D} is no multiple of the group {group}")
     dev = weight.device
     if codes is None and scales is None and zeros is None and use_zeros:
-        zeros = torch.empty(V, D // group, dtype=torch.uint8, device=dev)
+        zeros = _empty(stream, V, D // group, dtype=torch.uint8, device=dev)
     if codes is None:
-        codes = torch.empty(V, D // 2, dtype=torch.uint8, device=dev)
+        codes = _empty(stream, V, D // 2, dtype=torch.uint8, device=dev)
     if scales is None:
-        scales = torch.empty(V, D // group, dtype=scales_dtype, device=dev)
+        scales = _empty(stream, V, D // group, dtype=scales_dtype, device=dev)
     if _codes_operands(codes, scales, zeros) != (V, D, group):
         raise TypeError("codes and scales do not fit the weight and the group")
     _same_device(weight, codes, scales, zeros)
@@ -246,12 +252,12 @@ def sip_head_logits(hidden: torch.Tensor, codes: torch.Tensor, scales: torch.Ten
     if hidden.shape[1] != D:
         raise TypeError(f"hidden [B, D] and codes [V, D / 2] differ in D: {hidden.shape[1]} and {D}")
     if out is None:
-        out = torch.empty(B, (V + 7) // 8 * 8, dtype=dtype, device=dev)[:, :V]
+        out = _empty(stream, B, (V + 7) // 8 * 8, dtype=dtype, device=dev)[:, :V]
     _matrix(out, "out", (torch.bfloat16, torch.float32), (B, V))
     _same_device(hidden, codes, scales, zeros, out, workspace)
     if B == 0:
         return out
-    ws = _scratch(workspace, 0 if workspace is not None else lib.sip_head_workspace_bytes(B, V, D, group), dev)
+    ws = _scratch(workspace, 0 if workspace is not None else lib.sip_head_workspace_bytes(B, V, D, group), dev, stream)
     _check(lib.sip_head_logits(_ptr(hidden), B, D, _stride(hidden), _DTYPES[hidden.dtype], _ptr(codes), _stride(codes),
                                _ptr(scales), _DTYPES[scales.dtype], _ptr(zeros), group, V, _ptr(out), _stride(out),
                                _DTYPES[out.dtype], _ptr(ws), _nbytes(ws), _stream_handle(dev, stream)))
