@@ -193,7 +193,7 @@ def sip_sample(logits: torch.Tensor, params: Optional[Dict[str, Optional[torch.T
 
     ``logits`` is a 2-D device tensor whose rows are contiguous; ``V`` (default: its width)
     may be smaller than the row stride.  Outputs and workspace are allocated with torch when
-    not supplied.  Returns (ids [B], logprob ids [B,1+k] or None, logprobs [B,1+k] or None)."""
+    not supplied, as memory of the call's stream.  Returns (ids [B], logprob ids [B,1+k] or None, logprobs [B,1+k] or None)."""
     lib = load()
     if not logits.is_cuda or logits.dim() != 2 or logits.stride(1) != 1:
         raise TypeError("logits must be a 2-D device tensor with contiguous rows")
@@ -209,15 +209,15 @@ def sip_sample(logits: torch.Tensor, params: Optional[Dict[str, Optional[torch.T
             raise TypeError("hist_indptr must have B + 1 entries")
         nnz = hist_tokens.numel()
     if out_ids is None:
-        out_ids = torch.empty(B, dtype=torch.int32, device=dev)
+        out_ids = _empty(stream, B, dtype=torch.int32, device=dev)
     if k_logprobs >= 0:
         if out_lp_ids is None:
-            out_lp_ids = torch.empty(B, 1 + k_logprobs, dtype=torch.int32, device=dev)
+            out_lp_ids = _empty(stream, B, 1 + k_logprobs, dtype=torch.int32, device=dev)
         if out_lp is None:
-            out_lp = torch.empty(B, 1 + k_logprobs, dtype=torch.float32, device=dev)
+            out_lp = _empty(stream, B, 1 + k_logprobs, dtype=torch.float32, device=dev)
     if workspace is None:
         need = sip_workspace_bytes(B, V, dt, nnz, k_logprobs)
-        workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=dev)
+        workspace = _empty(stream, max(need, 256), dtype=torch.uint8, device=dev)
     sp = make_params(params, B)
     status = lib.sip_sample(_ptr(logits), B, V, logits.stride(0), dt, ctypes.byref(sp),
                             _ptr(hist_indptr) if nnz else None, _ptr(hist_tokens) if nnz else None, nnz,
@@ -349,15 +349,15 @@ def sip_sample_state(logits: torch.Tensor, params: Optional[Dict[str, Optional[t
     if not slot_of_row.is_cuda or slot_of_row.dtype != torch.int32 or slot_of_row.numel() != B:
         raise TypeError("slot_of_row must be a device tensor of B x int32")
     if out_ids is None:
-        out_ids = torch.empty(B, dtype=torch.int32, device=dev)
+        out_ids = _empty(stream, B, dtype=torch.int32, device=dev)
     if k_logprobs >= 0:
         if out_lp_ids is None:
-            out_lp_ids = torch.empty(B, 1 + k_logprobs, dtype=torch.int32, device=dev)
+            out_lp_ids = _empty(stream, B, 1 + k_logprobs, dtype=torch.int32, device=dev)
         if out_lp is None:
-            out_lp = torch.empty(B, 1 + k_logprobs, dtype=torch.float32, device=dev)
+            out_lp = _empty(stream, B, 1 + k_logprobs, dtype=torch.float32, device=dev)
     if workspace is None:
         need = sip_workspace_bytes(B, V, dt, B * L_max, k_logprobs)
-        workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=dev)
+        workspace = _empty(stream, max(need, 256), dtype=torch.uint8, device=dev)
     sp = make_params(params, B)
     status = lib.sip_sample_state(_ptr(logits), B, V, logits.stride(0), dt, ctypes.byref(sp), _ptr(state),
                                   _nbytes(state), slots, L_max, _ptr(slot_of_row), seed, step, _ptr(out_ids),
@@ -445,15 +445,15 @@ def sip_sample_sharded(shards, params: Optional[Dict[str, Optional[torch.Tensor]
             raise TypeError("hist_indptr must be int64 with B + 1 entries and hist_tokens int32")
         nnz = hist_tokens.numel()
     if out_ids is None:
-        out_ids = torch.empty(B, dtype=torch.int32, device=dev)
+        out_ids = _empty(stream, B, dtype=torch.int32, device=dev)
     if k_logprobs >= 0:
         if out_lp_ids is None:
-            out_lp_ids = torch.empty(B, 1 + k_logprobs, dtype=torch.int32, device=dev)
+            out_lp_ids = _empty(stream, B, 1 + k_logprobs, dtype=torch.int32, device=dev)
         if out_lp is None:
-            out_lp = torch.empty(B, 1 + k_logprobs, dtype=torch.float32, device=dev)
+            out_lp = _empty(stream, B, 1 + k_logprobs, dtype=torch.float32, device=dev)
     if workspace is None:
         need = sip_workspace_bytes_sharded(B, V_shard, t, dt, nnz, k_logprobs)
-        workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=dev)
+        workspace = _empty(stream, max(need, 256), dtype=torch.uint8, device=dev)
     sp = make_params(params, B)
     status = lib.sip_sample_sharded(st.table, t, B, V_shard, st.stride, dt, ctypes.byref(sp),
                                     _ptr(hist_indptr) if nnz else None, _ptr(hist_tokens) if nnz else None, nnz,
@@ -547,12 +547,12 @@ def sip_sample_call(*, logits: Optional[torch.Tensor] = None, shards=None, V: Op
         c.prompt_indptr, c.prompt_tokens, c.prompt_nnz = _ptr(prompt_indptr), _ptr(prompt_tokens), prompt_tokens.numel()
     c.seed, c.step, c.k_logprobs = seed, step, k_logprobs
     if out_ids is None:
-        out_ids = torch.empty(B, dtype=torch.int32, device=dev)
+        out_ids = _empty(stream, B, dtype=torch.int32, device=dev)
     if k_logprobs >= 0:
         if out_lp_ids is None:
-            out_lp_ids = torch.empty(B, 1 + k_logprobs, dtype=torch.int32, device=dev)
+            out_lp_ids = _empty(stream, B, 1 + k_logprobs, dtype=torch.int32, device=dev)
         if out_lp is None:
-            out_lp = torch.empty(B, 1 + k_logprobs, dtype=torch.float32, device=dev)
+            out_lp = _empty(stream, B, 1 + k_logprobs, dtype=torch.float32, device=dev)
     c.out_ids, c.out_lp_ids, c.out_lp = _ptr(out_ids), _ptr(out_lp_ids), _ptr(out_lp)
     if host_ids is not None or host_flag is not None:
         if host_ids is None or host_flag is None or not host_ids.is_pinned() or not host_flag.is_pinned():
@@ -562,7 +562,7 @@ def sip_sample_call(*, logits: Optional[torch.Tensor] = None, shards=None, V: Op
         need = int(lib.sip_call_workspace_bytes(ctypes.byref(c)))
         if need == 0:
             raise SipError(SIP_ERR_INVALID_ARG)
-        workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+        workspace = _empty(stream, need, dtype=torch.uint8, device=dev)
     c.workspace, c.workspace_bytes = _ptr(workspace), _nbytes(workspace)
     c.hip_stream = _stream_handle(dev, stream)
     status = lib.sip_sample_call(ctypes.byref(c))
