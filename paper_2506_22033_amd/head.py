@@ -70,10 +70,10 @@ def _vector(t: torch.Tensor, name: str, dtype, n: int) -> torch.Tensor:
     return t
 
 
-def _same_device(first: torch.Tensor, *others: Optional[torch.Tensor]) -> None:
-    for t in others:
-        if t is not None and t.device != first.device:
-            raise TypeError(f"tensors of one call must be on one device: {first.device} and {t.device}")
+def _same_device(device: torch.device, *tensors: Optional[torch.Tensor]) -> None:
+    for t in tensors:
+        if t is not None and t.device != device:
+            raise TypeError(f"tensors of one call must be on one device: {device} and {t.device}")
 
 
 def _stride(t: torch.Tensor) -> int:
@@ -82,7 +82,12 @@ def _stride(t: torch.Tensor) -> int:
 
 
 def _scratch(workspace: Optional[torch.Tensor], need: int, dev, stream) -> torch.Tensor:
-    return workspace if workspace is not None else _empty(stream, max(need, 256), dtype=torch.uint8, device=dev)
+    if workspace is None:
+        return _empty(stream, max(need, 256), dtype=torch.uint8, device=dev)
+    _same_device(dev, workspace)
+    if not workspace.is_contiguous():
+        raise TypeError("a workspace must be contiguous")
+    return workspace
 
 
 # ---- cross entropy
@@ -97,7 +102,7 @@ def _xent_operands(hidden, weight, targets):
     if hidden.shape[1] != weight.shape[1]:
         raise TypeError(f"hidden [N, D] and weight [V, D] differ in D: {hidden.shape[1]} and {weight.shape[1]}")
     _vector(targets, "targets", torch.int32, hidden.shape[0])
-    _same_device(hidden, weight, targets)
+    _same_device(hidden.device, weight, targets)
     return hidden.shape[0], weight.shape[0], hidden.shape[1]
 
 
@@ -112,7 +117,7 @@ def sip_xent_forward(hidden: torch.Tensor, weight: torch.Tensor, targets: torch.
     dev = hidden.device
     loss = _empty(stream, N, dtype=torch.float32, device=dev) if loss is None else _vector(loss, "loss", torch.float32, N)
     lse = _empty(stream, N, dtype=torch.float32, device=dev) if lse is None else _vector(lse, "lse", torch.float32, N)
-    _same_device(hidden, loss, lse, workspace)
+    _same_device(dev, loss, lse)
     if N == 0:
         return loss, lse
     ws = _scratch(workspace, 0 if workspace is not None else lib.sip_xent_workspace_bytes(N, V, D, 0), dev, stream)
@@ -143,7 +148,7 @@ def sip_xent_backward(hidden: torch.Tensor, weight: torch.Tensor, targets: torch
     if want_weight:
         gw = (_empty(stream, V, D, dtype=torch.bfloat16, device=dev) if grad_weight is None
               else _matrix(grad_weight, "grad_weight", (torch.bfloat16,), (V, D)))
-    _same_device(hidden, loss, lse, grad_loss, gh, gw, workspace)
+    _same_device(dev, loss, lse, grad_loss, gh, gw)
     if N == 0:
         if gw is not None:
             with _on(stream):
@@ -190,6 +195,7 @@ def sip_grad_clip(grads, max_norm: float, *, eps: float = 1e-6, norm: Optional[t
     lib = _load()
     t = grads if isinstance(grads, GradTable) else GradTable(grads)
     norm = _empty(stream, (), dtype=torch.float32, device=t.device) if norm is None else _vector(norm, "norm", torch.float32, 1)
+    _same_device(t.device, norm)
     ws = _scratch(workspace, 0 if workspace is not None else lib.sip_grad_clip_workspace_bytes(t.n), t.device, stream)
     _check(lib.sip_grad_clip(t.table, t.n, max_norm, eps, _ptr(norm), _ptr(ws), _nbytes(ws), _stream_handle(t.device, stream)))
     return norm
@@ -229,7 +235,7 @@ def sip_head_quantize(weight: torch.Tensor, group: int = 128, *, use_zeros: bool
         scales = _empty(stream, V, D // group, dtype=scales_dtype, device=dev)
     if _codes_operands(codes, scales, zeros) != (V, D, group):
         raise TypeError("codes and scales do not fit the weight and the group")
-    _same_device(weight, codes, scales, zeros)
+    _same_device(dev, codes, scales, zeros)
     _check(lib.sip_head_quantize(_ptr(weight), V, D, _stride(weight), group, _ptr(codes), _stride(codes), _ptr(scales),
                                  _DTYPES[scales.dtype], _ptr(zeros), _stream_handle(dev, stream)))
     return codes, scales, zeros
@@ -254,7 +260,7 @@ def sip_head_logits(hidden: torch.Tensor, codes: torch.Tensor, scales: torch.Ten
     if out is None:
         out = _empty(stream, B, (V + 7) // 8 * 8, dtype=dtype, device=dev)[:, :V]
     _matrix(out, "out", (torch.bfloat16, torch.float32), (B, V))
-    _same_device(hidden, codes, scales, zeros, out, workspace)
+    _same_device(dev, codes, scales, zeros, out)
     if B == 0:
         return out
     ws = _scratch(workspace, 0 if workspace is not None else lib.sip_head_workspace_bytes(B, V, D, group), dev, stream)

@@ -1,0 +1,34 @@
+"""The vocabulary head's binding: what it takes, what it refuses, and what its options mean."""
+import pytest
+import torch
+
+import paper_2506_22033_amd as sip
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+BF16 = torch.bfloat16
+
+
+def test_clipping_refuses_memory_that_the_device_cannot_reach():
+    """Raised before anything is enqueued."""
+    g = torch.ones(8, device=DEV)
+    need = sip.sip_grad_clip_workspace_bytes(1)
+    for kw in (dict(workspace=torch.empty(need, dtype=torch.uint8)), dict(norm=torch.empty(1)),
+               dict(workspace=torch.empty(1, dtype=torch.uint8, device=DEV).expand(need))):
+        with pytest.raises(TypeError):
+            sip.sip_grad_clip([g], 0.5, **kw)
+    assert (g == 1.0).all()
+
+
+def test_a_workspace_is_contiguous_device_memory():
+    h, w, t = torch.zeros(2, 64, dtype=BF16, device=DEV), torch.zeros(9, 64, dtype=BF16, device=DEV), torch.zeros(
+        2, dtype=torch.int32, device=DEV)
+    loss, lse = sip.sip_xent_forward(h, w, t)
+    codes, scales, zeros = sip.sip_head_quantize(w, 64)
+    for ws in (torch.empty(1 << 20, dtype=torch.uint8), torch.empty(1, dtype=torch.uint8, device=DEV).expand(1 << 20),
+               torch.empty(1 << 21, dtype=torch.uint8, device=DEV)[::2]):
+        for call in (lambda: sip.sip_xent_forward(h, w, t, workspace=ws),
+                     lambda: sip.sip_xent_backward(h, w, t, loss, lse, workspace=ws),
+                     lambda: sip.sip_head_logits(h, codes, scales, zeros, workspace=ws)):
+            with pytest.raises(TypeError):
+                call()
