@@ -220,14 +220,15 @@ def sip_head_quantize(weight: torch.Tensor, group: int = 128, *, use_zeros: bool
                       stream: Optional[torch.cuda.Stream] = None
                       ) -> Tuple[torch.Tensor, torch.Tensor, Optional[torch.Tensor]]:
     """(codes [V, D / 2], scales [V, D / group], zeros or None) of bf16 ``weight`` [V, D].  Outputs are allocated when
-    not supplied; where ``codes`` and ``scales`` are, ``zeros`` says whether the groups have zero points."""
+    not supplied, ``zeros`` if ``use_zeros``; where both ``codes`` and ``scales`` are, ``zeros`` alone says whether the groups
+    have zero points."""
     lib = _load()
     _matrix(weight, "weight", (torch.bfloat16,))
     V, D = weight.shape
     if group <= 0 or D % group != 0:
         raise TypeError(f"the width {D} is no multiple of the group {group}")
     dev = weight.device
-    if codes is None and scales is None and zeros is None and use_zeros:
+    if zeros is None and use_zeros and (codes is None or scales is None):
         zeros = _empty(stream, V, D // group, dtype=torch.uint8, device=dev)
     if codes is None:
         codes = _empty(stream, V, D // 2, dtype=torch.uint8, device=dev)

@@ -32,3 +32,21 @@ def test_a_workspace_is_contiguous_device_memory():
                      lambda: sip.sip_head_logits(h, codes, scales, zeros, workspace=ws)):
             with pytest.raises(TypeError):
                 call()
+
+
+def test_zero_points_are_made_unless_both_outputs_are_there_without_them():
+    w = (torch.randn(40, 128, generator=torch.Generator().manual_seed(0)) + 1.0).to(DEV, BF16)
+    want = sip.sip_head_quantize(w, 64)
+    assert want[2] is not None
+    codes, scales, zeros = (torch.empty_like(x) for x in want)
+    for kw in (dict(codes=codes), dict(scales=scales), dict(zeros=zeros), dict(codes=codes, zeros=zeros),
+               dict(codes=codes, scales=scales, zeros=zeros)):
+        got = sip.sip_head_quantize(w, 64, **kw)
+        assert all(torch.equal(a, b) for a, b in zip(got, want)), kw.keys()
+        for k, v in kw.items():
+            assert got[("codes", "scales", "zeros").index(k)] is v
+    plain = sip.sip_head_quantize(w, 64, use_zeros=False)
+    assert plain[2] is None and not torch.equal(plain[0], want[0])
+    for kw in (dict(codes=codes, scales=scales), dict(codes=codes, use_zeros=False), dict(scales=scales, use_zeros=False)):
+        got = sip.sip_head_quantize(w, 64, **kw)
+        assert got[2] is None and torch.equal(got[0], plain[0]) and torch.equal(got[1], plain[1])
