@@ -78,7 +78,7 @@ def _same_device(device: torch.device, *tensors: Optional[torch.Tensor]) -> None
 
 def _stride(t: torch.Tensor) -> int:
     """Row stride; that of a single row says nothing, and its width serves."""
-    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
 
 
 def _scratch(workspace: Optional[torch.Tensor], need: int, dev, stream) -> torch.Tensor:

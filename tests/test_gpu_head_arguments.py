@@ -50,3 +50,32 @@ def test_zero_points_are_made_unless_both_outputs_are_there_without_them():
     for kw in (dict(codes=codes, scales=scales), dict(codes=codes, use_zeros=False), dict(scales=scales, use_zeros=False)):
         got = sip.sip_head_quantize(w, 64, **kw)
         assert got[2] is None and torch.equal(got[0], plain[0]) and torch.equal(got[1], plain[1])
+
+
+def _single(t, pad):
+    """The one row of `t` as a row of a matrix whose row stride is its width and `pad`; aligned to 16 bytes."""
+    wide = torch.zeros(17, t.shape[1] + pad, dtype=t.dtype, device=DEV)
+    wide[16, :t.shape[1]] = t[0]
+    return wide[16:17, :t.shape[1]]
+
+
+def test_the_stride_of_a_single_row_says_nothing():
+    """One row of a matrix of an odd width."""
+    g = torch.Generator().manual_seed(3)
+    h, w = torch.randn(1, 64, generator=g).to(DEV, BF16), torch.randn(1, 64, generator=g).to(DEV, BF16)
+    many = torch.randn(50, 64, generator=g).to(DEV, BF16)
+    t = torch.zeros(1, dtype=torch.int32, device=DEV)
+    for pad in (3, 4):
+        for x, y in ((h, many), (h, w)):
+            xs, ys = _single(x, pad), y if y.shape[0] > 1 else _single(y, pad)
+            want = sip.sip_xent_forward(x, y, t)
+            assert all(torch.equal(a, b) for a, b in zip(sip.sip_xent_forward(xs, ys, t), want))
+            grads = sip.sip_xent_backward(x, y, t, *want)
+            for a, b in zip(sip.sip_xent_backward(xs, ys, t, *want, grad_hidden=_single(h, pad)), grads):
+                assert torch.equal(a, b)
+        codes, scales, zeros = sip.sip_head_quantize(many, 32)
+        assert torch.equal(sip.sip_head_logits(_single(h, pad), codes, scales, zeros), sip.sip_head_logits(h, codes, scales, zeros))
+        one = sip.sip_head_quantize(w, 32)
+        got = sip.sip_head_quantize(_single(w, pad), 32, codes=_single(one[0], pad))
+        assert all(torch.equal(a, b) for a, b in zip(got, one))
+        assert torch.equal(sip.sip_head_logits(h, _single(one[0], pad), *one[1:]), sip.sip_head_logits(h, *one))
