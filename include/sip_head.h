@@ -34,7 +34,7 @@ extern "C" {
  *   lse[i]  = ln sum_v exp(z[i, v])
  *   loss[i] = lse[i] - z[i, targets[i]]            (= -log-probability of the token)
  *
- * logit_scale is 1, or the reciprocal of the temperature that the tokens were sampled with.  A row
+ * logit_scale is 1, or the reciprocal of the temperature that the tokens were sampled with, 0 for an infinite one.  A row
  * whose target lies outside [0, V) -- a masked token -- costs nothing: loss and lse are 0, and
  * whatever its hidden state holds (NaN included) goes nowhere.  Logits are made a tile at a time from
  * bf16 operands with fp32 sums and never written; maxima and sums of exponentials are fp32, the

@@ -164,7 +164,14 @@ __global__ __launch_bounds__(S::kThreads) void xent_forward_kernel(XentArgs p) {
                              a0, b0, 0, p.D, (SIP_LDS char*)lds);
   // Maxima and sums as the logits are made: acc, times f for a base of 2.  (The target's logit is made by xent_loss_kernel.)
   const int lane = threadIdx.x & 63, v0 = a0 + wave_a<S>();
-  const float f = p.logit_scale * kLog2e;
+  float f = p.logit_scale * kLog2e;
+  if (f == 0.0f) {                                         // logits of 0, multiplied here: 0 times what marks an entry below is NaN
+#pragma unroll
+    for (int t = 0; t < S::kTA; ++t)
+#pragma unroll
+      for (int j = 0; j < S::kTB; ++j) acc[t][j] *= f;
+    f = 1.0f;
+  }
 #pragma unroll
   for (int j = 0; j < S::kTB; ++j) {
     const int i = b0 + wave_b<S>() + 16 * j + (lane & 15);
