@@ -258,10 +258,10 @@ __global__ __launch_bounds__(256) void xent_loss_kernel(XentArgs p) {
       join(wave_part[o].x, wave_part[o].y);
     }
     zt *= p.logit_scale;
-    const float gap = (float)((double)m * 0.69314718055994530942 + (double)logf(s) - zt);   // ln of the others' mass over the target's
-    const float loss = fmaxf(gap, 0.0f) + log1pf(expf(-fabsf(gap)));
-    p.loss[row] = gap != gap ? gap : loss;
-    p.lse[row] = (float)(zt + loss);
+    const double others = (double)m * 0.69314718055994530942 + (double)logf(s);            // ln of the others' mass
+    const float gap = (float)(others - zt), rest = log1pf(expf(-fabsf(gap)));
+    p.loss[row] = gap != gap ? gap : fmaxf(gap, 0.0f) + rest;
+    p.lse[row] = (float)((gap > 0.0f ? others : zt) + rest);                                // (from the larger: it does not cancel)
   }
 }
 

@@ -25,3 +25,22 @@ def test_an_infinite_temperature(N, V, D):
         assert ((loss - want).abs() <= 2.0 ** -20 * want).all() and ((lse - want).abs() <= 2.0 ** -20 * want).all()
         for g in sip.sip_xent_backward(hidden, weight, targets, loss, lse, logit_scale=zero):
             assert not g.any()
+
+
+def test_lse_of_a_token_that_is_nearly_impossible():
+    """lse does not depend on the target, whose own logit may lie far below: logits of -1 to 1, exact in fp32, and one of -L.
+    exp and the sums are off by some 2^-22 each, and so is the result by its rounding: 2^-21 of 1 + |lse|."""
+    V, D = 3001, 8
+    for L in (10.0, 1000.0, 1e5, 1e30, math.inf):
+        weight = torch.zeros(V, D, dtype=torch.bfloat16)
+        weight[:, 0] = torch.linspace(-1.0, 1.0, V).bfloat16()
+        weight[77, 0] = -L
+        hidden = torch.zeros(1, D, dtype=torch.bfloat16)
+        hidden[0, 0] = 1.0
+        t = torch.tensor([77], dtype=torch.int32, device=DEV)
+        loss, lse = sip.sip_xent_forward(hidden.to(DEV), weight.to(DEV), t)
+        z = weight[:, 0].double()
+        want = torch.logsumexp(z, 0)
+        assert abs(float(lse) - float(want)) <= 2.0 ** -21 * (1.0 + abs(float(want))), (L, float(lse), float(want))
+        gap = float(want - z[77])
+        assert float(loss) == gap or abs(float(loss) - gap) <= 2.0 ** -21 * (1.0 + gap)
