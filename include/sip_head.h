@@ -88,7 +88,7 @@ sip_status sip_xent_backward(const void* hidden, int32_t N, int32_t D, int64_t h
  * or another tensor of the same type; two entries must not overlap otherwise.  Squares are formed and
  * summed in fp64, in an order that depends only on the sizes.  A norm that is NaN makes every output
  * NaN, an infinite one makes them 0 (NaN where g is infinite); max_norm = +inf leaves the gradients as
- * they are and only measures.
+ * they are and only measures, and so does norm + eps = 0.
  *
  *  tensors    host array of n_tensors entries; n_tensors = 0 or entries of 0 elements are allowed.
  *  norm       device fp32, one value.

@@ -96,7 +96,8 @@ __global__ __launch_bounds__(kClipThreads) void clip_scale_kernel(ClipTable t, c
   if ((threadIdx.x & 63) == 0) wave_sum[threadIdx.x >> 6] = s;
   __syncthreads();
   const float x = (float)sqrt((wave_sum[0] + wave_sum[1]) + (wave_sum[2] + wave_sum[3])), bound = max_norm / (x + eps);
-  const float f = bound > 1.0f || max_norm == INFINITY ? 1.0f : bound;         // (a NaN stays, unless nothing bounds the norm)
+  // (a NaN stays, unless nothing bounds the norm or there is nothing but zeros)
+  const float f = bound > 1.0f || max_norm == INFINITY || x + eps == 0.0f ? 1.0f : bound;
   if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = x;
   clip_chunks(t, true, [&](int j, long long first, int n) {
     const bool bf16 = (t.count[j] & kClipBf16) != 0;
