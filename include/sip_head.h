@@ -135,7 +135,9 @@ sip_status sip_head_quantize(const void* weight, int32_t V, int32_t D, int64_t w
  *  logits   [B, logits_stride] fp32 or bf16, aligned to its element; only the first V entries of a row are written.
  *           logits_stride a multiple of 16 bytes makes rows that sip_sample() takes.
  *  workspace  256-byte aligned, at least sip_head_workspace_bytes(B, V, D, group) bytes.
- * Products are exact, sums fp32, scales are applied to the fp32 sum of a group; rounded once.
+ * Products are exact, sums fp32, scales are applied to the fp32 sum of a group; rounded once.  A code enters as 16 + q, and what
+ * that adds is taken off again, by group up to 32 rows (an fp32 state counts as three), by 256 entries beyond: states whose mean
+ * is far from zero lose about three bits more there.
  */
 size_t sip_head_workspace_bytes(int32_t B, int32_t V, int32_t D, int32_t group);
 sip_status sip_head_logits(const void* hidden, int32_t B, int32_t D, int64_t hidden_stride, sip_dtype hidden_dtype,

@@ -446,16 +446,35 @@ __global__ __launch_bounds__(kFewWaves * 64) void head_few_kernel(CodesArgs p) {
 // Rows of a block of MT * 16: as many whole states as fit it.
 __host__ __device__ inline int block_states(int mt, bool hidden_bf16) { return mt * 16 / rows_of_state(hidden_bf16); }
 __host__ __device__ inline int many_units(int D) { return (D + 255) / 256 * 2; }             // of 128 entries
-__host__ __device__ inline int many_groups(int D, int group) { return (D / group + 31) / 32 * 32; }
+__host__ __device__ inline int many_groups(int D, int group) { return many_units(D) * 128 / group; }   // zeros behind the last ones
 
-// The states in the order of the products, by block: [unit][product of the unit][tile of rows][lane], 16 bytes a lane; and behind
-// them the sums of the states by group, in three bf16 parts, as rows of a product over groups: [32 groups][part][tile][lane].
+// The states in the order of the products, by block: [pair of units][product][tile of rows][lane], 16 bytes a lane: eight products of
+// the states, and behind them zero_products() of the states' sums by group, as SumParts says.
+__host__ __device__ constexpr int zero_products(int group) { return group == 32 ? 2 : 1; }
 struct ManyLayout {
-  size_t sums, block;                                     // bytes of a block's states, and of all of it
+  size_t pair, block;                                     // bytes
   __host__ __device__ ManyLayout(int D, int group, int mt) {
-    sums = (size_t)many_units(D) * 4 * mt * 1024;
-    block = sums + (size_t)many_groups(D, group) / 32 * 3 * mt * 1024;
+    pair = (size_t)(8 + zero_products(group)) * mt * 1024;
+    block = many_units(D) / 2 * pair;
   }
+};
+
+// Products x y of fp32 values, four groups a matrix product, from bf16 parts that are a value's next 8 bits each.  Of a group
+// quarter j of the wave has a pair of terms, dword i that of group i: x0 y0; x0 y1 and x1 y0; x0 y2 and x2 y0; x1 y1 and x1 y2.
+// (The instruction aligns the eight terms of a quarter with their largest and cuts off what is below 24 bits, but rounds the
+// quarters' sums: terms of all sizes in one quarter lost 2^-23 of the product, always to the same side.)
+struct SumParts {
+  uint32_t part[3];                                        // bf16 in the upper half
+  __device__ explicit SumParts(float x) {
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+      part[i] = __builtin_bit_cast(uint32_t, x) & 0xffff0000u;
+      x -= __builtin_bit_cast(float, part[i]);
+    }
+  }
+  __device__ uint32_t two(int low, int high) const { return (part[low] >> 16) | part[high]; }
+  __device__ u32x4 x() const { return u32x4{part[0] >> 16, two(0, 1), two(0, 2), two(1, 1)}; }     // by quarter
+  __device__ u32x4 y() const { return u32x4{part[0] >> 16, two(1, 0), two(2, 0), two(1, 2)}; }
 };
 
 // A wave takes a tile of 16 rows and a group.
@@ -467,43 +486,43 @@ __global__ __launch_bounds__(256) void head_rows_kernel(CodesArgs p, int mt) {
   const int r = tile * 16 + (lane & 15), state = block * states + r / each;
   const bool live = r < states * each && state < p.B;
   const ManyLayout layout(p.D, GROUP, mt);
-  char* out = p.states + block * layout.block;
+  constexpr int kGroups = 256 / GROUP;                     // of a pair
+  char* out = p.states + block * layout.block + g / kGroups * layout.pair + tile * 1024;
   float sum = 0.0f;
   for (int c = g * (GROUP / 32); c < (g + 1) * (GROUP / 32); ++c) {
     const int k = c * 32 + quad * 8;
     const bf16x8 x = hidden_row(p, live ? state * each + r % each : 0, k, live && k < p.D);
-    if (c < many_units(p.D) * 4) *reinterpret_cast<bf16x8*>(out + ((size_t)c * mt + tile) * 1024 + lane * 16) = x;
+    *reinterpret_cast<bf16x8*>(out + c % 8 * mt * 1024 + lane * 16) = x;
 #pragma unroll
     for (int e = 0; e < 8; ++e) sum += (float)x[e];
   }
   sum += __shfl_xor(sum, 16);
   sum += __shfl_xor(sum, 32);
-  if (quad == 0) {
-    uint16_t* to = reinterpret_cast<uint16_t*>(out + layout.sums + ((size_t)(g >> 5) * 3 * mt + tile) * 1024 + (((g & 31) >> 3) * 16 + lane) * 16) + (g & 7);
-#pragma unroll
-    for (int part = 0; part < 3; ++part) {
-      const uint32_t top = __builtin_bit_cast(uint32_t, sum) & 0xffff0000u;
-      to[part * mt * 512] = (uint16_t)(top >> 16);
-      sum -= __builtin_bit_cast(float, top);
-    }
-  }
+  // (of 128 there are two groups, and two of zeros)
+  uint32_t* to = reinterpret_cast<uint32_t*>(out + (8 + g % kGroups / 4) * mt * 1024 + lane * 16) + g % kGroups % 4;
+  const u32x4 terms = SumParts(sum).x();
+  to[0] = quad == 0 ? terms[0] : quad == 1 ? terms[1] : quad == 2 ? terms[2] : terms[3];
+  if (GROUP == 128) to[2] = 0;
 }
 
 // WAVES * NT * 16 vocabulary entries by MT * 16 rows: 256 entries, or 64 where tiles of 256 would leave compute units without
-// one (31 fp32 states, V = 5164, D = 5568: 62 us instead of 116).  A wave has NT * 16 of the entries and all rows, so that a
+// one (31 fp32 states, V = 5164, D = 5568: 60 us instead of 116).  A wave has NT * 16 of the entries and all rows, so that a
 // code becomes a bf16 value once.  It goes through a pair of units -- 256 entries of a state, a line of each row's codes -- at a
 // time: states through LDS, codes and scales straight into registers, all of the next pair's loaded while this one's products
 // are made.
 //   sum_g s (sum_d (16 + q) x - (16 + zero) sum_d x)
-// The second part is a product over groups of its own, in 3 x 3 bf16 parts of which the six that matter are taken: with
-// 8 row tiles it saves 32 multiplications a group and tile of entries.
-// 256 rows, V = 152064, D = 4096, fp32 logits, groups of 128, 64, 32: 381, 447, 605 us, 837, 714, 527 TFLOP/s.  In groups of 64
+// The second part of a pair is a product over its groups, in bf16 parts (SumParts), ahead of the first: with 8 row tiles it saves 32
+// multiplications a group and tile of entries.  What cancels between the two, the more the further the states' mean is from
+// zero, cancels within 256 entries.  States of mean 1, D = 4096, groups of 128 and 32: off by 4.3e-7 and 1.0e-6 of the result; with a
+// row's second part added as a whole 2.2e-6 and 9.8e-6, for 3 to 10 % less time.
+// 256 rows, V = 152064, D = 4096, fp32 logits, groups of 128, 64, 32: 393, 450, 647 us, 811, 709, 493 TFLOP/s.  In groups of 64
 // matrix cores are busy for 30 % of it and vector units for 40 (half of that the scales' multiplications), which two waves of a
 // SIMD do not hide behind each other altogether; reads further ahead or four waves of half the entries changed nothing.
 template <int GROUP, bool SCALES_BF16, int MT, int WAVES, int NT>
 __global__ __launch_bounds__(WAVES * 64) void head_many_kernel(CodesArgs p) {
-  constexpr int kEntries = WAVES * NT * 16, kGroups = 256 / GROUP, kPairBytes = 8 * MT * 1024, kLoads = kPairBytes / (WAVES * 1024);
-  constexpr int kPitch = kEntries + 4, kScaleBytes = SCALES_BF16 ? 2 : 4;
+  constexpr int kEntries = WAVES * NT * 16, kGroups = 256 / GROUP, kZero = zero_products(GROUP);
+  constexpr int kPieces = (8 + kZero) * MT, kPairBytes = kPieces * 1024, kLoads = (kPieces + WAVES - 1) / WAVES;
+  constexpr int kPitch = kEntries + 4;
   constexpr int kRing = 2 * kPairBytes, kOut = MT * 16 * kPitch * 4;
   __shared__ __attribute__((aligned(1024))) char lds_bytes[kRing > kOut ? kRing : kOut];
   SIP_LDS char* lds = (SIP_LDS char*)lds_bytes;
@@ -521,6 +540,7 @@ __global__ __launch_bounds__(WAVES * 64) void head_many_kernel(CodesArgs p) {
     const u32x4 buffer = {(uint32_t)at, (uint32_t)(at >> 32) & 0xffff, kPairBytes, 0x00020000};
 #pragma unroll
     for (int l = 0; l < kLoads; ++l) {
+      if (kPieces % WAVES != 0 && l * WAVES + wave >= kPieces) break;
       const uint32_t piece = (l * WAVES + wave) * 1024;
       asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
                    :: "s"(lds0 + (uint32_t)(pair & 1) * kPairBytes + piece), "v"(piece + lane * 16), "s"(buffer) : "memory");
@@ -540,11 +560,6 @@ __global__ __launch_bounds__(WAVES * 64) void head_many_kernel(CodesArgs p) {
         next_codes[t][e] = *(const SIP_GLOBAL u32x4*)((const SIP_GLOBAL uint8_t*)p.codes + (uint64_t)row[t] * stride +
                                                       min(pair * 128 + quad * 32 + e * 16, p.D / 2 - 16));
   };
-  auto scale_at = [&](int t, int g) -> float {
-    const uint32_t at = row[t] * groups + min(g, groups - 1);
-    if constexpr (SCALES_BF16) return __builtin_bit_cast(float, (uint32_t)((const SIP_GLOBAL uint16_t*)p.scales)[at] << 16);
-    else return ((const SIP_GLOBAL float*)p.scales)[at];
-  };
   float scales[NT][kGroups];
   uint32_t next_scales[NT][kGroups];                       // as they are loaded: to shift them there would wait for them
   auto load_scales = [&](int pair) {
@@ -557,64 +572,27 @@ __global__ __launch_bounds__(WAVES * 64) void head_many_kernel(CodesArgs p) {
         else next_scales[t][g] = ((const SIP_GLOBAL uint32_t*)p.scales)[at];
       }
   };
+  uint32_t next_zeros[NT][kZero];                          // of group 4 c + my quarter
+  const uint32_t zeros_mask = p.zeros ? ~0u : 0u;
+  auto load_zeros = [&](int pair) {
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int c = 0; c < kZero; ++c)
+        next_zeros[t][c] = zeros[(row[t] * groups + min(pair * kGroups + c * 4 + quad % kGroups, groups - 1)) & zeros_mask];
+  };
   load_states(0);
   load_scales(0);
+  load_zeros(0);
   load_codes(0);
 
   f32x4 total[NT][MT] = {};
-  for (int g0 = 0; g0 < groups; g0 += 32) {
-    bf16x8 w[NT][3];
-#pragma unroll
-    for (int t = 0; t < NT; ++t) {
-      float scale[8], zero[8];
-      if (groups % 8 == 0) {                               // eight at once
-        const uint32_t at = row[t] * groups + min(g0 + quad * 8, groups - 8);
-        GroupScales<8, SCALES_BF16> eight;
-        eight.s.load((const SIP_GLOBAL uint8_t*)p.scales + (uint64_t)at * kScaleBytes, ((uint64_t)p.scales & 3) != 0);
-        eight.z.load(zeros + (p.zeros ? at : 0), ((uint64_t)zeros & 3) != 0);
-        eight.settle();
-#pragma unroll
-        for (int e = 0; e < 8; ++e) { scale[e] = eight.scale(e); zero[e] = eight.zero(e); }
-      } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const int g = g0 + quad * 8 + e;
-          scale[e] = scale_at(t, g);
-          zero[e] = (float)zeros[p.zeros ? row[t] * groups + min(g, groups - 1) : 0];
-        }
-      }
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        float f = scale[e] * (-16.0f - zero[e]);
-#pragma unroll
-        for (int part = 0; part < 3; ++part) {
-          const uint32_t top = __builtin_bit_cast(uint32_t, f) & 0xffff0000u;
-          w[t][part][e] = __builtin_bit_cast(__bf16, (uint16_t)(top >> 16));
-          f -= __builtin_bit_cast(float, top);
-        }
-      }
-    }
-#pragma unroll
-    for (int m = 0; m < MT; ++m) {
-      bf16x8 x[3];
-#pragma unroll
-      for (int part = 0; part < 3; ++part)
-        x[part] = *reinterpret_cast<const bf16x8*>(from + layout.sums + ((size_t)(g0 / 32 * 3 + part) * MT + m) * 1024 + lane * 16);
-#pragma unroll
-      for (int t = 0; t < NT; ++t)
-#pragma unroll
-        for (int sum = 2; sum >= 0; --sum)
-#pragma unroll
-          for (int part = 0; part <= sum; ++part)
-            total[t][m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[part], w[t][sum - part], total[t][m], 0, 0, 0);
-    }
-  }
-  // A step: the products of a tile of rows and a group, and with them the multiplications of the step before and the reads of
-  // the one behind.
+  // A step: the products of a tile of rows and a group -- with the tile's first group the zero points' --, and with them the
+  // multiplications of the step before and the reads of the one behind.
   constexpr int kEach = GROUP / 32, kSteps = MT * kGroups;
   const CodeValues code_values;
   for (int pair = 0; pair < pairs; ++pair) {
-    bf16x8 w[NT][8];                                       // product c of the pair: dword c / 2 of load c % 2
+    bf16x8 w[NT][8], w_zero[NT][kZero];                    // product c of the pair: dword c / 2 of load c % 2
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
 #pragma unroll
@@ -625,16 +603,28 @@ __global__ __launch_bounds__(WAVES * 64) void head_many_kernel(CodesArgs p) {
       }
 #pragma unroll
       for (int g = 0; g < kGroups; ++g) scales[t][g] = __builtin_bit_cast(float, SCALES_BF16 ? next_scales[t][g] << 16 : next_scales[t][g]);
+#pragma unroll
+      for (int c = 0; c < kZero; ++c) {
+        float s = scales[t][c * 4];
+#pragma unroll
+        for (int q = 1; q < 4 && q < kGroups; ++q) s = quad == q ? scales[t][c * 4 + q] : s;
+        if (quad >= kGroups) s = 0.0f;
+        w_zero[t][c] = __builtin_bit_cast(bf16x8, UnitOrder<32, 1>::order(0, SumParts(s * (-16.0f - (float)next_zeros[t][c])).y()));
+      }
     }
     // this pair's states have arrived, and everybody has read the last one's
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
     const uint32_t states_at = lds0 + (uint32_t)(pair & 1) * kPairBytes + lane * 16;
-    bf16x8 x[2][kEach];
+    bf16x8 x[2][kEach], sums[2][kZero];
     f32x4 acc[2][NT];
     auto read = [&](int step) {
 #pragma unroll
       for (int j = 0; j < kEach; ++j)
         x[step & 1][j] = *(const SIP_LDS bf16x8*)(uintptr_t)(states_at + ((step % kGroups * kEach + j) * MT + step / kGroups) * 1024);
+      if (step % kGroups == 0)
+#pragma unroll
+        for (int c = 0; c < kZero; ++c)
+          sums[step / kGroups & 1][c] = *(const SIP_LDS bf16x8*)(uintptr_t)(states_at + ((8 + c) * MT + step / kGroups) * 1024);
     };
     auto scale = [&](int step) {
 #pragma unroll
@@ -647,12 +637,20 @@ __global__ __launch_bounds__(WAVES * 64) void head_many_kernel(CodesArgs p) {
     if (pair + 1 < pairs) {
       load_states(pair + 1);
       load_scales(pair + 1);
+      load_zeros(pair + 1);
       load_codes(pair + 1);
     }
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int step = 0; step < kSteps; ++step) {
+      const bool first = step % kGroups == 0, reads_sums = step + 1 < kSteps && (step + 1) % kGroups == 0;
       if (step + 1 < kSteps) read(step + 1);
+      if (first)
+#pragma unroll
+        for (int c = 0; c < kZero; ++c)
+#pragma unroll
+          for (int t = 0; t < NT; ++t)
+            total[t][step / kGroups] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(sums[step / kGroups & 1][c], w_zero[t][c], total[t][step / kGroups], 0, 0, 0);
 #pragma unroll
       for (int j = 0; j < kEach; ++j)
 #pragma unroll
@@ -660,6 +658,8 @@ __global__ __launch_bounds__(WAVES * 64) void head_many_kernel(CodesArgs p) {
           acc[step & 1][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[step & 1][j], w[t][step % kGroups * kEach + j], j == 0 ? f32x4{} : acc[step & 1][t], 0, 0, 0);
       if (step > 0) scale(step - 1);
       __builtin_amdgcn_sched_group_barrier(0x100, kEach, 0);
+      if (reads_sums) __builtin_amdgcn_sched_group_barrier(0x100, kZero, 0);
+      if (first) __builtin_amdgcn_sched_group_barrier(0x008, kZero * NT, 0);
 #pragma unroll
       for (int n = 0; n < kEach * NT; ++n) {               // in turn: a product, and multiplications while it runs
         __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
