@@ -66,9 +66,9 @@ sip_status sip_xent_forward(const void* hidden, int32_t N, int32_t D, int64_t hi
  *  grad_loss    [N] fp32, NULL = all ones.
  *  grad_hidden  [N, grad_hidden_stride] bf16, NULL = not wanted; rows of masked tokens are zero.
  *  grad_weight  [V, grad_weight_stride] bf16, NULL = not wanted.  Both are overwritten.
- * The logits are made again, a piece of the vocabulary at a time; dz of a piece is held as bf16, in
- * calls of up to 64 tokens as the sum of two bf16 (without scale * logit_scale, which the fp32 sums
- * are multiplied with), sums over the vocabulary and over the tokens are fp32 across pieces, and the
+ * The logits are made again, a piece of the vocabulary at a time; dz of a piece is held as bf16, where
+ * no more than 64 tokens take part as the sum of two bf16 (without scale * logit_scale, which the fp32
+ * sums are multiplied with), sums over the vocabulary and over the tokens are fp32 across pieces, and the
  * gradients are rounded once.
  */
 sip_status sip_xent_backward(const void* hidden, int32_t N, int32_t D, int64_t hidden_stride, const void* weight,

@@ -57,19 +57,14 @@ Cheapest cheapest(std::initializer_list<XentShape> among, long long a, long long
 }
 XentShape score_shape(int a, int tokens, int D) { return cheapest({kWide, kQuarter, kNarrow, kSmall, kTiny}, a, tokens, D).shape; }
 
-// Up to here a token's dz is held in two bf16 parts, as two rows: dz's rounding is an error of its own in every gradient, and
-// where few tokens make it up it may all go one way.  These calls are bound by reading the head and writing its gradient:
-// V = 128256, D = 4096 take 850 us instead of 762 for 64 tokens, 735 instead of 717 for one.
-constexpr int kTwoPartRows = 64;
-
 // How a cross entropy of this shape is cut, and where its parts lie in the workspace.
 struct XentPlan {
   XentShape score;              // tiles of the logits
   int parts;                    // waves' partial sums of a token
   int piece;                    // vocabulary entries whose dz is held at once
   XentShape score_piece, hidden, weight;
-  int rows_each;                // rows of dz that a token has
-  sip::Parts hidden_parts, weight_parts;   // for all N rows (without their room)
+  sip::Parts hidden_parts, weight_parts;   // for all N tokens (without their room)
+  int hidden_kept, hidden_joined;          // tiles of grad_hidden whose sums are kept, and that are joined
   size_t count, rows, part, dense, dz, hidden_sum, weight_sum, bytes;
 };
 
@@ -90,20 +85,24 @@ XentPlan xent_plan(int32_t N, int32_t V, int32_t D, bool backward) {
     const int pieces = tiles(V, (int)std::min<long long>(most, 1 << 20));
     p.piece = tiles(tiles(V, pieces), 256) * 256;
     const int left = std::min(p.piece, V);
-    p.rows_each = N <= kTwoPartRows ? 2 : 1;
-    p.score_piece = p.rows_each == 2 ? cheapest({kQuarter, kNarrow, kSmall, kTiny}, left, N, D).shape : score_shape(left, N, D);
-    const long long dz_rows = (long long)N * p.rows_each;
+    p.score_piece = score_shape(left, N, D);
+    // rows of dz: two each if no more than kTwoPartRows of the tokens take part
+    const int two_part_rows = 2 * std::min<int>(N, sip::kTwoPartRows);
+    const long long dz_rows = std::max<int>(N, two_part_rows);
     const Cheapest h = cheapest({kWide, kNarrow, kSmall}, D, dz_rows, left, 128), w = cheapest({kWide, kSmall}, D, left, dz_rows, 128);
     p.hidden = h.shape;
     p.weight = w.shape;
     p.hidden_parts = {nullptr, tiles(D, kShapeA[h.shape]) * tiles(dz_rows, kShapeB[h.shape]), h.parts, 0};
     p.weight_parts = {nullptr, tiles(D, kShapeA[w.shape]) * tiles(left, kShapeB[w.shape]), w.parts, 0};
-    auto room = [](const sip::Parts& q, XentShape s) { return (size_t)q.count * q.tiles * kShapeA[s] * kShapeB[s] * 4; };
+    auto room = [](int count, int n_tiles, XentShape s) { return (size_t)count * n_tiles * kShapeA[s] * kShapeB[s] * 4; };
+    // (where one kernel makes all of grad_hidden, sums are kept of tokens in two parts alone)
+    p.hidden_kept = p.hidden_parts.count == 1 && p.piece >= V ? tiles(D, kShapeA[h.shape]) * tiles(two_part_rows, kShapeB[h.shape]) : p.hidden_parts.tiles;
+    p.hidden_joined = p.hidden_parts.count == 1 ? tiles(D, kShapeA[h.shape]) * tiles(two_part_rows / 2, kShapeB[h.shape]) : p.hidden_parts.tiles;
     at = both;
     p.dense = take((size_t)dz_rows * D * 2);
     p.dz = take((size_t)dz_rows * p.piece * 2);
-    p.hidden_sum = take(p.hidden_parts.count == 1 && p.piece >= V && p.rows_each == 1 ? 0 : room(p.hidden_parts, p.hidden));
-    p.weight_sum = take(p.weight_parts.count == 1 ? 0 : room(p.weight_parts, p.weight));
+    p.hidden_sum = take(room(p.hidden_parts.count, p.hidden_kept, p.hidden));
+    p.weight_sum = take(p.weight_parts.count == 1 ? 0 : room(p.weight_parts.count, p.weight_parts.tiles, p.weight));
     p.bytes = std::max(p.bytes, at);
   }
   return p;
@@ -152,7 +151,6 @@ sip::XentArgs xent_args(const void* hidden, int32_t N, int32_t D, int64_t hidden
   a.dense = reinterpret_cast<uint16_t*>(ws + pl.dense);
   a.dz = reinterpret_cast<uint16_t*>(ws + pl.dz);
   a.piece = pl.piece;
-  a.rows_each = pl.rows_each;
   a.hidden_parts = pl.hidden_parts; a.hidden_parts.sum = reinterpret_cast<float*>(ws + pl.hidden_sum);
   a.weight_parts = pl.weight_parts; a.weight_parts.sum = reinterpret_cast<float*>(ws + pl.weight_sum);
   return a;
@@ -268,20 +266,17 @@ sip_status sip_xent_backward(const void* hidden, int32_t N, int32_t D, int64_t h
   for (int v0 = 0; v0 < V; v0 += pl.piece) {
     a.v0 = v0;
     const int left = std::min(pl.piece, V - v0);
-    auto make_dz = [&](auto shape, auto two_parts) {
+    with_shape<kWide, kQuarter, kNarrow, kSmall, kTiny>(pl.score_piece, [&](auto shape) {
       typedef decltype(shape) S;
-      hipLaunchKernelGGL((sip::xent_dz_kernel<S, decltype(two_parts)::value>), dim3(tile_grid((long long)tiles(left, S::kA) * tiles(N, S::kB))),
-                         dim3(S::kThreads), 0, stream, a);
-    };
-    if (pl.rows_each == 2) with_shape<kQuarter, kNarrow, kSmall, kTiny>(pl.score_piece, [&](auto shape) { make_dz(shape, std::true_type()); });
-    else with_shape<kWide, kQuarter, kNarrow, kSmall, kTiny>(pl.score_piece, [&](auto shape) { make_dz(shape, std::false_type()); });
+      hipLaunchKernelGGL(sip::xent_dz_kernel<S>, dim3(tile_grid((long long)tiles(left, S::kA) * tiles(N, S::kB))), dim3(S::kThreads), 0, stream, a);
+    });
     if (grad_hidden)
       with_shape<kWide, kNarrow, kSmall>(pl.hidden, [&](auto shape) {
         typedef decltype(shape) S;
         hipLaunchKernelGGL(sip::xent_grad_hidden_kernel<S>, dim3(tile_grid(pl.hidden_parts.tiles), pl.hidden_parts.count), dim3(S::kThreads), 0,
                            stream, a);
-        if ((pl.hidden_parts.count > 1 || pl.rows_each > 1) && v0 + pl.piece >= V)
-          hipLaunchKernelGGL((sip::xent_join_kernel<S, true>), dim3(pl.hidden_parts.tiles, S::kTA * S::kTB), dim3(S::kThreads), 0, stream, a);
+        if (v0 + pl.piece >= V)
+          hipLaunchKernelGGL((sip::xent_join_kernel<S, true>), dim3(pl.hidden_joined, S::kTA * S::kTB), dim3(S::kThreads), 0, stream, a);
       });
     if (grad_weight)
       with_shape<kWide, kSmall>(pl.weight, [&](auto shape) {

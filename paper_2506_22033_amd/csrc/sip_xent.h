@@ -39,12 +39,18 @@ struct XentArgs {
   int* rows;                              // [N] their indices, ascending
   float2* part;                           // [N][parts] maximum and sum of a wave's logits without the target
   int parts;
-  uint16_t* dense;                        // the rows that take part, one after the other, [rows_each][count][D]
-  uint16_t* dz; int piece;                // gradient of a piece's logits, [rows_each][count][piece]
-  int rows_each;                          // 2: dz in two parts, what bf16 holds of it and what that leaves
+  uint16_t* dense;                        // the rows that take part, one after the other, [dz_parts()][count][D]
+  uint16_t* dz; int piece;                // gradient of a piece's logits, [dz_parts()][count][piece]
   Parts hidden_parts, weight_parts;
   int v0;                                 // the piece's first vocabulary entry
 };
+
+// Up to here a token's dz is held in two bf16 parts, as two rows: what bf16 holds of it, and what that leaves.  Its rounding is an error
+// of its own in every gradient, and where few tokens make one up it may all go one way.  What counts is the tokens that take
+// part.  These calls are bound by reading the head and writing its gradient: V = 128256, D = 4096 take 850 us instead of 762
+// for 64 tokens, 735 instead of 717 for one; 41 tokens among 2048, D = 2048, 514 instead of 470.
+constexpr int kTwoPartRows = 64;
+__host__ __device__ inline int dz_parts(int count) { return count <= kTwoPartRows ? 2 : 1; }
 
 // One workgroup lists the rows, eight targets a thread a turn.  What is read is N integers once: latency.
 __global__ __launch_bounds__(1024) void xent_rows_kernel(XentArgs p) {
@@ -84,11 +90,11 @@ __global__ __launch_bounds__(1024) void xent_rows_kernel(XentArgs p) {
 
 // Row `blockIdx.x` of the list to its place in `dense`; row `blockIdx.x` of grad_hidden to zero if it is masked.
 __global__ __launch_bounds__(256) void xent_gather_kernel(XentArgs p) {
-  const int i = blockIdx.x;
-  if (i < *p.count) {
+  const int i = blockIdx.x, n = *p.count;
+  if (i < n) {
     const uint4* src = reinterpret_cast<const uint4*>(p.hidden + p.rows[i] * p.hidden_stride);
-    for (int part = 0; part < p.rows_each; ++part) {
-      uint4* dst = reinterpret_cast<uint4*>(p.dense + (i + (long long)part * *p.count) * p.D);
+    for (int part = 0; part < dz_parts(n); ++part) {
+      uint4* dst = reinterpret_cast<uint4*>(p.dense + (i + (long long)part * n) * p.D);
       for (int c = threadIdx.x; c < p.D / 8; c += 256) dst[c] = src[c];
     }
   }
@@ -126,22 +132,35 @@ template <class S> __device__ inline int wave_b() { return (int)(threadIdx.x >> 
 // The tile's values value(i, j) -- the lane's four of block (i, j) -- as bf16, row by row through LDS, to where row(b) says
 // (nullptr: nowhere), columns [a0, a_end).  A lane holds four neighbours of one row: eight bytes, whose 16-byte group goes
 // to place group ^ row, so that 16 rows meet every bank once; rows leave in 16-byte groups.
+// `two`: of the first kTwo rows alone, and as rows kTwo + b what bf16 leaves of row b.
+template <class S> constexpr int kTwo = S::kB < kTwoPartRows ? S::kB : kTwoPartRows;
 template <class S, class Value, class Row>
-__device__ inline void store_tile(SIP_LDS char* lds, int a0, int a_end, Value value, Row row) {
+__device__ inline void store_tile(SIP_LDS char* lds, int a0, int a_end, Value value, Row row, bool two = false) {
   constexpr int kPitch = S::kA * 2, kGroups = S::kA / 8, kMask = kGroups < 16 ? kGroups - 1 : 15;
+  static_assert(2 * kTwo<S> * kPitch <= S::kLds && S::kB * kPitch <= S::kLds, "room for the rows");
   const int lane = threadIdx.x & 63;
 #pragma unroll
   for (int j = 0; j < S::kTB; ++j) {
     const int b = wave_b<S>() + 16 * j + (lane & 15);
+    if (two && b >= kTwo<S>) break;
 #pragma unroll
     for (int i = 0; i < S::kTA; ++i) {
       const int a = wave_a<S>() + 16 * i + acc_a(lane);
-      *reinterpret_cast<SIP_LDS u32x2*>(lds + b * kPitch + (((a >> 3) ^ (b & kMask)) << 4) + ((a & 4) << 1)) = bf16_pack(value(i, j));
+      f32x4 x = value(i, j);
+      auto put = [&](int r) {
+        *reinterpret_cast<SIP_LDS u32x2*>(lds + r * kPitch + (((a >> 3) ^ (r & kMask)) << 4) + ((a & 4) << 1)) = bf16_pack(x);
+      };
+      put(b);
+      if (two) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] -= (float)(__bf16)x[e];
+        put(kTwo<S> + b);
+      }
     }
   }
   __syncthreads();
 #pragma unroll 4
-  for (int g = threadIdx.x; g < S::kB * kGroups; g += S::kThreads) {
+  for (int g = threadIdx.x; g < (two ? 2 * kTwo<S> : S::kB) * kGroups; g += S::kThreads) {
     const int b = g / kGroups, c = g % kGroups;
     uint16_t* to = row(b);
     if (to && a0 + c * 8 < a_end)
@@ -267,7 +286,7 @@ __global__ __launch_bounds__(256) void xent_loss_kernel(XentArgs p) {
 
 // dz of a tile of the piece's logits: the product of xent_forward_kernel once more, which takes a third of the backward pass (8192
 // tokens, V = 128256, D = 4096: 19.5 ms together, 1.32 PFLOP/s); logits kept from the forward pass would be 4.2 GB.  Columns past the vocabulary are zeros: what multiplies dz reads groups of eight.
-template <class S, bool TWO_PARTS>
+template <class S>
 __global__ __launch_bounds__(S::kThreads) void xent_dz_kernel(XentArgs p) {
   __shared__ __attribute__((aligned(1024))) char lds[S::kLds];
   const int n = *p.count, left = min(p.piece, p.V - p.v0);
@@ -301,17 +320,11 @@ __global__ __launch_bounds__(S::kThreads) void xent_dz_kernel(XentArgs p) {
         }
     }
   }
-  store_tile<S>((SIP_LDS char*)lds, a0, p.piece, [&](int i, int j) { return acc[i][j]; },
-                [&](int b) { return b0 + b < n ? p.dz + (long long)(b0 + b) * p.piece : nullptr; });
-  if constexpr (TWO_PARTS) {
-    __syncthreads();
-    store_tile<S>((SIP_LDS char*)lds, a0, p.piece, [&](int i, int j) {
-      f32x4 left;
-#pragma unroll
-      for (int r = 0; r < 4; ++r) left[r] = acc[i][j][r] - (float)(__bf16)acc[i][j][r];
-      return left;
-    }, [&](int b) { return b0 + b < n ? p.dz + (long long)(n + b0 + b) * p.piece : nullptr; });
-  }
+  const bool two = dz_parts(n) == 2;
+  store_tile<S>((SIP_LDS char*)lds, a0, p.piece, [&](int i, int j) { return acc[i][j]; }, [&](int r) {
+    const int part = two && r >= kTwo<S>, i = b0 + r - part * kTwo<S>;
+    return i < n ? p.dz + (long long)(part * n + i) * p.piece : nullptr;
+  }, two);
 }
 
 // How a launch for up to parts.tiles tiles of parts.count parts deals out `tiles` (1 .. parts.tiles) of `k` terms each: the
@@ -343,7 +356,7 @@ __device__ inline void store_grad_hidden(const XentArgs& p, SIP_LDS char* lds, c
 template <class S>
 __global__ __launch_bounds__(S::kThreads) void xent_grad_hidden_kernel(XentArgs p) {
   __shared__ __attribute__((aligned(1024))) char lds[S::kLds];
-  const int n = *p.count * p.rows_each, tiles_a = div_up(p.D, S::kA), tiles = tiles_a * div_up(n, S::kB);
+  const int each = dz_parts(*p.count), n = *p.count * each, tiles_a = div_up(p.D, S::kA), tiles = tiles_a * div_up(n, S::kB);
   if (tiles == 0) return;
   const Parts parts = dealt(p.hidden_parts, tiles, min(p.piece, p.V));
   int ta, tb, part;
@@ -354,7 +367,7 @@ __global__ __launch_bounds__(S::kThreads) void xent_grad_hidden_kernel(XentArgs 
   Gemm<S, kCols, kRows>::tile(acc, Operand{p.weight + p.v0 * p.weight_stride, p.weight_stride, p.D, nullptr},
                              Operand{p.dz, p.piece, n, nullptr}, a0, b0, k_begin, k_end, (SIP_LDS char*)lds);
   f32x4* sum = sum_tile<S>(parts, part, tb * tiles_a + ta);
-  const bool last = gridDim.y == 1 && p.rows_each == 1 && p.v0 + p.piece >= p.V;
+  const bool last = gridDim.y == 1 && each == 1 && p.v0 + p.piece >= p.V;
 #pragma unroll
   for (int i = 0; i < S::kTA; ++i)
 #pragma unroll
@@ -366,16 +379,18 @@ __global__ __launch_bounds__(S::kThreads) void xent_grad_hidden_kernel(XentArgs 
 }
 
 // The parts of grad_hidden (or of grad_weight's rows of a piece), added up in their order: workgroup (x, y) joins block y of each
-// wave's in tile x.
+// wave's in tile x.  (grad_hidden: unless xent_grad_hidden_kernel stored the result, which only the device knows.)
 template <class S, bool HIDDEN>
 __global__ __launch_bounds__(S::kThreads) void xent_join_kernel(XentArgs p) {
   const int tiles_a = div_up(p.D, S::kA), ta = blockIdx.x % tiles_a, tb = blockIdx.x / tiles_a, lane = threadIdx.x & 63;
   const int i = blockIdx.y / S::kTB, j = blockIdx.y % S::kTB;
   const int a = ta * S::kA + wave_a<S>() + 16 * i + acc_a(lane), b = tb * S::kB + wave_b<S>() + 16 * j + (lane & 15);
   if (a >= p.D || b >= (HIDDEN ? *p.count : min(p.piece, p.V - p.v0))) return;
-  const Parts parts = HIDDEN ? dealt(p.hidden_parts, tiles_a * div_up(*p.count * p.rows_each, S::kB), min(p.piece, p.V)) : p.weight_parts;
+  const int each = HIDDEN ? dz_parts(*p.count) : 1;
+  if (HIDDEN && each == 1 && p.hidden_parts.count == 1) return;
+  const Parts parts = HIDDEN ? dealt(p.hidden_parts, tiles_a * div_up(*p.count * each, S::kB), min(p.piece, p.V)) : p.weight_parts;
   f32x4 total = {};
-  for (int row = HIDDEN ? p.rows_each - 1 : 0; row >= 0; --row) {
+  for (int row = each - 1; row >= 0; --row) {
     // where row b + row * count lies: its tile, its wave and block, its lane
     const int at = HIDDEN ? b + row * *p.count : b, in = at % S::kB;
     const int wave = in / S::kWaveB * (S::kA / S::kWaveA) + wave_a<S>() / S::kWaveA, block = i * S::kTB + in % S::kWaveB / 16;
@@ -390,7 +405,7 @@ __global__ __launch_bounds__(S::kThreads) void xent_join_kernel(XentArgs p) {
 template <class S>
 __global__ __launch_bounds__(S::kThreads) void xent_grad_weight_kernel(XentArgs p) {
   __shared__ __attribute__((aligned(1024))) char lds[S::kLds];
-  const int n = *p.count * p.rows_each, left = min(p.piece, p.V - p.v0), tiles_a = div_up(p.D, S::kA);
+  const int n = *p.count * dz_parts(*p.count), left = min(p.piece, p.V - p.v0), tiles_a = div_up(p.D, S::kA);
   int ta, tb, part;
   if (!tile_of(blockIdx.y * gridDim.x + blockIdx.x, tiles_a, div_up(left, S::kB), p.weight_parts.count, ta, tb, part)) return;
   const int a0 = ta * S::kA, b0 = tb * S::kB;

@@ -44,3 +44,27 @@ def test_lse_of_a_token_that_is_nearly_impossible():
         assert abs(float(lse) - float(want)) <= 2.0 ** -21 * (1.0 + abs(float(want))), (L, float(lse), float(want))
         gap = float(want - z[77])
         assert float(loss) == gap or abs(float(loss) - gap) <= 2.0 ** -21 * (1.0 + gap)
+
+
+@pytest.mark.parametrize("N,live,V,D", [(65, 1, 3001, 136), (100, 2, 20000, 256), (100, 64, 3001, 136), (128, 40, 4097, 520), (2000, 3, 20000, 256),
+                                        (5000, 64, 3000, 64), (3000, 17, 70000, 1032), (65536, 9, 5000, 16)])
+def test_few_tokens_among_masked_ones(N, live, V, D):
+    """What counts for dz's two parts is the tokens that take part: the bound is that of a call of nothing else (2^-8 of 2^-8 of a
+    term lost in dz; the result's rounding, 2^-8; the probabilities' error; sums in fp32, a random walk)."""
+    hidden, weight, targets = make(N, V, D, seed=N + live)
+    g = torch.Generator().manual_seed(live)
+    off = torch.randperm(N, generator=g)[live:].to(DEV)
+    targets[off] = -100
+    hidden[off] = math.nan
+    loss, lse = sip.sip_xent_forward(hidden, weight, targets, 0.8)
+    gh, gw = sip.sip_xent_backward(hidden, weight, targets, loss, lse, None, 0.5, 0.8)
+    ref = reference(hidden, weight, targets, 0.8, None, 0.5)
+    p_err = 8 * 2.0 ** -24 * math.sqrt(D) * float(ref[4].max()) + 2.0 ** -20
+    for got, want, terms, count in ((gh, ref[2], ref[5], V), (gw, ref[3], ref[6], live)):
+        bound = 2.0 ** -8 * want.abs() + (2.0 ** -16 + p_err + 4 * 2.0 ** -24 * math.sqrt(count)) * 1.01 * terms + 1e-30
+        assert ((got.double() - want).abs() <= bound).all()
+    assert not gh[off].any()
+    # each gradient alone, the same bits
+    a, _ = sip.sip_xent_backward(hidden, weight, targets, loss, lse, None, 0.5, 0.8, want_weight=False)
+    _, b = sip.sip_xent_backward(hidden, weight, targets, loss, lse, None, 0.5, 0.8, want_hidden=False)
+    assert torch.equal(a, gh) and torch.equal(b, gw)
