@@ -48,7 +48,8 @@ extern "C" {
  *  loss,    [N] fp32.
  *  lse
  *  workspace  256-byte aligned, at least sip_xent_workspace_bytes(N, V, D, 0) bytes for
- *             sip_xent_forward(), (N, V, D, 1) for either; contents need not be kept.
+ *             sip_xent_forward(), (N, V, D, 1) for either; contents need not be kept.  What
+ *             is enough for N tokens is enough for fewer of the same V and D.
  */
 size_t sip_xent_workspace_bytes(int32_t N, int32_t V, int32_t D, int32_t backward);
 sip_status sip_xent_forward(const void* hidden, int32_t N, int32_t D, int64_t hidden_stride, const void* weight,

@@ -43,6 +43,10 @@ double tiles_cost(XentShape s, long long a, long long b, long long k, int parts)
   const double read = 2e-6 * a * k / (s == kTiny ? 4.5 : 5.2) + 2e-6 * a * k / 17.0 * (tiles(b, kShapeB[s]) - 1);
   return std::max(us, read) + 0.4 * std::min(us, read);   // (the one hides the other in part)
 }
+// The most workgroups that n_tiles tiles are dealt out among, and into how many parts of at least 256 terms: what bounds the room of
+// the parts' sums.  (Without it one shape in a thousand would take up to 7 % less time by tiles_cost(), and twice the room.)
+constexpr int kPartsMost = 128, kDealtTiles = 1024;      // tiles that may be dealt out at all
+inline long long dealt_most(long long n_tiles) { return std::min<long long>(std::max<long long>(4 * n_tiles, 1024), 2 * kDealtTiles); }
 // The tile that is expected to take the least time, and into how many parts it pays to deal the sums (at most `most`).
 struct Cheapest { XentShape shape; int parts; };
 Cheapest cheapest(std::initializer_list<XentShape> among, long long a, long long b, long long k, int most = 1) {
@@ -50,12 +54,18 @@ Cheapest cheapest(std::initializer_list<XentShape> among, long long a, long long
   double best = -1.0;
   for (XentShape s : among)
     for (int n = 1; n <= most && (n == 1 || k / n >= 256); ++n) {
+      const long long n_tiles = (long long)tiles(a, kShapeA[s]) * tiles(b, kShapeB[s]);
+      if (n > 1 && n * n_tiles > dealt_most(n_tiles)) break;
       const double cost = tiles_cost(s, a, b, k, n) + (n > 1 ? 6.0 + 4e-6 * n * a * b : 0.0);              // (the join)
       if (best < 0.0 || cost < best) { best = cost; c = {s, n}; }
     }
   return c;
 }
 XentShape score_shape(int a, int tokens, int D) { return cheapest({kWide, kQuarter, kNarrow, kSmall, kTiny}, a, tokens, D).shape; }
+// Partial sums of a token in the forward pass, one for each wave's entries; and the room up to which they may be narrower than the
+// widest tile's (no shape has come near it: narrower tiles are for few).
+inline int score_parts(XentShape s, int V) { return tiles(V, kShapeA[s]) * (kShapeA[s] / kShapeWaveA[s]); }
+constexpr size_t kScorePartsRoom = 16 << 20;
 
 // How a cross entropy of this shape is cut, and where its parts lie in the workspace.
 struct XentPlan {
@@ -68,10 +78,24 @@ struct XentPlan {
   size_t count, rows, part, dense, dz, hidden_sum, weight_sum, bytes;
 };
 
+// Rows of dz, for whatever number of N tokens takes part.
+inline int xent_dz_rows(int N) { return std::max<int>(N, 2 * std::min<int>(N, sip::kTwoPartRows)); }
+// Vocabulary entries of a piece: dz takes half a gigabyte at most.  The fewer the more tokens there are.
+constexpr long long kDzMost = 1ll << 28;
+inline int xent_piece(int N, int V) {
+  const long long most = std::max<long long>(256, kDzMost / N / 256 * 256);
+  const int pieces = tiles(V, (int)std::min<long long>(most, 1 << 20));
+  return tiles(tiles(V, pieces), 256) * 256;
+}
+// Up to here grad_hidden does without the widest tile: its parts' sums take four times the room, for 1 % less time in one shape of a
+// hundred.
+constexpr int kNarrowRows = 128;
+
 XentPlan xent_plan(int32_t N, int32_t V, int32_t D, bool backward) {
   XentPlan p{};
   p.score = score_shape(V, N, D);
-  p.parts = tiles(V, kShapeA[p.score]) * (kShapeA[p.score] / kShapeWaveA[p.score]);
+  if ((size_t)N * score_parts(p.score, V) * 8 > kScorePartsRoom) p.score = kWide;
+  p.parts = score_parts(p.score, V);
   size_t at = 0;
   auto take = [&](size_t n) { const size_t here = at; at += head_align(n); return here; };
   p.count = take(4);
@@ -81,15 +105,15 @@ XentPlan xent_plan(int32_t N, int32_t V, int32_t D, bool backward) {
   p.part = take((size_t)N * p.parts * 8);
   p.bytes = at;
   if (backward) {
-    const long long most = std::max<long long>(256, ((1ll << 28) / N) / 256 * 256);   // dz: half a gigabyte at most, or 256 columns
-    const int pieces = tiles(V, (int)std::min<long long>(most, 1 << 20));
-    p.piece = tiles(tiles(V, pieces), 256) * 256;
+    p.piece = xent_piece(N, V);
     const int left = std::min(p.piece, V);
     p.score_piece = score_shape(left, N, D);
     // rows of dz: two each if no more than kTwoPartRows of the tokens take part
     const int two_part_rows = 2 * std::min<int>(N, sip::kTwoPartRows);
-    const long long dz_rows = std::max<int>(N, two_part_rows);
-    const Cheapest h = cheapest({kWide, kNarrow, kSmall}, D, dz_rows, left, 128), w = cheapest({kWide, kSmall}, D, left, dz_rows, 128);
+    const long long dz_rows = xent_dz_rows(N);
+    const Cheapest h = dz_rows > kNarrowRows ? cheapest({kWide, kNarrow, kSmall}, D, dz_rows, left, kPartsMost)
+                                             : cheapest({kNarrow, kSmall}, D, dz_rows, left, kPartsMost);
+    const Cheapest w = cheapest({kWide, kSmall}, D, left, dz_rows, kPartsMost);
     p.hidden = h.shape;
     p.weight = w.shape;
     p.hidden_parts = {nullptr, tiles(D, kShapeA[h.shape]) * tiles(dz_rows, kShapeB[h.shape]), h.parts, 0};
@@ -106,6 +130,34 @@ XentPlan xent_plan(int32_t N, int32_t V, int32_t D, bool backward) {
     p.bytes = std::max(p.bytes, at);
   }
   return p;
+}
+
+// A workspace for N tokens and for fewer: the most that xent_plan() asks for up to N, or a little more.  It only grows with N, though
+// the plans' needs do not: few tokens have two rows of dz each, and smaller tiles or more parts where those pay.
+size_t xent_most_bytes(int32_t N, int32_t V, int32_t D, bool backward) {
+  const size_t lists = head_align(4) + head_align((size_t)N * 4);
+  const size_t score = std::max((size_t)N * score_parts(kWide, V) * 8, std::min((size_t)N * score_parts(kTiny, V) * 8, kScorePartsRoom));
+  if (!backward) return lists + head_align(score);
+  const long long dz_rows = xent_dz_rows(N), columns = tiles(V, 256) * 256;
+  // tiles that are dealt out, no more than n_tiles, for sums of up to k terms
+  auto dealt = [](long long n_tiles, long long k) {
+    n_tiles = std::min<long long>(n_tiles, kDealtTiles);
+    return std::min(dealt_most(n_tiles), n_tiles * std::min<long long>(kPartsMost, k / 256));
+  };
+  size_t hidden = 0, weight = 0;
+  for (XentShape s : {kWide, kNarrow, kSmall}) {
+    if (s == kWide && dz_rows <= kNarrowRows) continue;
+    const long long n_tiles = (long long)tiles(D, kShapeA[s]) * tiles(dz_rows, kShapeB[s]);
+    hidden = std::max(hidden, (size_t)std::max(n_tiles, dealt(n_tiles, V)) * kShapeA[s] * kShapeB[s] * 4);
+  }
+  if (dz_rows >= 2 * 256)
+    for (XentShape s : {kWide, kSmall}) {
+      const long long fewest = (long long)tiles(D, kShapeA[s]) * tiles(std::min(xent_piece(N, V), V), kShapeB[s]);
+      if (fewest <= kDealtTiles)
+        weight = std::max(weight, (size_t)dealt((long long)tiles(D, kShapeA[s]) * tiles(V, kShapeB[s]), dz_rows) * kShapeA[s] * kShapeB[s] * 4);
+    }
+  const size_t dz = (size_t)std::min(dz_rows * columns, kDzMost) * 2;
+  return lists + std::max(head_align(score), head_align((size_t)dz_rows * D * 2) + head_align(dz) + head_align(hidden) + head_align(weight));
 }
 
 // f(S{}) with the tile's type, one of those named.
@@ -218,7 +270,7 @@ void many_rows_of(const sip::CodesArgs& a, hipStream_t stream) {
 extern "C" {
 
 size_t sip_xent_workspace_bytes(int32_t N, int32_t V, int32_t D, int32_t backward) {
-  return xent_shape_ok(N, V, D) ? xent_plan(N, V, D, backward != 0).bytes : 0;
+  return xent_shape_ok(N, V, D) ? xent_most_bytes(N, V, D, backward != 0) : 0;
 }
 
 sip_status sip_xent_forward(const void* hidden, int32_t N, int32_t D, int64_t hidden_stride, const void* weight,

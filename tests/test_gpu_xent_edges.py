@@ -68,3 +68,18 @@ def test_few_tokens_among_masked_ones(N, live, V, D):
     a, _ = sip.sip_xent_backward(hidden, weight, targets, loss, lse, None, 0.5, 0.8, want_weight=False)
     _, b = sip.sip_xent_backward(hidden, weight, targets, loss, lse, None, 0.5, 0.8, want_hidden=False)
     assert torch.equal(a, gh) and torch.equal(b, gw)
+
+
+def test_one_workspace_for_batches_of_any_size():
+    """A workspace that is enough for the largest batch serves the smaller ones, both ways, and gives their bits."""
+    V, D, most = 3001, 264, 700
+    ws = torch.empty(sip.sip_xent_workspace_bytes(most, V, D, True), dtype=torch.uint8, device=DEV)
+    small = torch.empty(sip.sip_xent_workspace_bytes(most, V, D, False), dtype=torch.uint8, device=DEV)
+    for N in (700, 699, 513, 384, 257, 130, 128, 100, 65, 64, 63, 33, 20, 3, 1):
+        hidden, weight, targets = make(N, V, D, seed=N, masked=0.1)
+        want = sip.sip_xent_forward(hidden, weight, targets)
+        for w in (ws, small):
+            assert all(torch.equal(a, b) for a, b in zip(sip.sip_xent_forward(hidden, weight, targets, workspace=w), want))
+        for a, b in zip(sip.sip_xent_backward(hidden, weight, targets, *want, workspace=ws),
+                        sip.sip_xent_backward(hidden, weight, targets, *want)):
+            assert torch.equal(a, b)
