@@ -442,7 +442,7 @@ sip_status sip_head_logits(const void* hidden, int32_t B, int32_t D, int64_t hid
   const sip_status ok = codes_check(codes, codes_stride, scales, scales_dtype, V, D, group);
   if (ok != SIP_OK) return ok;
   const int x_size = hidden_dtype == SIP_F32 ? 4 : 2, z_size = logits_dtype == SIP_F32 ? 4 : 2;
-  if (hidden_stride < D || hidden_stride * x_size % 16 != 0 || !aligned16(hidden) || logits_stride < V ||
+  if (hidden_stride < D || hidden_stride % (16 / x_size) != 0 || !aligned16(hidden) || logits_stride < V ||
       reinterpret_cast<uintptr_t>(logits) % z_size != 0)
     return SIP_ERR_INVALID_ARG;
   if (B > SIP_MAX_B || hidden_stride > (1ll << 32) || logits_stride > (1ll << 32)) return SIP_ERR_UNSUPPORTED;
