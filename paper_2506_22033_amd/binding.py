@@ -52,9 +52,9 @@ class SipCall(ctypes.Structure):
 
 
 class SipError(RuntimeError):
-    def __init__(self, status: int):
+    def __init__(self, status: int, call: str = "sip_sample"):
         self.status = status
-        super().__init__(f"sip_sample failed: {sip_status_string(status)} (status {status})")
+        super().__init__(f"{call} failed: {sip_status_string(status)} (status {status})")
 
 
 _lib = None

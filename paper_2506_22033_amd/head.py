@@ -51,9 +51,11 @@ def _load() -> ctypes.CDLL:
     return lib
 
 
-def _check(status: int) -> None:
+def _call(name: str, dev: torch.device, stream: Optional[torch.cuda.Stream], *args) -> None:
+    """The library's ``name`` on ``stream``, its last argument."""
+    status = getattr(_load(), name)(*args, _stream_handle(dev, stream))
     if status != SIP_OK:
-        raise SipError(status)
+        raise SipError(status, name)
 
 
 def _matrix(t: torch.Tensor, name: str, dtypes, shape=None) -> torch.Tensor:
@@ -121,8 +123,8 @@ def sip_xent_forward(hidden: torch.Tensor, weight: torch.Tensor, targets: torch.
     if N == 0:
         return loss, lse
     ws = _scratch(workspace, 0 if workspace is not None else lib.sip_xent_workspace_bytes(N, V, D, 0), dev, stream)
-    _check(lib.sip_xent_forward(_ptr(hidden), N, D, _stride(hidden), _ptr(weight), V, _stride(weight), _ptr(targets),
-                                logit_scale, _ptr(loss), _ptr(lse), _ptr(ws), _nbytes(ws), _stream_handle(dev, stream)))
+    _call("sip_xent_forward", dev, stream, _ptr(hidden), N, D, _stride(hidden), _ptr(weight), V, _stride(weight),
+          _ptr(targets), logit_scale, _ptr(loss), _ptr(lse), _ptr(ws), _nbytes(ws))
     return loss, lse
 
 
@@ -155,10 +157,9 @@ def sip_xent_backward(hidden: torch.Tensor, weight: torch.Tensor, targets: torch
                 gw.zero_()
         return gh, gw
     ws = _scratch(workspace, 0 if workspace is not None else lib.sip_xent_workspace_bytes(N, V, D, 1), dev, stream)
-    _check(lib.sip_xent_backward(_ptr(hidden), N, D, _stride(hidden), _ptr(weight), V, _stride(weight), _ptr(targets),
-                                 logit_scale, _ptr(loss), _ptr(lse), _ptr(grad_loss), scale, _ptr(gh),
-                                 0 if gh is None else _stride(gh), _ptr(gw), 0 if gw is None else _stride(gw), _ptr(ws),
-                                 _nbytes(ws), _stream_handle(dev, stream)))
+    _call("sip_xent_backward", dev, stream, _ptr(hidden), N, D, _stride(hidden), _ptr(weight), V, _stride(weight),
+          _ptr(targets), logit_scale, _ptr(loss), _ptr(lse), _ptr(grad_loss), scale, _ptr(gh),
+          0 if gh is None else _stride(gh), _ptr(gw), 0 if gw is None else _stride(gw), _ptr(ws), _nbytes(ws))
     return gh, gw
 
 
@@ -197,7 +198,7 @@ def sip_grad_clip(grads, max_norm: float, *, eps: float = 1e-6, norm: Optional[t
     norm = _empty(stream, (), dtype=torch.float32, device=t.device) if norm is None else _vector(norm, "norm", torch.float32, 1)
     _same_device(t.device, norm)
     ws = _scratch(workspace, 0 if workspace is not None else lib.sip_grad_clip_workspace_bytes(t.n), t.device, stream)
-    _check(lib.sip_grad_clip(t.table, t.n, max_norm, eps, _ptr(norm), _ptr(ws), _nbytes(ws), _stream_handle(t.device, stream)))
+    _call("sip_grad_clip", t.device, stream, t.table, t.n, max_norm, eps, _ptr(norm), _ptr(ws), _nbytes(ws))
     return norm
 
 
@@ -222,7 +223,6 @@ def sip_head_quantize(weight: torch.Tensor, group: int = 128, *, use_zeros: bool
     """(codes [V, D / 2], scales [V, D / group], zeros or None) of bf16 ``weight`` [V, D].  Outputs are allocated when
     not supplied, ``zeros`` if ``use_zeros``; where both ``codes`` and ``scales`` are, ``zeros`` alone says whether the groups
     have zero points."""
-    lib = _load()
     _matrix(weight, "weight", (torch.bfloat16,))
     V, D = weight.shape
     if group <= 0 or D % group != 0:
@@ -237,8 +237,8 @@ def sip_head_quantize(weight: torch.Tensor, group: int = 128, *, use_zeros: bool
     if _codes_operands(codes, scales, zeros) != (V, D, group):
         raise TypeError("codes and scales do not fit the weight and the group")
     _same_device(dev, codes, scales, zeros)
-    _check(lib.sip_head_quantize(_ptr(weight), V, D, _stride(weight), group, _ptr(codes), _stride(codes), _ptr(scales),
-                                 _DTYPES[scales.dtype], _ptr(zeros), _stream_handle(dev, stream)))
+    _call("sip_head_quantize", dev, stream, _ptr(weight), V, D, _stride(weight), group, _ptr(codes), _stride(codes),
+          _ptr(scales), _DTYPES[scales.dtype], _ptr(zeros))
     return codes, scales, zeros
 
 
@@ -265,7 +265,7 @@ def sip_head_logits(hidden: torch.Tensor, codes: torch.Tensor, scales: torch.Ten
     if B == 0:
         return out
     ws = _scratch(workspace, 0 if workspace is not None else lib.sip_head_workspace_bytes(B, V, D, group), dev, stream)
-    _check(lib.sip_head_logits(_ptr(hidden), B, D, _stride(hidden), _DTYPES[hidden.dtype], _ptr(codes), _stride(codes),
-                               _ptr(scales), _DTYPES[scales.dtype], _ptr(zeros), group, V, _ptr(out), _stride(out),
-                               _DTYPES[out.dtype], _ptr(ws), _nbytes(ws), _stream_handle(dev, stream)))
+    _call("sip_head_logits", dev, stream, _ptr(hidden), B, D, _stride(hidden), _DTYPES[hidden.dtype], _ptr(codes),
+          _stride(codes), _ptr(scales), _DTYPES[scales.dtype], _ptr(zeros), group, V, _ptr(out), _stride(out),
+          _DTYPES[out.dtype], _ptr(ws), _nbytes(ws))
     return out

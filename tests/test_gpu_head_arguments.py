@@ -79,3 +79,20 @@ def test_the_stride_of_a_single_row_says_nothing():
         got = sip.sip_head_quantize(_single(w, pad), 32, codes=_single(one[0], pad))
         assert all(torch.equal(a, b) for a, b in zip(got, one))
         assert torch.equal(sip.sip_head_logits(h, _single(one[0], pad), *one[1:]), sip.sip_head_logits(h, *one))
+
+
+def test_errors_name_the_call():
+    h, w, t = torch.zeros(2, 12, dtype=BF16, device=DEV), torch.zeros(9, 12, dtype=BF16, device=DEV), torch.zeros(
+        2, dtype=torch.int32, device=DEV)
+    x = torch.zeros(2, device=DEV)
+    with pytest.raises(sip.SipError, match="sip_xent_forward failed"):
+        sip.sip_xent_forward(h, w, t)
+    with pytest.raises(sip.SipError, match="sip_xent_backward failed"):
+        sip.sip_xent_backward(h, w, t, x, x)
+    with pytest.raises(sip.SipError, match="sip_grad_clip failed"):
+        sip.sip_grad_clip([x], -1.0)
+    with pytest.raises(sip.SipError, match="sip_head_quantize failed"):
+        sip.sip_head_quantize(torch.zeros(4, 48, dtype=BF16, device=DEV), 16)
+    with pytest.raises(sip.SipError, match="sip_head_logits failed"):
+        sip.sip_head_logits(torch.zeros(2, 48, dtype=BF16, device=DEV), torch.zeros(4, 24, dtype=torch.uint8, device=DEV), torch.ones(4, 3, device=DEV))
+    assert "sip_sample failed" in str(sip.SipError(1))
