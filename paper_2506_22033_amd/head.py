@@ -52,8 +52,14 @@ def _load() -> ctypes.CDLL:
 
 
 def _call(name: str, dev: torch.device, stream: Optional[torch.cuda.Stream], *args) -> None:
-    """The library's ``name`` on ``stream``, its last argument."""
-    status = getattr(_load(), name)(*args, _stream_handle(dev, stream))
+    """The library's ``name`` on ``stream`` (its last argument), with the tensors' device as the current one: a device's default
+    stream is that of whichever is current."""
+    fn = getattr(_load(), name)
+    if dev.index == torch.cuda.current_device():
+        status = fn(*args, _stream_handle(dev, stream))
+    else:
+        with torch.cuda.device(dev):
+            status = fn(*args, _stream_handle(dev, stream))
     if status != SIP_OK:
         raise SipError(status, name)
 

@@ -96,3 +96,24 @@ def test_errors_name_the_call():
     with pytest.raises(sip.SipError, match="sip_head_logits failed"):
         sip.sip_head_logits(torch.zeros(2, 48, dtype=BF16, device=DEV), torch.zeros(4, 24, dtype=torch.uint8, device=DEV), torch.ones(4, 3, device=DEV))
     assert "sip_sample failed" in str(sip.SipError(1))
+
+
+def test_the_tensors_device_is_the_current_one_during_a_call(monkeypatch):
+    """With another device current, a device's default stream would be that other's.  (On one device: the current one is said to
+    be another.)"""
+    w = torch.ones(8, 64, dtype=BF16, device=DEV)
+    want = sip.sip_head_quantize(w, 64)
+    entered = []
+
+    class Recorded(torch.cuda.device):
+        def __enter__(self):
+            entered.append(self.idx)
+            return super().__enter__()
+
+    monkeypatch.setattr(torch.cuda, "device", Recorded)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
+    got = sip.sip_head_quantize(w, 64)
+    monkeypatch.undo()
+    assert entered == [w.device.index]
+    sip.sip_head_quantize(w, 64)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
