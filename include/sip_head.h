@@ -121,7 +121,8 @@ sip_status sip_grad_clip(const sip_grad* tensors, int32_t n_tensors, float max_n
  * smaller of 0 and the smallest weight and hi the larger of 0 and the largest,
  *   zeros given:  s = (hi - lo) / 15,         zero = clamp(rint(-lo / s), 0, 15)
  *   zeros NULL:   s = max(hi, -lo) / 7,       zero = 8
- * s rounded to its type (and 1 if that is 0), q = clamp(rint(w / s) + zero, 0, 15), all in fp32.
+ * s rounded to its type (and 1 if that is 0), q = clamp(rint(w / s) + zero, 0, 15), all in fp32.  A group that
+ * holds an infinity or a NaN gets that as its scale: logits made from it are not finite.
  */
 sip_status sip_head_quantize(const void* weight, int32_t V, int32_t D, int64_t weight_stride, int32_t group,
                              uint8_t* codes, int64_t codes_stride, void* scales, sip_dtype scales_dtype,
@@ -137,8 +138,9 @@ sip_status sip_head_quantize(const void* weight, int32_t V, int32_t D, int64_t w
  *           logits_stride a multiple of 16 bytes makes rows that sip_sample() takes.
  *  workspace  256-byte aligned, at least sip_head_workspace_bytes(B, V, D, group) bytes.
  * Products are exact, sums fp32, scales are applied to the fp32 sum of a group; rounded once.  A code enters as 16 + q, and what
- * that adds is taken off again, by group up to 32 rows (an fp32 state counts as three), by 256 entries beyond: states whose mean
- * is far from zero lose about three bits more there.
+ * that adds is taken off again: by group for up to 16 rows with D from 128 to 8192, or 32 with D up to 4096 (an fp32 state counts
+ * as three), else by 256 entries, where states whose mean is far from zero lose about three bits more.  An infinity or a NaN in a
+ * hidden state makes the whole of its row infinite or NaN, and other rows nothing.
  */
 size_t sip_head_workspace_bytes(int32_t B, int32_t V, int32_t D, int32_t group);
 sip_status sip_head_logits(const void* hidden, int32_t B, int32_t D, int64_t hidden_stride, sip_dtype hidden_dtype,

@@ -266,8 +266,9 @@ constexpr int few_tiles(int group, bool scales_bf16, int units, int mt) {
 // Products: 16 + q against the states, from - (16 + zero) times the group's sum of the states on; the scale on the fp32
 // sum of a group.
 // Bound by reading the head: one row, V = 128256, D = 4096, groups of 128 51 us, 5.3 TB/s.  With groups of 32, fp32 scales and
-// 7 fp32 states (two rows of tiles), V = 151643, D = 2080, 106 us, 2.0 TB/s: a tile a turn is all that registers hold then, and
-// scales, sums by group and the codes' conversion take the vector units longer than the reads take.
+// 7 fp32 states (two rows of tiles), V = 151643, D = 2080, 106 us, 2.0 TB/s: a tile a turn is all that registers hold then,
+// scales, sums by group and the codes' conversion take the vector units longer than the reads take, and of the 17 units the last
+// wave has three where the others have two, which wait for it every turn.
 template <int GROUP, bool SCALES_BF16, int UNITS, int MT>
 __global__ __launch_bounds__(kFewWaves * 64) void head_few_kernel(CodesArgs p) {
   constexpr int NT = few_tiles(GROUP, SCALES_BF16, UNITS, MT);
@@ -516,7 +517,7 @@ __global__ __launch_bounds__(256) void head_rows_kernel(CodesArgs p, int mt) {
 // zero, cancels within 256 entries.  States of mean 1, D = 4096, groups of 128 and 32: off by 4.3e-7 and 1.0e-6 of the result; with a
 // row's second part added as a whole 2.2e-6 and 9.8e-6, for 3 to 10 % less time.
 // 256 rows, V = 152064, D = 4096, fp32 logits, groups of 128, 64, 32: 393, 450, 647 us, 811, 709, 493 TFLOP/s.  In groups of 64
-// matrix cores are busy for 30 % of it and vector units for 40 (half of that the scales' multiplications), which two waves of a
+// matrix cores are busy for 33 % of it and vector units for 43 (half of that the scales' multiplications), which two waves of a
 // SIMD do not hide behind each other altogether; reads further ahead or four waves of half the entries changed nothing.
 template <int GROUP, bool SCALES_BF16, int MT, int WAVES, int NT>
 __global__ __launch_bounds__(WAVES * 64) void head_many_kernel(CodesArgs p) {

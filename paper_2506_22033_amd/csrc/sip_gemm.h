@@ -4,8 +4,8 @@
 //
 // Tiles of both operands go from memory to LDS without passing registers, a unit of 64 k at a time -- whole 128-byte lines
 // of either form --, one unit of B and two of A ahead of their use in the widest tile: a unit's products take 2048 cycles of the
-// matrix cores, a load that misses the L2 some 2500.  Four waves hold a quarter of the tile each (128 x 128: 256
-// accumulators a lane), so that LDS serves 64 bytes a cycle of the 128 it has.  What an element is read as 16-byte groups
+// matrix cores, a load that misses the L2 some 2500.  There eight waves hold 128 x 64 each (128 accumulators a lane), two a SIMD,
+// for which LDS serves 96 bytes a cycle of the 128 it has.  What an element is read as 16-byte groups
 // for, eight of its neighbours along k, a kCols tile delivers by transposing reads.  Groups lie in LDS permuted (swizzled) so
 // that the lanes of a read meet every bank once.
 #pragma once
@@ -118,7 +118,7 @@ struct FragmentReader {
 #pragma unroll
       for (int s = 0; s < K / 32; ++s) at[s] = i * K * 2 + (((4 * s + (lane >> 4)) ^ swizzle_rows(i)) << 4);
     } else {
-      // (i0 a multiple of 64: block t's 16-byte groups are those of block 0 with 2 t in the bits that the swizzle turns)
+      // (i0 a multiple of 16 T, T a power of two: block t's 16-byte groups are those of block 0 with 2 t in bits that are clear there)
       const int k = 8 * (lane >> 4) + ((lane & 15) >> 2), i = i0 + ((lane & 3) << 2);
       at[0] = k * I * 2 + (((i >> 3) ^ swizzle_cols(k)) << 4) + ((i & 4) << 1);
     }
@@ -172,8 +172,8 @@ struct Gemm {
     auto read_b = [&](int j, int u, int s) { fb[s & 1][j] = rb.read(lds0 + kLdsB + (uint32_t)u % S::kSlotsB * S::kBytesB, s, j); };
     constexpr int kRow = S::kTB, kProducts = S::kTA * kRow;
     constexpr int kBefore = S::kTA > 2 ? 2 : 1;            // rows of a unit's second step that come before its barrier
-    // Of the loads between two barriers, those that are issued before product q behind the first: evenly spread.  (Four waves'
-    // loads in a row wait for the address unit, 16 cycles a load, and the products behind them too.)
+    // Of the loads between two barriers, those that are issued before product q behind the first: evenly spread.  (All in a row
+    // they wait for the address unit, 16 cycles a load, and the products behind them too.)
     auto issued = [](int q) constexpr { return q * S::kLoads / (2 * kProducts); };
 #pragma unroll
     for (int u = 0; u < S::kSlotsA - 1; ++u) {

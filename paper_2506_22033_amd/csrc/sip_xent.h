@@ -168,9 +168,9 @@ __device__ inline void store_tile(SIP_LDS char* lds, int a0, int a_end, Value va
   }
 }
 
-// A tile of logits, reduced to its maximum and sum of exponentials per token and wave.  With many tokens bound by the matrix cores
-// at the clock that their power leaves (1.6 of 2.4 GHz, busy for 72 % of it): 8192 tokens, V = 128256, D = 4096 6.5 ms,
-// 1.33 PFLOP/s; with few by reading the head.
+// A tile of logits, reduced to its maximum and sum of exponentials per token and wave.  With many tokens bound by the matrix cores,
+// busy for 68 % of the cycles at the 1.7 to 1.9 of 2.4 GHz that the card keeps up under them, and by the ends of the tiles: 8192
+// tokens, V = 128256, D = 4096 6.5 ms, 1.32 PFLOP/s; with few by reading the head.
 template <class S>
 __global__ __launch_bounds__(S::kThreads) void xent_forward_kernel(XentArgs p) {
   __shared__ __attribute__((aligned(1024))) char lds[S::kLds];

@@ -2,7 +2,8 @@
 pointers.  Argument marshalling only; there is no fallback.
 
 A call runs on ``stream`` (default: torch's current stream).  The outputs and the scratch memory that it allocates because they
-were not supplied belong to that stream, as under ``torch.cuda.stream(stream)``."""
+were not supplied belong to that stream, as under ``torch.cuda.stream(stream)``.  The calls are no operations of torch's: a tensor that
+requires a gradient is read like any other, and nothing is recorded; gradients are what sip_xent_backward returns."""
 from __future__ import annotations
 
 import ctypes
