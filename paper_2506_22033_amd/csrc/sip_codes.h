@@ -481,9 +481,9 @@ struct SumParts {
 // A wave takes a tile of 16 rows and a group.
 template <int GROUP>
 __global__ __launch_bounds__(256) void head_rows_kernel(CodesArgs p, int mt) {
-  const int lane = threadIdx.x & 63, quad = lane >> 4, g = blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63, quad = lane >> 4, g = blockIdx.y * 4 + (threadIdx.x >> 6);
   if (g >= many_groups(p.D, GROUP)) return;
-  const int block = blockIdx.y / mt, tile = blockIdx.y % mt, each = rows_of_state(p.hidden_bf16), states = block_states(mt, p.hidden_bf16);
+  const int block = blockIdx.x / mt, tile = blockIdx.x % mt, each = rows_of_state(p.hidden_bf16), states = block_states(mt, p.hidden_bf16);
   const int r = tile * 16 + (lane & 15), state = block * states + r / each;
   const bool live = r < states * each && state < p.B;
   const ManyLayout layout(p.D, GROUP, mt);

@@ -253,7 +253,7 @@ size_t many_bytes(int32_t B, int32_t D, int32_t group, bool hidden_bf16) {
 template <int GROUP>
 void many_rows_of(const sip::CodesArgs& a, hipStream_t stream) {
   const int mt = many_tiles(a.B, a.hidden_bf16), blocks = tiles(a.B, sip::block_states(mt, a.hidden_bf16));
-  hipLaunchKernelGGL(sip::head_rows_kernel<GROUP>, dim3(tiles(sip::many_groups(a.D, GROUP), 4), blocks * mt), dim3(256), 0, stream, a, mt);
+  hipLaunchKernelGGL(sip::head_rows_kernel<GROUP>, dim3(blocks * mt, tiles(sip::many_groups(a.D, GROUP), 4)), dim3(256), 0, stream, a, mt);
   auto launch = [&](auto row_tiles, auto waves, auto nt) {
     constexpr int kMt = decltype(row_tiles)::value, kWaves = decltype(waves)::value, kNt = decltype(nt)::value;
     const dim3 grid(tiles(tiles(a.V, kWaves * kNt * 16), 8) * 8 * blocks), threads(kWaves * 64);
