@@ -6,7 +6,8 @@
  * turns those into tokens.  The functions here score given tokens under W and differentiate that
  * score without ever holding the logits (sip_xent_*), bound a set of gradients by their common norm
  * (sip_grad_clip), bring W to 4 bits (sip_head_quantize), and make the logits of a decode step from
- * such weights in the form that sip_sample() takes (sip_head_logits).
+ * such weights in the form that sip_sample() takes (sip_head_logits), with every request's own low-rank adapter on top
+ * (sip_head_adapt).  sip_embed() and its gradient are the matrix's other use, from tokens to vectors.
  *
  * Conventions are those of sip.h: DEVICE pointers, caller-owned buffers, everything enqueued on
  * `hip_stream`, argument errors found on the host before anything is enqueued, no allocation and no
@@ -26,6 +27,8 @@ extern "C" {
 #define SIP_MAX_D 16384        /* widest hidden state                                              */
 #define SIP_MAX_TOKENS 65536   /* most tokens of one sip_xent_* call                               */
 #define SIP_MAX_TENSORS 65536  /* most tensors of one sip_grad_clip() call                         */
+#define SIP_MAX_RANK 128       /* widest low-rank adapter                                          */
+#define SIP_MAX_ADAPTERS 4096  /* most adapters of one sip_head_adapt() call                       */
 
 /*
  * ---- Cross entropy of given tokens under the head, and its gradient ----------------------------
@@ -147,6 +150,69 @@ sip_status sip_head_logits(const void* hidden, int32_t B, int32_t D, int64_t hid
                            const uint8_t* codes, int64_t codes_stride, const void* scales, sip_dtype scales_dtype,
                            const uint8_t* zeros, int32_t group, int32_t V, void* logits, int64_t logits_stride,
                            sip_dtype logits_dtype, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * ---- Low-rank adapters of many requests beside the shared head ---------------------------------------
+ *
+ *   t[b, j]       = sum_d down[a, j, d] * hidden[b, d],   a = adapter_of_row[b]
+ *   logits[b, v] += scales[a] * sum_j up[a, v, j] * t[b, j]
+ *
+ * in place, behind whatever made the logits.  A row whose adapter lies outside [0, adapters) is not touched, and what its
+ * hidden state holds goes nowhere.
+ *
+ *  hidden    [B, hidden_stride] bf16 or fp32, B up to SIP_MAX_TOKENS, rows aligned to 16 bytes.
+ *  down      [adapters, rank, D] bf16, up [adapters, V, rank] bf16, contiguous, aligned to 16 bytes.  An adapter of a
+ *            smaller rank is filled up with zeros.
+ *  rank      a multiple of 8 up to SIP_MAX_RANK; D a multiple of 8.
+ *  scales    [adapters] fp32, NULL = 1.
+ *  logits    [B, logits_stride] fp32 or bf16, aligned to its element; only the first V entries of a row are read or written.
+ *  workspace 256-byte aligned, at least sip_head_adapt_workspace_bytes(B, adapters, rank, D) bytes.  What is enough for B
+ *            rows is enough for fewer.
+ * Products and sums are fp32, t is kept in fp32; the new logit is rounded once.
+ */
+size_t sip_head_adapt_workspace_bytes(int32_t B, int32_t adapters, int32_t rank, int32_t D);
+sip_status sip_head_adapt(const void* hidden, int32_t B, int32_t D, int64_t hidden_stride, sip_dtype hidden_dtype,
+                          const void* down, const void* up, int32_t adapters, int32_t rank, const int32_t* adapter_of_row,
+                          const float* scales, int32_t V, void* logits, int64_t logits_stride, sip_dtype logits_dtype,
+                          void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * ---- Embedding: rows of the matrix by token, and their gradient ---------------------------------------
+ *
+ *   out[i] = scale * weight[ids[i]]
+ *
+ * in fp32, rounded once.  A token outside [0, V) -- padding -- gives a row of zeros.
+ *
+ *  weight  [V, weight_stride] bf16 or fp32 (sip_embed), or a head of 4-bit codes as sip_head_quantize() makes it
+ *          (sip_embed_codes), which then serves both ends of a model: weight = scales * (q - zeros).
+ *  D       a multiple of 8, of the group for codes.
+ *  ids     [N] int32; N = 0 is allowed and does nothing.  N up to SIP_MAX_B.
+ *  out     [N, out_stride] bf16 or fp32.  Rows of weight and out are aligned to 16 bytes.
+ */
+sip_status sip_embed(const void* weight, sip_dtype weight_dtype, int32_t V, int32_t D, int64_t weight_stride, const int32_t* ids,
+                     int32_t N, float scale, void* out, int64_t out_stride, sip_dtype out_dtype, void* hip_stream);
+sip_status sip_embed_codes(const uint8_t* codes, int64_t codes_stride, const void* scales, sip_dtype scales_dtype,
+                           const uint8_t* zeros, int32_t group, int32_t V, int32_t D, const int32_t* ids, int32_t N, float scale,
+                           void* out, int64_t out_stride, sip_dtype out_dtype, void* hip_stream);
+
+/*
+ *   grad_weight[v] = scale * sum_{i: ids[i] = v} grad_out[i]   (+ grad_weight[v] if accumulate)
+ *
+ * Tokens are sorted, and a row of grad_weight is the fp32 sum of its tokens' rows in an order that depends on the
+ * tokens alone, scaled, added to what was there if asked for, and rounded once.  A token outside [0, V) takes no part, whatever
+ * its row of grad_out holds.  With accumulate != 0 rows of grad_weight that no token names are not touched; without, they
+ * become zeros.  (A matrix that is head and embedding at once: sip_xent_backward() first, then this call with accumulate.)
+ *
+ *  grad_out    [N, grad_out_stride] bf16 or fp32, grad_weight [V, grad_weight_stride] bf16 or fp32; rows aligned to 16 bytes.
+ *  N           0 .. SIP_MAX_TOKENS; D a multiple of 8.
+ *  workspace   256-byte aligned, at least sip_embed_workspace_bytes(N, V, D) bytes.  What is enough for N tokens is enough
+ *              for fewer.
+ */
+size_t sip_embed_workspace_bytes(int32_t N, int32_t V, int32_t D);
+sip_status sip_embed_backward(const void* grad_out, int64_t grad_out_stride, sip_dtype grad_out_dtype, const int32_t* ids, int32_t N,
+                              int32_t V, int32_t D, float scale, int32_t accumulate, void* grad_weight,
+                              int64_t grad_weight_stride, sip_dtype grad_weight_dtype, void* workspace, size_t workspace_bytes,
+                              void* hip_stream);
 
 #ifdef __cplusplus
 }

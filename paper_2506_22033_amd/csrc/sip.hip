@@ -898,5 +898,7 @@ int sip_version(void) { return 100; }
 
 }  // extern "C"
 
-// The vocabulary head (include/sip_head.h).
+// The vocabulary head, adapters and embedding (include/sip_head.h); beam search (include/sip_beam.h).
 #include "sip_vocab.h"
+#include "sip_vector.h"
+#include "sip_search.h"

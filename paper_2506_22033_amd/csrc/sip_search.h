@@ -1,0 +1,87 @@
+// Host side of the entry points declared in include/sip_beam.h: argument checks, workspace carving, launches.
+#pragma once
+#include <cmath>
+
+#include "../../include/sip_beam.h"
+#include "sip_beam.h"
+#include "sip_host.h"
+
+namespace {
+
+inline int beam_chunks(int32_t V) { return tiles(V, sip::kBeamChunk); }
+bool beam_shape_ok(int32_t groups, int32_t width, int32_t V, int32_t n) {
+  return groups > 0 && width > 0 && V > 0 && n > 0 && width <= SIP_MAX_BEAMS && V <= SIP_MAX_V && n <= SIP_MAX_CONTINUATIONS &&
+         (int64_t)groups * width <= SIP_MAX_B;
+}
+static_assert(SIP_MAX_V <= 64 * sip::kBeamChunk, "beam_merge_kernel: a lane a chunk, kHeads lists a lane");
+size_t beam_part_bytes(int64_t lists) { return head_align((size_t)lists * sizeof(sip::BeamPart)); }
+
+}  // namespace
+
+extern "C" {
+
+size_t sip_beam_workspace_bytes(int32_t groups, int32_t width, int32_t V, int32_t n) {
+  if (!beam_shape_ok(groups, width, V, n)) return 0;
+  const int64_t lists = (int64_t)groups * width * beam_chunks(V);
+  return beam_part_bytes(lists) + head_align((size_t)lists * n * 8);
+}
+
+sip_status sip_beam_select(const void* logits, int32_t groups, int32_t width, int32_t V, int64_t row_stride, sip_dtype dtype,
+                           float logit_scale, const float* scores, const uint8_t* finished, int32_t end_token,
+                           const float* rank_scale, int32_t n, int32_t* tokens, int32_t* parents, float* out_scores,
+                           void* workspace, size_t workspace_bytes, void* hip_stream) {
+  if (!logits || !scores || !tokens || !parents || !out_scores || groups <= 0 || width <= 0 || V <= 0 || n <= 0 || !dtype_ok(dtype))
+    return SIP_ERR_INVALID_ARG;
+  if (!rows_ok(logits, V, row_stride, dtype) || !(logit_scale >= 1e-30f && logit_scale <= 1e30f)) return SIP_ERR_INVALID_ARG;
+  if (finished && (end_token < 0 || end_token >= V)) return SIP_ERR_INVALID_ARG;
+  if (!beam_shape_ok(groups, width, V, n) || row_stride > (1ll << 32)) return SIP_ERR_UNSUPPORTED;
+  if (!workspace_ok(workspace, workspace_bytes, sip_beam_workspace_bytes(groups, width, V, n))) return SIP_ERR_WORKSPACE;
+  sip::BeamArgs a{};
+  a.logits = logits; a.row_stride = row_stride;
+  a.groups = groups; a.width = width; a.V = V; a.n = n;
+  a.chunks = beam_chunks(V);
+  a.scale = (double)logit_scale;
+  // below the exact product, so that c_lo > 0: (-inf) c_hi + (-inf) c_lo is -inf then
+  const double c = a.scale * 1.4426950408889634074;
+  a.c_hi = (float)c;
+  if ((double)a.c_hi >= c) a.c_hi = std::nextafterf(a.c_hi, 0.0f);
+  a.c_lo = (float)(c - (double)a.c_hi);
+  a.scores = scores; a.finished = finished; a.rank_scale = rank_scale; a.end_token = end_token;
+  a.tokens = tokens; a.parents = parents; a.out_scores = out_scores;
+  const int64_t lists = (int64_t)groups * width * a.chunks;
+  a.part = static_cast<sip::BeamPart*>(workspace);
+  a.cand = reinterpret_cast<unsigned long long*>(static_cast<char*>(workspace) + beam_part_bytes(lists));
+  hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+  if (dtype == SIP_BF16) hipLaunchKernelGGL(sip::beam_chunk_kernel<true>, dim3(lists), dim3(sip::kBeamThreads), 0, stream, a);
+  else hipLaunchKernelGGL(sip::beam_chunk_kernel<false>, dim3(lists), dim3(sip::kBeamThreads), 0, stream, a);
+  constexpr int kFew = sip::merge_room(512, 31), kMany = sip::merge_room(SIP_MAX_BEAMS * 64, SIP_MAX_CONTINUATIONS);
+  if (sip::merge_room(width * a.chunks, n) <= kFew)
+    hipLaunchKernelGGL(sip::beam_merge_kernel<kFew>, dim3(groups), dim3(sip::kMergeThreads), 0, stream, a);
+  else
+    hipLaunchKernelGGL(sip::beam_merge_kernel<kMany>, dim3(groups), dim3(sip::kMergeThreads), 0, stream, a);
+  return launched();
+}
+
+sip_status sip_state_reorder(void* state, size_t state_bytes, int32_t slots, int32_t L_max, int32_t groups, int32_t width,
+                             const int32_t* slot_of_row, const int32_t* parents, const int32_t* tokens, void* hip_stream) {
+  if (slots <= 0 || L_max <= 0 || slots > SIP_MAX_SLOTS || L_max > SIP_MAX_L || groups < 0 || width <= 0) return SIP_ERR_INVALID_ARG;
+  if (groups > 0 && (!slot_of_row || !parents)) return SIP_ERR_INVALID_ARG;
+  if (width > SIP_MAX_BEAMS || (int64_t)groups * width > SIP_MAX_B) return SIP_ERR_UNSUPPORTED;
+  if (!workspace_ok(state, state_bytes, sip::state_total(slots, L_max))) return SIP_ERR_WORKSPACE;
+  if (groups == 0) return SIP_OK;
+  const sip::StateView v = sip::state_view(state, slots, L_max);
+  sip::ReorderArgs a{};
+  a.head = v.head; a.len = v.len; a.ndist = v.ndist; a.tokens = v.tokens; a.table = v.table;
+  a.slots = slots; a.L_max = L_max; a.groups = groups; a.width = width;
+  a.slot_of_row = slot_of_row; a.parents = parents; a.new_tokens = tokens;
+  a.token_blocks = tiles(L_max, sip::kReorderThreads * 4);
+  hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+  const dim3 grid((unsigned)groups * (unsigned)(a.token_blocks + 8)), threads(sip::kReorderThreads);
+  if (width <= 8) hipLaunchKernelGGL(sip::state_reorder_kernel<8>, grid, threads, 0, stream, a);
+  else if (width <= 32) hipLaunchKernelGGL(sip::state_reorder_kernel<32>, grid, threads, 0, stream, a);
+  else hipLaunchKernelGGL(sip::state_reorder_kernel<64>, grid, threads, 0, stream, a);
+  hipLaunchKernelGGL(sip::state_reorder_append_kernel, dim3(groups), dim3(64), 0, stream, a);
+  return launched();
+}
+
+}  // extern "C"

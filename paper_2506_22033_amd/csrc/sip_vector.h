@@ -1,0 +1,187 @@
+// Host side of the entry points of include/sip_head.h on the way from tokens to vectors, and of the adapters: argument checks,
+// workspace carving, launches.
+#pragma once
+#include <algorithm>
+
+#include "../../include/sip_head.h"
+#include "sip_adapt.h"
+#include "sip_embed.h"
+#include "sip_host.h"
+
+namespace {
+
+bool matrix_shape_ok(int32_t V, int32_t D) { return V > 0 && D > 0 && D % 8 == 0 && V <= SIP_MAX_V && D <= SIP_MAX_D; }
+
+sip_status embed_check(int32_t V, int32_t D, const int32_t* ids, int32_t N, const void* out, int64_t out_stride, sip_dtype out_dtype) {
+  if (V <= 0 || D <= 0 || D % 8 != 0 || N < 0 || !dtype_ok(out_dtype)) return SIP_ERR_INVALID_ARG;
+  if (N > 0 && (!ids || !rows_ok(out, D, out_stride, out_dtype))) return SIP_ERR_INVALID_ARG;
+  if (V > SIP_MAX_V || D > SIP_MAX_D || N > SIP_MAX_B || out_stride > (1ll << 32)) return SIP_ERR_UNSUPPORTED;
+  return SIP_OK;
+}
+sip::EmbedArgs embed_args(int32_t V, int32_t D, const int32_t* ids, int32_t N, float scale, void* out, int64_t out_stride,
+                          sip_dtype out_dtype) {
+  sip::EmbedArgs a{};
+  a.V = V; a.D = D; a.N = N; a.ids = ids; a.scale = scale;
+  a.out = out; a.out_stride = out_stride; a.out_bf16 = out_dtype == SIP_BF16;
+  return a;
+}
+dim3 embed_grid(int32_t N, int32_t D) { return dim3(std::min<long long>(tiles((long long)N * (D / 8), 256), 1 << 20)); }
+
+// Entries of a piece of the sorted tokens: 4 to 32, as many as leave every SIMD two waves.
+constexpr long long kEmbedLanes = kChip * 4 * 64 * 2;
+int embed_piece(int32_t N, int32_t D) {
+  int piece = 4;
+  while (piece < 32 && (long long)N * (D / 8) >= 2 * piece * kEmbedLanes) piece *= 2;
+  return piece;
+}
+// The most pieces of N tokens or fewer.
+int embed_pieces_most(int32_t N, int32_t D) {
+  int most = tiles(N, embed_piece(N, D));
+  for (int piece = 4; piece < embed_piece(N, D); piece *= 2)
+    most = std::max(most, tiles((2 * piece * kEmbedLanes - 1) / (D / 8), piece));
+  return most;
+}
+struct EmbedPlan { int piece, pieces; size_t live, key[2], pos[2], part, bytes; };
+EmbedPlan embed_plan(int32_t N, int32_t D) {       // (of N tokens or fewer, but for `piece` and `pieces`)
+  EmbedPlan p{};
+  size_t at = 0;
+  auto take = [&](size_t n) { const size_t here = at; at += head_align(n); return here; };
+  p.live = take(4);
+  for (int i = 0; i < 2; ++i) { p.key[i] = take((size_t)N * 4); p.pos[i] = take((size_t)N * 4); }
+  p.piece = embed_piece(N, D);
+  p.pieces = tiles(N, p.piece);
+  p.part = take((size_t)embed_pieces_most(N, D) * 2 * D * 4);
+  p.bytes = at;
+  return p;
+}
+
+struct AdaptPlan { size_t count, rows, batch, t, bytes; };
+AdaptPlan adapt_plan(int32_t B, int32_t rank) {
+  AdaptPlan p{};
+  size_t at = 0;
+  auto take = [&](size_t n) { const size_t here = at; at += head_align(n); return here; };
+  p.count = take(4);
+  p.rows = take((size_t)B * 4);
+  p.batch = take((size_t)B * 8);
+  p.t = take((size_t)B * rank * 4);
+  p.bytes = at;
+  return p;
+}
+bool adapt_shape_ok(int32_t B, int32_t adapters, int32_t rank, int32_t D) {
+  return B > 0 && adapters > 0 && rank > 0 && rank % 8 == 0 && D > 0 && D % 8 == 0 && B <= SIP_MAX_TOKENS && adapters <= SIP_MAX_ADAPTERS &&
+         rank <= SIP_MAX_RANK && D <= SIP_MAX_D;
+}
+
+}  // namespace
+
+extern "C" {
+
+sip_status sip_embed(const void* weight, sip_dtype weight_dtype, int32_t V, int32_t D, int64_t weight_stride, const int32_t* ids,
+                     int32_t N, float scale, void* out, int64_t out_stride, sip_dtype out_dtype, void* hip_stream) {
+  if (!dtype_ok(weight_dtype) || !rows_ok(weight, D, weight_stride, weight_dtype)) return SIP_ERR_INVALID_ARG;
+  const sip_status ok = embed_check(V, D, ids, N, out, out_stride, out_dtype);
+  if (ok != SIP_OK) return ok;
+  if (weight_stride > (1ll << 32)) return SIP_ERR_UNSUPPORTED;
+  if (N == 0) return SIP_OK;
+  sip::EmbedArgs a = embed_args(V, D, ids, N, scale, out, out_stride, out_dtype);
+  a.weight = weight; a.weight_stride = weight_stride; a.weight_bf16 = weight_dtype == SIP_BF16;
+  hipLaunchKernelGGL(sip::embed_kernel<false>, embed_grid(N, D), dim3(256), 0, static_cast<hipStream_t>(hip_stream), a);
+  return launched();
+}
+
+sip_status sip_embed_codes(const uint8_t* codes, int64_t codes_stride, const void* scales, sip_dtype scales_dtype,
+                           const uint8_t* zeros, int32_t group, int32_t V, int32_t D, const int32_t* ids, int32_t N, float scale,
+                           void* out, int64_t out_stride, sip_dtype out_dtype, void* hip_stream) {
+  if (!codes || !scales || !dtype_ok(scales_dtype) || V <= 0 || D <= 0) return SIP_ERR_INVALID_ARG;
+  if (group != 32 && group != 64 && group != 128) return group > 0 ? SIP_ERR_UNSUPPORTED : SIP_ERR_INVALID_ARG;
+  if (D % group != 0 || codes_stride < D / 2 || codes_stride % 16 != 0 || !aligned16(codes)) return SIP_ERR_INVALID_ARG;
+  if (reinterpret_cast<uintptr_t>(scales) % dtype_bytes(scales_dtype) != 0) return SIP_ERR_INVALID_ARG;
+  const sip_status ok = embed_check(V, D, ids, N, out, out_stride, out_dtype);
+  if (ok != SIP_OK) return ok;
+  if (codes_stride > (1ll << 32)) return SIP_ERR_UNSUPPORTED;
+  if (N == 0) return SIP_OK;
+  sip::EmbedArgs a = embed_args(V, D, ids, N, scale, out, out_stride, out_dtype);
+  a.codes = codes; a.codes_stride = codes_stride; a.scales = scales; a.scales_bf16 = scales_dtype == SIP_BF16;
+  a.zeros = zeros; a.group = group;
+  hipLaunchKernelGGL(sip::embed_kernel<true>, embed_grid(N, D), dim3(256), 0, static_cast<hipStream_t>(hip_stream), a);
+  return launched();
+}
+
+size_t sip_embed_workspace_bytes(int32_t N, int32_t V, int32_t D) {
+  if (!matrix_shape_ok(V, D) || N < 0 || N > SIP_MAX_TOKENS) return 0;
+  return embed_plan(std::max(N, 1), D).bytes;
+}
+
+sip_status sip_embed_backward(const void* grad_out, int64_t grad_out_stride, sip_dtype grad_out_dtype, const int32_t* ids, int32_t N,
+                              int32_t V, int32_t D, float scale, int32_t accumulate, void* grad_weight,
+                              int64_t grad_weight_stride, sip_dtype grad_weight_dtype, void* workspace, size_t workspace_bytes,
+                              void* hip_stream) {
+  if (V <= 0 || D <= 0 || D % 8 != 0 || N < 0 || !dtype_ok(grad_out_dtype) || !dtype_ok(grad_weight_dtype)) return SIP_ERR_INVALID_ARG;
+  if (N > 0 && (!ids || !rows_ok(grad_out, D, grad_out_stride, grad_out_dtype))) return SIP_ERR_INVALID_ARG;
+  if (!rows_ok(grad_weight, D, grad_weight_stride, grad_weight_dtype)) return SIP_ERR_INVALID_ARG;
+  if (!matrix_shape_ok(V, D) || N > SIP_MAX_TOKENS || grad_out_stride > (1ll << 32) || grad_weight_stride > (1ll << 32))
+    return SIP_ERR_UNSUPPORTED;
+  if (!workspace_ok(workspace, workspace_bytes, sip_embed_workspace_bytes(N, V, D))) return SIP_ERR_WORKSPACE;
+  if (N == 0 && accumulate) return SIP_OK;
+  const EmbedPlan pl = embed_plan(std::max(N, 1), D);
+  char* ws = static_cast<char*>(workspace);
+  sip::EmbedGradArgs a{};
+  a.grad = grad_out; a.grad_stride = grad_out_stride; a.grad_bf16 = grad_out_dtype == SIP_BF16;
+  a.ids = ids; a.N = N; a.V = V; a.D = D; a.scale = scale; a.accumulate = accumulate != 0;
+  a.out = grad_weight; a.out_stride = grad_weight_stride; a.out_bf16 = grad_weight_dtype == SIP_BF16;
+  a.piece = pl.piece;
+  a.live = reinterpret_cast<int*>(ws + pl.live);
+  for (int i = 0; i < 2; ++i) {
+    a.key[i] = reinterpret_cast<uint32_t*>(ws + pl.key[i]);
+    a.pos[i] = reinterpret_cast<uint32_t*>(ws + pl.pos[i]);
+  }
+  a.part = reinterpret_cast<float*>(ws + pl.part);
+  hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+  const int fill = accumulate ? 0 : (int)std::min<long long>(tiles((long long)V * (D / 8), sip::kSortThreads), 2 * kChip);
+  hipLaunchKernelGGL(sip::embed_sort_kernel, dim3(1 + fill), dim3(sip::kSortThreads), 0, stream, a);
+  if (N > 0) {
+    const dim3 grid(tiles((long long)pl.pieces * (D / 8), 256));
+    if (a.grad_bf16) hipLaunchKernelGGL(sip::embed_sum_kernel<true>, grid, dim3(256), 0, stream, a);
+    else hipLaunchKernelGGL(sip::embed_sum_kernel<false>, grid, dim3(256), 0, stream, a);
+    hipLaunchKernelGGL(sip::embed_join_kernel, dim3(pl.pieces, tiles(D, 128)), dim3(256), 0, stream, a);
+  }
+  return launched();
+}
+
+size_t sip_head_adapt_workspace_bytes(int32_t B, int32_t adapters, int32_t rank, int32_t D) {
+  return adapt_shape_ok(B, adapters, rank, D) ? adapt_plan(B, rank).bytes : 0;
+}
+
+sip_status sip_head_adapt(const void* hidden, int32_t B, int32_t D, int64_t hidden_stride, sip_dtype hidden_dtype,
+                          const void* down, const void* up, int32_t adapters, int32_t rank, const int32_t* adapter_of_row,
+                          const float* scales, int32_t V, void* logits, int64_t logits_stride, sip_dtype logits_dtype,
+                          void* workspace, size_t workspace_bytes, void* hip_stream) {
+  if (B <= 0 || D <= 0 || D % 8 != 0 || V <= 0 || adapters <= 0 || rank <= 0 || rank % 8 != 0 || !dtype_ok(hidden_dtype) ||
+      !dtype_ok(logits_dtype))
+    return SIP_ERR_INVALID_ARG;
+  if (!rows_ok(hidden, D, hidden_stride, hidden_dtype) || !down || !up || !aligned16(down) || !aligned16(up) || !adapter_of_row)
+    return SIP_ERR_INVALID_ARG;
+  if (!logits || logits_stride < V || reinterpret_cast<uintptr_t>(logits) % dtype_bytes(logits_dtype) != 0) return SIP_ERR_INVALID_ARG;
+  if (!adapt_shape_ok(B, adapters, rank, D) || V > SIP_MAX_V || hidden_stride > (1ll << 32) || logits_stride > (1ll << 32))
+    return SIP_ERR_UNSUPPORTED;
+  const AdaptPlan pl = adapt_plan(B, rank);
+  if (!workspace_ok(workspace, workspace_bytes, pl.bytes)) return SIP_ERR_WORKSPACE;
+  char* ws = static_cast<char*>(workspace);
+  sip::AdaptArgs a{};
+  a.hidden = hidden; a.hidden_stride = hidden_stride; a.hidden_bf16 = hidden_dtype == SIP_BF16;
+  a.B = B; a.D = D; a.V = V; a.rank = rank; a.adapters = adapters;
+  a.down = static_cast<const uint16_t*>(down); a.up = static_cast<const uint16_t*>(up);
+  a.adapter_of_row = adapter_of_row; a.scales = scales;
+  a.logits = logits; a.logits_stride = logits_stride; a.logits_bf16 = logits_dtype == SIP_BF16;
+  a.count = reinterpret_cast<int*>(ws + pl.count);
+  a.rows = reinterpret_cast<int*>(ws + pl.rows);
+  a.batch = reinterpret_cast<int2*>(ws + pl.batch);
+  a.t = reinterpret_cast<float*>(ws + pl.t);
+  hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+  hipLaunchKernelGGL(sip::adapt_rows_kernel, dim3(1), dim3(1024), 0, stream, a);
+  hipLaunchKernelGGL(sip::adapt_down_kernel, dim3(B, rank / 8), dim3(256), 0, stream, a);
+  hipLaunchKernelGGL(sip::adapt_up_kernel, dim3(tiles(V, 256), std::min(B, 4096)), dim3(256), 0, stream, a);
+  return launched();
+}
+
+}  // extern "C"

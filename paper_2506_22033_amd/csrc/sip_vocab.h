@@ -6,15 +6,10 @@
 #include "../../include/sip_head.h"
 #include "sip_clip.h"
 #include "sip_codes.h"
+#include "sip_host.h"
 #include "sip_xent.h"
 
 namespace {
-
-inline size_t head_align(size_t x) { return (x + 255) / 256 * 256; }
-inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-inline bool workspace_ok(const void* p, size_t have, size_t need) {
-  return p && (reinterpret_cast<uintptr_t>(p) & 255u) == 0 && have >= need;
-}
 
 // Tiles of the cross entropy's products.
 typedef sip::GemmShape<256, 256, 128, 64, 3, 2> Wide;
@@ -24,9 +19,6 @@ typedef sip::GemmShape<128, 128, 64, 64, 2, 2> Small;
 typedef sip::GemmShape<64, 32, 16, 32, 4, 4> Tiny;
 enum XentShape { kWide, kQuarter, kNarrow, kSmall, kTiny };
 constexpr int kShapeA[] = {256, 256, 128, 128, 64}, kShapeB[] = {256, 64, 32, 128, 32}, kShapeWaveA[] = {128, 64, 32, 64, 16};
-
-inline int tiles(long long n, int tile) { return (int)((n + tile - 1) / tile); }
-constexpr int kChip = 256;                             // workgroups of a compute unit each
 
 // What a product of a x b with sums over k, dealt out in `parts`, is expected to take in us, from products of one round (a unit of 64 k, one
 // workgroup on its compute unit; each further one at once; how many LDS has room for) and of many rounds of one unit (a
@@ -207,8 +199,6 @@ sip::XentArgs xent_args(const void* hidden, int32_t N, int32_t D, int64_t hidden
   a.weight_parts = pl.weight_parts; a.weight_parts.sum = reinterpret_cast<float*>(ws + pl.weight_sum);
   return a;
 }
-
-inline sip_status launched() { return hipGetLastError() == hipSuccess ? SIP_OK : SIP_ERR_HIP; }
 
 template <int N> using Int = std::integral_constant<int, N>;
 

@@ -17,6 +17,8 @@ from .binding import SIP_BF16, SIP_F32, SIP_OK, SipError, _empty, _nbytes, _on, 
 SIP_MAX_D = 16384
 SIP_MAX_TOKENS = 65536
 SIP_MAX_TENSORS = 65536
+SIP_MAX_RANK = 128
+SIP_MAX_ADAPTERS = 4096
 
 _DTYPES = {torch.float32: SIP_F32, torch.bfloat16: SIP_BF16}
 _p, _i, _l, _f, _z = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_float, ctypes.c_size_t
@@ -37,6 +39,12 @@ _SIGNATURES = {
     "sip_head_workspace_bytes": (_z, [_i, _i, _i, _i]),
     "sip_head_logits": (ctypes.c_int, [_p, _i, _i, _l, ctypes.c_int, _p, _l, _p, ctypes.c_int, _p, _i, _i, _p, _l,
                                        ctypes.c_int, _p, _z, _p]),
+    "sip_head_adapt_workspace_bytes": (_z, [_i, _i, _i, _i]),
+    "sip_head_adapt": (ctypes.c_int, [_p, _i, _i, _l, ctypes.c_int, _p, _p, _i, _i, _p, _p, _i, _p, _l, ctypes.c_int, _p, _z, _p]),
+    "sip_embed": (ctypes.c_int, [_p, ctypes.c_int, _i, _i, _l, _p, _i, _f, _p, _l, ctypes.c_int, _p]),
+    "sip_embed_codes": (ctypes.c_int, [_p, _l, _p, ctypes.c_int, _p, _i, _i, _i, _p, _i, _f, _p, _l, ctypes.c_int, _p]),
+    "sip_embed_workspace_bytes": (_z, [_i, _i, _i]),
+    "sip_embed_backward": (ctypes.c_int, [_p, _l, ctypes.c_int, _p, _i, _i, _i, _f, _i, _p, _l, ctypes.c_int, _p, _z, _p]),
 }
 _ready = None
 
@@ -276,3 +284,102 @@ def sip_head_logits(hidden: torch.Tensor, codes: torch.Tensor, scales: torch.Ten
           _stride(codes), _ptr(scales), _DTYPES[scales.dtype], _ptr(zeros), group, V, _ptr(out), _stride(out),
           _DTYPES[out.dtype], _ptr(ws), _nbytes(ws))
     return out
+
+
+# ---- low-rank adapters
+
+def sip_head_adapt_workspace_bytes(B: int, adapters: int, rank: int, D: int) -> int:
+    return int(_load().sip_head_adapt_workspace_bytes(B, adapters, rank, D))
+
+
+def _stack(t: torch.Tensor, name: str, shape) -> torch.Tensor:
+    if not t.is_cuda or t.dtype != torch.bfloat16 or t.dim() != 3 or not t.is_contiguous() or tuple(t.shape) != shape:
+        raise TypeError(f"{name} must be a contiguous device tensor {shape} of bfloat16")
+    return t
+
+
+def sip_head_adapt(logits: torch.Tensor, hidden: torch.Tensor, down: torch.Tensor, up: torch.Tensor, adapter_of_row: torch.Tensor,
+                   scales: Optional[torch.Tensor] = None, *, workspace: Optional[torch.Tensor] = None,
+                   stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """Adds ``scales[a] * up[a] @ (down[a] @ hidden[b])`` to ``logits`` [B, V] (float32 or bfloat16, in place), ``a`` being
+    ``adapter_of_row[b]`` (int32; outside [0, adapters): the row stays as it is).  ``hidden`` [B, D] is bf16 or fp32, ``down`` [adapters,
+    rank, D] and ``up`` [adapters, V, rank] are bf16, ``scales`` [adapters] fp32 (None: 1)."""
+    lib = _load()
+    _matrix(logits, "logits", (torch.bfloat16, torch.float32))
+    _matrix(hidden, "hidden", (torch.bfloat16, torch.float32))
+    (B, V), D, dev = logits.shape, hidden.shape[1], logits.device
+    if hidden.shape[0] != B:
+        raise TypeError(f"logits [B, V] and hidden [B, D] differ in B: {B} and {hidden.shape[0]}")
+    adapters, rank = down.shape[:2] if down.dim() == 3 else (0, 0)
+    _stack(down, "down", (adapters, rank, D))
+    _stack(up, "up", (adapters, V, rank))
+    _vector(adapter_of_row, "adapter_of_row", torch.int32, B)
+    if scales is not None:
+        _vector(scales, "scales", torch.float32, adapters)
+    _same_device(dev, hidden, down, up, adapter_of_row, scales)
+    if B == 0:
+        return logits
+    ws = _scratch(workspace, 0 if workspace is not None else lib.sip_head_adapt_workspace_bytes(B, adapters, rank, D), dev, stream)
+    _call("sip_head_adapt", dev, stream, _ptr(hidden), B, D, _stride(hidden), _DTYPES[hidden.dtype], _ptr(down), _ptr(up), adapters,
+          rank, _ptr(adapter_of_row), _ptr(scales), V, _ptr(logits), _stride(logits), _DTYPES[logits.dtype], _ptr(ws), _nbytes(ws))
+    return logits
+
+
+# ---- embedding
+
+def _ids(ids: torch.Tensor) -> int:
+    _vector(ids, "ids", torch.int32, ids.numel())
+    return ids.numel()
+
+
+def sip_embed(weight: torch.Tensor, ids: torch.Tensor, scale: float = 1.0, *, out: Optional[torch.Tensor] = None,
+              dtype: Optional[torch.dtype] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """[N, D]: ``scale`` times the rows of ``weight`` [V, D] (bf16 or fp32) that ``ids`` [N] (int32) name, zeros for a token outside
+    [0, V).  Without ``out`` in ``dtype``, by default that of ``weight``."""
+    _matrix(weight, "weight", (torch.bfloat16, torch.float32))
+    (V, D), N, dev = weight.shape, _ids(ids), weight.device
+    out = _empty(stream, N, D, dtype=weight.dtype if dtype is None else dtype, device=dev) if out is None else out
+    _matrix(out, "out", (torch.bfloat16, torch.float32), (N, D))
+    _same_device(dev, ids, out)
+    _call("sip_embed", dev, stream, _ptr(weight), _DTYPES[weight.dtype], V, D, _stride(weight), _ptr(ids), N, scale, _ptr(out),
+          _stride(out), _DTYPES[out.dtype])
+    return out
+
+
+def sip_embed_codes(codes: torch.Tensor, scales: torch.Tensor, zeros: Optional[torch.Tensor], ids: torch.Tensor, scale: float = 1.0,
+                    *, out: Optional[torch.Tensor] = None, dtype: torch.dtype = torch.bfloat16,
+                    stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """sip_embed() from a matrix of 4-bit codes, as sip_head_quantize() makes it."""
+    V, D, group = _codes_operands(codes, scales, zeros)
+    N, dev = _ids(ids), codes.device
+    out = _empty(stream, N, D, dtype=dtype, device=dev) if out is None else out
+    _matrix(out, "out", (torch.bfloat16, torch.float32), (N, D))
+    _same_device(dev, scales, zeros, ids, out)
+    _call("sip_embed_codes", dev, stream, _ptr(codes), _stride(codes), _ptr(scales), _DTYPES[scales.dtype], _ptr(zeros), group, V, D,
+          _ptr(ids), N, scale, _ptr(out), _stride(out), _DTYPES[out.dtype])
+    return out
+
+
+def sip_embed_workspace_bytes(N: int, V: int, D: int) -> int:
+    return int(_load().sip_embed_workspace_bytes(N, V, D))
+
+
+def sip_embed_backward(grad_out: torch.Tensor, ids: torch.Tensor, V: int, scale: float = 1.0, *,
+                       grad_weight: Optional[torch.Tensor] = None, accumulate: bool = False, dtype: torch.dtype = torch.bfloat16,
+                       workspace: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """grad_weight [V, D]: row v is ``scale`` times the sum of the rows of ``grad_out`` [N, D] (bf16 or fp32) whose token in ``ids``
+    [N] (int32) is v, added to what ``grad_weight`` holds if ``accumulate``.  Tokens outside [0, V) take no part."""
+    lib = _load()
+    _matrix(grad_out, "grad_out", (torch.bfloat16, torch.float32))
+    (N, D), dev = grad_out.shape, grad_out.device
+    _vector(ids, "ids", torch.int32, N)
+    if grad_weight is None:
+        if accumulate:
+            raise TypeError("accumulate needs a grad_weight to add to")
+        grad_weight = _empty(stream, V, D, dtype=dtype, device=dev)
+    _matrix(grad_weight, "grad_weight", (torch.bfloat16, torch.float32), (V, D))
+    _same_device(dev, ids, grad_weight)
+    ws = _scratch(workspace, 0 if workspace is not None else lib.sip_embed_workspace_bytes(N, V, D), dev, stream)
+    _call("sip_embed_backward", dev, stream, _ptr(grad_out), _stride(grad_out), _DTYPES[grad_out.dtype], _ptr(ids), N, V, D, scale,
+          int(accumulate), _ptr(grad_weight), _stride(grad_weight), _DTYPES[grad_weight.dtype], _ptr(ws), _nbytes(ws))
+    return grad_weight
