@@ -8,10 +8,13 @@
 
 namespace sip {
 
-constexpr int kAdaptRows = 16;                           // rows of one adapter that a workgroup serves at once
+// Rows that share an adapter are served sixteen at a time, a batch: the sixteen columns of a matrix instruction, whose rows are an
+// adapter's.  Both products read their adapter from memory straight into the instruction's registers.
+constexpr int kAdaptRows = 16;
+constexpr int kAdaptDirect = 64;                         // up to so many rows a wave finds its batch by itself
 
 struct AdaptArgs {
-  const void* hidden; long long hidden_stride; int hidden_bf16;
+  const void* hidden; long long hidden_stride;
   int B, D, V, rank, adapters;
   const uint16_t* down; const uint16_t* up;
   const int* adapter_of_row; const float* scales;
@@ -19,11 +22,11 @@ struct AdaptArgs {
   // workspace
   int* count;                                            // batches
   int* rows;                                             // [B] rows that have an adapter, by adapter
-  int2* batch;                                           // [B] first of a batch in `rows` and its size; the adapter is that of its rows
-  float* t;                                              // [B][rank] scales[a] * down[a] hidden[b]
+  int4* batch;                                           // [B] first of a batch in `rows`, its size, its adapter
+  float* t;                                              // [batches][16][rank] scales[a] * down[a] hidden[b]
 };
 
-// One workgroup lists the rows by adapter, in batches of up to kAdaptRows.  (The order of an adapter's rows changes no result.)
+// One workgroup lists the rows by adapter, in batches.  (The order of an adapter's rows changes no result.)
 __global__ __launch_bounds__(1024) void adapt_rows_kernel(AdaptArgs p) {
   __shared__ int first[SIP_MAX_ADAPTERS], wave_n[16], wave_m[16];
   const int t = threadIdx.x, lane = t & 63, w = t >> 6, A = p.adapters;
@@ -50,7 +53,7 @@ __global__ __launch_bounds__(1024) void adapt_rows_kernel(AdaptArgs p) {
     }
     if (i < A) {
       first[i] = bn;
-      for (int j = 0; j < m; ++j) p.batch[bm + j] = make_int2(bn + j * kAdaptRows, min(kAdaptRows, n - j * kAdaptRows));
+      for (int j = 0; j < m; ++j) p.batch[bm + j] = make_int4(bn + j * kAdaptRows, min(kAdaptRows, n - j * kAdaptRows), i, 0);
     }
     __syncthreads();
   }
@@ -59,51 +62,159 @@ __global__ __launch_bounds__(1024) void adapt_rows_kernel(AdaptArgs p) {
   if (t == 0) *p.count = batches;
 }
 
-// t of one row, eight of its entries a workgroup: two a wave.
-__global__ __launch_bounds__(256) void adapt_down_kernel(AdaptArgs p) {
-  const int b = blockIdx.x, lane = threadIdx.x & 63, w = threadIdx.x >> 6, adapter = p.adapter_of_row[b];
-  if ((unsigned)adapter >= (unsigned)p.adapters) return;
-  const float scale = p.scales ? p.scales[adapter] : 1.0f;
-  for (int j = blockIdx.y * 8 + w * 2; j < blockIdx.y * 8 + w * 2 + 2; ++j) {
-    float s = 0.0f;
-    for (int c = lane * 8; c < p.D; c += 512) {
-      const f32x8 x = as_floats(load_eight(p.hidden, b * p.hidden_stride + c, p.hidden_bf16), p.hidden_bf16);
-      const f32x8 y = as_floats(load_eight(p.down, ((long long)adapter * p.rank + j) * p.D + c, true), true);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) s += x[e] * y[e];
-    }
-    for (int d = 32; d; d >>= 1) s += __shfl_xor(s, d);
-    if (lane == 0) p.t[(long long)b * p.rank + j] = s * scale;
+// A batch as a wave sees it: its size (0: there is none), its adapter, and the row of column lane % 16 (-1: none).
+struct Batch { int n, adapter, row; };
+template <bool DIRECT>
+__device__ inline Batch batch_of(const AdaptArgs& p, int i) {
+  const int lane = threadIdx.x & 63;
+  Batch x = {0, 0, -1};
+  if constexpr (DIRECT) {
+    // Lane b is row b; its place among its adapter's rows.  Every sixteenth leads a batch; the i-th leader's is the one.
+    int a = lane < p.B ? p.adapter_of_row[lane] : -1, place = 0;
+    if ((unsigned)a >= (unsigned)p.adapters) a = -1;
+    for (int j = 0; j < p.B; ++j) place += j < lane && __builtin_amdgcn_readlane(a, j) == a;
+    unsigned long long leaders = __ballot(a >= 0 && place % kAdaptRows == 0);
+    for (int j = 0; j < i; ++j) leaders &= leaders - 1;
+    if (!leaders) return x;
+    const int leader = __builtin_ctzll(leaders), from = __builtin_amdgcn_readlane(place, leader);
+    x.adapter = __builtin_amdgcn_readlane(a, leader);
+    unsigned long long mine = __ballot(a == x.adapter && place >= from && place < from + kAdaptRows);
+    x.n = __popcll(mine);
+    for (int j = 0; j < (lane & 15); ++j) mine &= mine - 1;
+    if ((lane & 15) < x.n) x.row = __builtin_ctzll(mine);
+  } else {
+    const int4 b = p.batch[i];                           // (read whether there is one or not)
+    if (i >= *p.count) return x;
+    x.n = b.y;
+    x.adapter = b.z;
+    if ((lane & 15) < x.n) x.row = p.rows[b.x + (lane & 15)];
   }
+  return x;
 }
 
-// A lane: one vocabulary entry of one batch's rows.
-__global__ __launch_bounds__(256) void adapt_up_kernel(AdaptArgs p) {
-  const int v = blockIdx.x * 256 + threadIdx.x;
-  for (int i = blockIdx.y; i < *p.count; i += gridDim.y) {
-    const int2 batch = p.batch[i];
-    const int adapter = p.adapter_of_row[p.rows[batch.x]];
-    if (v >= p.V) continue;
-    float sum[kAdaptRows] = {};
-    for (int j = 0; j < p.rank; j += 8) {
-      const f32x8 u = as_floats(load_eight(p.up, ((long long)adapter * p.V + v) * p.rank + j, true), true);
+// Eight floats as the sum of three bf16 each, which hold all their bits.
+struct Split { bf16x8 part[3]; };
+__device__ inline Split split_of(f32x8 x) {
+  Split s;
 #pragma unroll
-      for (int r = 0; r < kAdaptRows; ++r) {
-        if (r >= batch.y) break;
-        const float* t = p.t + (long long)p.rows[batch.x + r] * p.rank + j;
+  for (int i = 0; i < 3; ++i)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) sum[r] = __builtin_fmaf(u[e], t[e], sum[r]);
+    for (int e = 0; e < 8; ++e) {
+      const __bf16 b = (__bf16)x[e];
+      s.part[i][e] = b;
+      x[e] -= (float)b;
+    }
+  return s;
+}
+
+// t of a batch, sixteen entries a workgroup: its waves share the sum over D and join their parts in order.
+constexpr int kDownWaves = 16;
+template <bool BF16, bool DIRECT>
+__global__ __launch_bounds__(kDownWaves * 64) void adapt_down_kernel(AdaptArgs p) {
+  __shared__ __align__(16) f32x4 sums[kDownWaves][64];
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, k = 8 * (lane >> 4);
+  const Batch x = batch_of<DIRECT>(p, blockIdx.x);
+  if (x.n == 0) return;
+  const int j = blockIdx.y * 16 + (lane & 15);
+  const uint16_t* down = p.down + ((long long)x.adapter * p.rank + j) * p.D;
+  const bool live = j < p.rank;
+  const float scale = p.scales ? p.scales[x.adapter] : 1.0f;
+  f32x4 acc = {0, 0, 0, 0};
+  const bf16x8 none = {};
+  constexpr int kAhead = BF16 ? 8 : 4;                   // steps whose loads are under way at once
+  for (int c0 = w * 32; c0 < p.D; c0 += kAhead * kDownWaves * 32) {
+    bf16x8 a[kAhead];
+    Eight h[kAhead];
+#pragma unroll
+    for (int s = 0; s < kAhead; ++s) {
+      const int c = c0 + s * kDownWaves * 32 + k;
+      a[s] = live && c < p.D ? *reinterpret_cast<const bf16x8*>(down + c) : none;
+      h[s] = Eight{};
+      if (x.row >= 0 && c < p.D) h[s] = load_eight(p.hidden, x.row * p.hidden_stride + c, BF16);
+    }
+#pragma unroll
+    for (int s = 0; s < kAhead; ++s) {
+      if constexpr (BF16) {
+        acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[s], __builtin_bit_cast(bf16x8, h[s].w[0]), acc, 0, 0, 0);
+      } else {
+        const Split b = split_of(as_floats(h[s], false));
+#pragma unroll
+        for (int i = 2; i >= 0; --i) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[s], b.part[i], acc, 0, 0, 0);
+      }
+    }
+  }
+  sums[w][lane] = acc;
+  __syncthreads();
+  if (w > 0) return;
+  for (int i = 1; i < kDownWaves; ++i) acc += sums[i][lane];
+  const int j0 = blockIdx.y * 16 + acc_a(lane);
+  if (x.row < 0 || j0 >= p.rank) return;
+  *reinterpret_cast<f32x4*>(p.t + ((long long)blockIdx.x * kAdaptRows + (lane & 15)) * p.rank + j0) = acc * scale;
+}
+
+// The additions of one batch to `tiles` of kUpWaves * 16 logits each.  A wave's share of a tile is sixteen entries of the vocabulary, of
+// which a lane has four neighbours of one row.  VECTOR: logits are fp32 in rows that start at 16 bytes.
+constexpr int kUpWaves = 4, kUpEntries = kUpWaves * 16;
+template <int STEPS, bool DIRECT, bool VECTOR>
+__global__ __launch_bounds__(kUpWaves * 64) void adapt_up_kernel(AdaptArgs p, int batches, int tiles) {
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, k = 8 * (lane >> 4);
+  // batches of one adapter go through the same entries one after the other on one XCD, whose L2 then has them
+  const int local = blockIdx.x >> 3, i = local % batches, v0 = ((local / batches) * 8 + (blockIdx.x & 7)) * tiles * kUpEntries;
+  if (v0 >= p.V) return;
+  const Batch x = batch_of<DIRECT>(p, i);
+  if (x.n == 0) return;
+  Split t[STEPS];
+#pragma unroll
+  for (int s = 0; s < STEPS; ++s) {
+    f32x8 f = {0, 0, 0, 0, 0, 0, 0, 0};
+    if (x.row >= 0 && 32 * s + k < p.rank)
+      f = as_floats(load_eight(p.t, ((long long)i * kAdaptRows + (lane & 15)) * p.rank + 32 * s + k, false), false);
+    t[s] = split_of(f);
+  }
+  const uint16_t* up = p.up + (long long)x.adapter * p.V * p.rank;
+  const bf16x8 none = {};
+  constexpr int kAhead = STEPS > 2 ? 2 : 4;              // tiles whose loads are under way at once
+  for (int tile0 = 0; tile0 < tiles; tile0 += kAhead) {
+    bf16x8 a[kAhead][STEPS];
+    f32x4 z[kAhead];
+    auto at_of = [&](int j) { return v0 + ((tile0 + j) * kUpWaves + w) * 16; };          // a tile's first entry; V: there is none
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      const int v = tile0 + j < tiles ? at_of(j) : p.V, entry = v + (lane & 15), at = v + acc_a(lane);
+#pragma unroll
+      for (int s = 0; s < STEPS; ++s)
+        a[j][s] = entry < p.V && 32 * s + k < p.rank ? *reinterpret_cast<const bf16x8*>(up + (long long)entry * p.rank + 32 * s + k) : none;
+      z[j] = f32x4{0, 0, 0, 0};
+      if (x.row < 0 || at >= p.V) continue;
+      const long long z0 = x.row * p.logits_stride + at;
+      if (VECTOR && at + 4 <= p.V) {
+        z[j] = *reinterpret_cast<const f32x4*>(static_cast<const float*>(p.logits) + z0);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (at + e < p.V) z[j][e] = p.logits_bf16 ? (float)static_cast<const __bf16*>(p.logits)[z0 + e] : static_cast<const float*>(p.logits)[z0 + e];
       }
     }
 #pragma unroll
-    for (int r = 0; r < kAdaptRows; ++r) {
-      if (r >= batch.y) break;
-      const long long at = p.rows[batch.x + r] * p.logits_stride + v;
-      if (p.logits_bf16) {
-        __bf16* z = static_cast<__bf16*>(p.logits) + at;
-        *z = (__bf16)((float)*z + sum[r]);
+    for (int j = 0; j < kAhead; ++j) {
+      const int at = (tile0 + j < tiles ? at_of(j) : p.V) + acc_a(lane);
+      f32x4 acc = {0, 0, 0, 0};
+#pragma unroll
+      for (int part = 2; part >= 0; --part)
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[j][s], t[s].part[part], acc, 0, 0, 0);
+      acc += z[j];
+      if (x.row < 0 || at >= p.V) continue;
+      const long long z0 = x.row * p.logits_stride + at;
+      if (VECTOR && at + 4 <= p.V) {
+        *reinterpret_cast<f32x4*>(static_cast<float*>(p.logits) + z0) = acc;
       } else {
-        static_cast<float*>(p.logits)[at] += sum[r];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          if (at + e >= p.V) break;
+          if (p.logits_bf16) static_cast<__bf16*>(p.logits)[z0 + e] = (__bf16)acc[e];
+          else static_cast<float*>(p.logits)[z0 + e] = acc[e];
+        }
       }
     }
   }

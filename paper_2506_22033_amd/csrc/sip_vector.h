@@ -2,6 +2,7 @@
 // workspace carving, launches.
 #pragma once
 #include <algorithm>
+#include <type_traits>
 
 #include "../../include/sip_head.h"
 #include "sip_adapt.h"
@@ -55,15 +56,17 @@ EmbedPlan embed_plan(int32_t N, int32_t D) {       // (of N tokens or fewer, but
   return p;
 }
 
+// Batches of B rows at most: one for every adapter that a row has, and one more for every sixteen rows.
+int adapt_batches(int32_t B, int32_t adapters) { return std::min(B, adapters + B / sip::kAdaptRows); }
 struct AdaptPlan { size_t count, rows, batch, t, bytes; };
-AdaptPlan adapt_plan(int32_t B, int32_t rank) {
+AdaptPlan adapt_plan(int32_t B, int32_t adapters, int32_t rank) {
   AdaptPlan p{};
   size_t at = 0;
   auto take = [&](size_t n) { const size_t here = at; at += head_align(n); return here; };
   p.count = take(4);
   p.rows = take((size_t)B * 4);
-  p.batch = take((size_t)B * 8);
-  p.t = take((size_t)B * rank * 4);
+  p.batch = take((size_t)B * 16);
+  p.t = take((size_t)adapt_batches(B, adapters) * sip::kAdaptRows * rank * 4);
   p.bytes = at;
   return p;
 }
@@ -149,7 +152,7 @@ sip_status sip_embed_backward(const void* grad_out, int64_t grad_out_stride, sip
 }
 
 size_t sip_head_adapt_workspace_bytes(int32_t B, int32_t adapters, int32_t rank, int32_t D) {
-  return adapt_shape_ok(B, adapters, rank, D) ? adapt_plan(B, rank).bytes : 0;
+  return adapt_shape_ok(B, adapters, rank, D) ? adapt_plan(B, adapters, rank).bytes : 0;
 }
 
 sip_status sip_head_adapt(const void* hidden, int32_t B, int32_t D, int64_t hidden_stride, sip_dtype hidden_dtype,
@@ -164,23 +167,47 @@ sip_status sip_head_adapt(const void* hidden, int32_t B, int32_t D, int64_t hidd
   if (!logits || logits_stride < V || reinterpret_cast<uintptr_t>(logits) % dtype_bytes(logits_dtype) != 0) return SIP_ERR_INVALID_ARG;
   if (!adapt_shape_ok(B, adapters, rank, D) || V > SIP_MAX_V || hidden_stride > (1ll << 32) || logits_stride > (1ll << 32))
     return SIP_ERR_UNSUPPORTED;
-  const AdaptPlan pl = adapt_plan(B, rank);
+  const AdaptPlan pl = adapt_plan(B, adapters, rank);
   if (!workspace_ok(workspace, workspace_bytes, pl.bytes)) return SIP_ERR_WORKSPACE;
   char* ws = static_cast<char*>(workspace);
   sip::AdaptArgs a{};
-  a.hidden = hidden; a.hidden_stride = hidden_stride; a.hidden_bf16 = hidden_dtype == SIP_BF16;
+  a.hidden = hidden; a.hidden_stride = hidden_stride;
   a.B = B; a.D = D; a.V = V; a.rank = rank; a.adapters = adapters;
   a.down = static_cast<const uint16_t*>(down); a.up = static_cast<const uint16_t*>(up);
   a.adapter_of_row = adapter_of_row; a.scales = scales;
   a.logits = logits; a.logits_stride = logits_stride; a.logits_bf16 = logits_dtype == SIP_BF16;
   a.count = reinterpret_cast<int*>(ws + pl.count);
   a.rows = reinterpret_cast<int*>(ws + pl.rows);
-  a.batch = reinterpret_cast<int2*>(ws + pl.batch);
+  a.batch = reinterpret_cast<int4*>(ws + pl.batch);
   a.t = reinterpret_cast<float*>(ws + pl.t);
+  const bool vector = logits_dtype == SIP_F32 && aligned16(logits) && logits_stride % 4 == 0;
   hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-  hipLaunchKernelGGL(sip::adapt_rows_kernel, dim3(1), dim3(1024), 0, stream, a);
-  hipLaunchKernelGGL(sip::adapt_down_kernel, dim3(B, rank / 8), dim3(256), 0, stream, a);
-  hipLaunchKernelGGL(sip::adapt_up_kernel, dim3(tiles(V, 256), std::min(B, 4096)), dim3(256), 0, stream, a);
+  const bool direct = B <= sip::kAdaptDirect;
+  const int batches = adapt_batches(B, adapters), steps = tiles(rank, 32);
+  int each = 16;                                         // tiles of a workgroup: fewer where that leaves the chip half empty
+  while (each > 1 && (long long)tiles(V, sip::kUpEntries * each) * batches < 8 * kChip) each /= 2;
+  if (!direct) hipLaunchKernelGGL(sip::adapt_rows_kernel, dim3(1), dim3(1024), 0, stream, a);
+  const dim3 down_grid(batches, tiles(rank, 16)), up_grid(tiles(tiles(V, sip::kUpEntries * each), 8) * 8 * batches);
+  auto launch = [&](auto in_direct) {
+    constexpr bool kDirect = decltype(in_direct)::value;
+    if (hidden_dtype == SIP_BF16) hipLaunchKernelGGL((sip::adapt_down_kernel<true, kDirect>), down_grid, dim3(sip::kDownWaves * 64), 0, stream, a);
+    else hipLaunchKernelGGL((sip::adapt_down_kernel<false, kDirect>), down_grid, dim3(sip::kDownWaves * 64), 0, stream, a);
+    auto add = [&](auto in_steps, auto in_vector) {
+      constexpr int kSteps = decltype(in_steps)::value;
+      constexpr bool kVector = decltype(in_vector)::value;
+      hipLaunchKernelGGL((sip::adapt_up_kernel<kSteps, kDirect, kVector>), up_grid, dim3(sip::kUpWaves * 64), 0, stream, a, batches, each);
+    };
+    auto add_steps = [&](auto in_vector) {
+      if (steps == 1) add(std::integral_constant<int, 1>{}, in_vector);
+      else if (steps == 2) add(std::integral_constant<int, 2>{}, in_vector);
+      else if (steps == 3) add(std::integral_constant<int, 3>{}, in_vector);
+      else add(std::integral_constant<int, 4>{}, in_vector);
+    };
+    if (vector) add_steps(std::true_type{});
+    else add_steps(std::false_type{});
+  };
+  if (direct) launch(std::true_type{});
+  else launch(std::false_type{});
   return launched();
 }
 
