@@ -3,6 +3,7 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "../../include/sip_head.h"
 #include "sip_gemm.h"
 
 namespace sip {
@@ -82,159 +83,343 @@ __global__ __launch_bounds__(256) void embed_kernel(EmbedArgs a) {
 
 // ---------------------------------------------------------------- gradient
 // The tokens are sorted, equal ones in the order of their positions.  The sorted list is cut into pieces; a lane sums eight
-// neighbouring columns of a piece's rows, token by token.  What a token has in one piece alone is final; what crosses the
-// border of a piece goes to the workspace in fp32, and a second kernel adds it up in order.
+// neighbouring columns of a piece's rows, token by token.  A cut that would fall into a token of few entries (`whole`) moves to its
+// end, so that a token is in one piece, and its sum final; sums of a longer one's parts go to the workspace in fp32, and a third kernel
+// adds them up in order.
 
 constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64;
+constexpr int kSortPairs = 256;                          // entries of a bucket that are compared with one another
+constexpr int kSortBits = 6, kSortBins = 1 << kSortBits; // most of a digit
+constexpr int kBucketMost = 4096;                        // tokens of a bucket
+constexpr int kPosBits = 16;                             // an entry: the token within its bucket, and the position below
 
 struct EmbedGradArgs {
-  const void* grad; long long grad_stride; int grad_bf16;
+  const void* grad; long long grad_stride;
   const int* ids;
   int N, V, D;
   float scale;
-  int accumulate;
   void* out; long long out_stride; int out_bf16;
-  int piece;                                             // entries of a piece
+  int shift, buckets;                                    // bucket of a token: its bits from `shift` on
+  int piece, whole;                                      // entries of a piece, and of a token that is not cut: powers of two
   // workspace
   int* live;                                             // entries that take part
-  uint32_t* key[2]; uint32_t* pos[2];                    // [N] tokens and their positions, sorted in the first pair
+  uint32_t* key; uint32_t* pos;                          // [N + 8] tokens and their positions, sorted
+  int* cut;                                              // [pieces] where a piece begins
+  uint32_t* spare[2];                                    // [N] for buckets that LDS does not hold
   float* part;                                           // [pieces][2][D] sums of what crosses a border: on the left, on the right
 };
 
-// Workgroup 0 sorts: three passes of a stable sort by seven bits each, lowest first; a wave has a run of entries.  Masked tokens come
-// last.  The others fill grad_weight with zeros, unless it is added to.
-__global__ __launch_bounds__(kSortThreads) void embed_sort_kernel(EmbedGradArgs a) {
-  constexpr int kBits = 7, kBins = 1 << kBits;
-  __shared__ uint32_t at[kBins][kSortWaves], wave_total[kSortWaves];
+// Stable sort of n entries by `bits` of the token, a digit after the other; from and to are LDS or global memory.  Returns where the
+// result is.  A wave has a run of entries, and counters of its own (their rows in LDS a bank apart).
+typedef uint32_t SortCounters[kSortWaves][kSortBins + 1];
+template <class P>
+__device__ inline P sort_entries(P from, P to, int n, int bits, SortCounters& at, uint32_t* wave_total) {
   const int t = threadIdx.x, lane = t & 63, w = t >> 6;
-  if (blockIdx.x > 0) {
-    const long long per_row = a.D / 8, total = per_row * a.V, step = (gridDim.x - 1) * (long long)kSortThreads;
-    const f32x8 none = {0, 0, 0, 0, 0, 0, 0, 0};
-    for (long long u = (blockIdx.x - 1) * (long long)kSortThreads + t; u < total; u += step) {
-      const long long v = u / per_row;
-      store_eight(a.out, v * a.out_stride + (u - v * per_row) * 8, a.out_bf16, none);
-    }
-    return;
-  }
-  const int run = (a.N + kSortThreads - 1) / kSortThreads * 64, first = w * run, last = min(a.N, first + run);
-  for (int pass = 0; pass < 3; ++pass) {
-    const int shift = pass * kBits;
-    const uint32_t* key_in = pass ? a.key[(pass - 1) & 1] : nullptr;
-    const uint32_t* pos_in = pass ? a.pos[(pass - 1) & 1] : nullptr;
-    uint32_t* key_out = a.key[pass & 1];
-    uint32_t* pos_out = a.pos[pass & 1];
-    auto key_of = [&](int i) {
-      if (pass) return key_in[i];
-      const uint32_t v = (uint32_t)a.ids[i];
-      return v < (uint32_t)a.V ? v : (uint32_t)a.V;
-    };
-    for (int i = t; i < kBins * kSortWaves; i += kSortThreads) at[i / kSortWaves][i % kSortWaves] = 0;
-    __syncthreads();
-    for (int i = first + lane; i < last; i += 64) atomicAdd(&at[key_of(i) >> shift & (kBins - 1)][w], 1u);
-    __syncthreads();
-    // where a wave's entries of a digit begin: those of lower digits, then those of earlier waves (2048 numbers, two a thread)
-    uint32_t* flat = &at[0][0];
-    const uint32_t x0 = flat[2 * t], x1 = flat[2 * t + 1];
-    uint32_t sum = x0 + x1;
-    for (int d = 1; d < 64; d <<= 1) {
-      const uint32_t other = __shfl_up(sum, d);
-      if (lane >= d) sum += other;
-    }
-    if (lane == 63) wave_total[w] = sum;
-    __syncthreads();
-    uint32_t before = sum - x0 - x1;
-    for (int j = 0; j < w; ++j) before += wave_total[j];
-    flat[2 * t] = before;
-    flat[2 * t + 1] = before + x0;
-    __syncthreads();
-    for (int i0 = first; i0 < last; i0 += 64) {
-      const int i = i0 + lane;
-      const bool mine = i < last;
-      const uint32_t key = mine ? key_of(i) : 0, digit = key >> shift & (kBins - 1);
+  const int run = (n + kSortThreads - 1) / kSortThreads * 64, first = min(n, w * run), last = min(n, first + run);
+  const int digits = (bits + kSortBits - 1) / kSortBits;
+  const unsigned long long below = (1ull << lane) - 1;
+  static_assert(kSortBins == 64 && kSortBins * kSortWaves == kSortThreads, "a number a thread");
+  for (int d = 0, low = 0; d < digits; ++d) {
+    const int wide = (bits - low + digits - d - 1) / (digits - d), shift = kPosBits + low;
+    const uint32_t mask = (1u << wide) - 1;
+    low += wide;
+    // the lanes with my digit
+    auto match = [&](uint32_t digit, bool mine) {
       unsigned long long same = __ballot(mine);
-#pragma unroll
-      for (int b = 0; b < kBits; ++b) {
+      for (int b = 0; b < wide; ++b) {
         const unsigned long long set = __ballot(digit >> b & 1);
         same &= digit >> b & 1 ? set : ~set;
       }
-      const int rank = __popcll(same & ((1ull << lane) - 1));
+      return same;
+    };
+    at[w][lane] = 0;
+    for (int i0 = first; i0 < last; i0 += 64) {
+      const bool mine = i0 + lane < last;
+      const uint32_t digit = (mine ? from[i0 + lane] : 0) >> shift & mask;
+      const unsigned long long same = match(digit, mine);
+      if (mine && !(same & below)) at[w][digit] += __popcll(same);
+    }
+    __syncthreads();
+    // where a wave's entries of a digit begin: those of lower digits, then those of earlier waves
+    uint32_t& mine_at = at[t % kSortWaves][t / kSortWaves];
+    const uint32_t x = mine_at;
+    uint32_t sum = x;
+    for (int s = 1; s < 64; s <<= 1) {
+      const uint32_t other = __shfl_up(sum, s);
+      if (lane >= s) sum += other;
+    }
+    if (lane == 63) wave_total[w] = sum;
+    __syncthreads();
+    uint32_t before = lane < w ? wave_total[lane] : 0;
+    for (int s = 1; s < kSortWaves; s <<= 1) before += __shfl_xor(before, s);
+    mine_at = __shfl(before, 0) + sum - x;
+    __syncthreads();
+    for (int i0 = first; i0 < last; i0 += 64) {
+      const bool mine = i0 + lane < last;
+      const uint32_t entry = mine ? from[i0 + lane] : 0, digit = entry >> shift & mask;
+      const unsigned long long same = match(digit, mine);
       uint32_t base = 0;
-      if (mine) base = at[digit][w];
-      if (mine && rank == 0) at[digit][w] = base + __popcll(same);
-      if (mine) {
-        key_out[base + rank] = key;
-        pos_out[base + rank] = pass ? pos_in[i] : (uint32_t)i;
-      }
+      if (mine) base = at[w][digit];
+      if (mine && !(same & below)) at[w][digit] = base + __popcll(same);
+      if (mine) to[base + __popcll(same & below)] = entry;
     }
     __syncthreads();                                     // (and what was written is read by the workgroup itself)
+    const P other = from;
+    from = to;
+    to = other;
   }
-  const uint32_t* key = a.key[0];
-  if (t == 0) *a.live = 0;
-  __syncthreads();
-  for (int i = t; i < a.N; i += kSortThreads)
-    if (key[i] < (uint32_t)a.V && (i + 1 == a.N || key[i + 1] >= (uint32_t)a.V)) *a.live = i + 1;
+  return from;
 }
 
-__device__ inline void embed_store(const EmbedGradArgs& a, int v, int c, f32x8 sum) {
+// Zeros in all rows of grad_weight: 16 bytes a lane (up to 2^31 in all), of `lanes` lanes mine.
+__device__ inline void clear_rows(const EmbedGradArgs& a, uint32_t mine, uint32_t lanes) {
+  const uint32_t size = a.out_bf16 ? 2 : 4, per_row = a.D * size / 16, end = per_row * (uint32_t)a.V;
+  u32x4* out = static_cast<u32x4*>(a.out);
+  if (a.out_stride == a.D) {
+#pragma unroll 4
+    for (uint32_t u = mine; u < end; u += lanes) out[u] = u32x4{0, 0, 0, 0};
+  } else {
+    const long long pitch = a.out_stride * size / 16;
+    for (uint32_t u = mine; u < end; u += lanes) {
+      const uint32_t v = u / per_row;
+      out[v * pitch + (u - v * per_row)] = u32x4{0, 0, 0, 0};
+    }
+  }
+}
+
+// A workgroup a bucket of the vocabulary: it reads all tokens, lists those of its bucket in order, counts those of the buckets before, and
+// sorts its own.  The workgroups behind fill grad_weight with zeros meanwhile, unless it is added to.  ROOM: entries of a bucket
+// that LDS holds, twice; larger buckets are sorted in the workspace.
+struct __attribute__((packed, aligned(4))) FourIds { uint32_t x[4]; };
+template <int ROOM>
+__global__ __launch_bounds__(kSortThreads) void embed_sort_kernel(EmbedGradArgs a) {
+  __shared__ uint32_t room[2][ROOM];
+  __shared__ SortCounters at;
+  __shared__ uint32_t wave_total[kSortWaves], wave_before[kSortWaves];
+  const int t = threadIdx.x, lane = t & 63, w = t >> 6;
+  if ((int)blockIdx.x >= a.buckets) {
+    clear_rows(a, (blockIdx.x - a.buckets) * kSortThreads + t, (gridDim.x - a.buckets) * kSortThreads);
+    return;
+  }
+  // A wave's run of ids, four neighbours a lane, kQuads loads under way at once.
+  constexpr int kQuads = 4;
+  const int bucket = blockIdx.x, run = (a.N + kSortThreads * 4 - 1) / (kSortThreads * 4) * 256, first = w * run, last = min(a.N, first + run);
+  const uint32_t low = (uint32_t)bucket << a.shift, size = min((uint32_t)a.V - low, 1u << a.shift);
+  FourIds id[kQuads];
+  auto load = [&](int i0) {
+#pragma unroll
+    for (int j = 0; j < kQuads; ++j) {
+      const int i = i0 + j * 256 + lane * 4;
+      id[j] = FourIds{{0xffffffffu, 0xffffffffu, 0xffffffffu, 0xffffffffu}};
+      if (i + 4 <= last) id[j] = *reinterpret_cast<const FourIds*>(a.ids + i);
+      else
+        for (int e = 0; e < 3; ++e)
+          if (i + e < last) id[j].x[e] = (uint32_t)a.ids[i + e];
+    }
+  };
+  uint32_t n = 0, before = 0;                            // of the wave's ids
+  for (int i0 = first; i0 < last; i0 += kQuads * 256) {
+    load(i0);
+#pragma unroll
+    for (int j = 0; j < kQuads; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        n += __popcll(__ballot(id[j].x[e] - low < size));
+        before += __popcll(__ballot(id[j].x[e] < low));
+      }
+  }
+  if (lane == 0) { wave_total[w] = n; wave_before[w] = before; }
+  __syncthreads();
+  uint32_t mine_n = lane < kSortWaves ? wave_total[lane] : 0, base = lane < w ? mine_n : 0, start = lane < kSortWaves ? wave_before[lane] : 0;
+  for (int s = 1; s < kSortWaves; s <<= 1) {
+    mine_n += __shfl_xor(mine_n, s);
+    base += __shfl_xor(base, s);
+    start += __shfl_xor(start, s);
+  }
+  n = __shfl(mine_n, 0);
+  base = __shfl(base, 0);
+  start = __shfl(start, 0);
+  if (bucket == a.buckets - 1 && t == 0) *a.live = (int)(start + n);
+  if (n == 0) return;
+  const bool in_lds = n <= ROOM;
+  uint32_t* spare0 = a.spare[0] + start;
+  uint32_t* spare1 = a.spare[1] + start;
+  const unsigned long long below = (1ull << lane) - 1;
+  for (int i0 = first; i0 < last; i0 += kQuads * 256) {
+    if (run > kQuads * 256) load(i0);
+#pragma unroll
+    for (int j = 0; j < kQuads; ++j) {
+      unsigned long long mine[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) mine[e] = __ballot(id[j].x[e] - low < size);
+      if (mine[0] | mine[1] | mine[2] | mine[3]) {
+        uint32_t to = base;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          to += __popcll(mine[e] & below);
+          base += __popcll(mine[e]);
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (mine[e] >> lane & 1) {
+            const uint32_t entry = (id[j].x[e] - low) << kPosBits | (uint32_t)(i0 + j * 256 + lane * 4 + e);
+            if (in_lds) room[0][to] = entry;
+            else spare0[to] = entry;
+            ++to;
+          }
+      }
+    }
+  }
+  __syncthreads();
+  // what is sorted goes out, and where the pieces' borders among it lie
+  auto finish = [&](auto sorted) {
+    for (uint32_t i = t; i < n; i += kSortThreads) {
+      const uint32_t entry = sorted[i];
+      a.key[start + i] = (uint32_t)bucket << a.shift | entry >> kPosBits;
+      a.pos[start + i] = entry & ((1u << kPosBits) - 1);
+    }
+    for (uint32_t border = (start + a.piece - 1) / a.piece * a.piece + t * a.piece; border < start + n; border += kSortThreads * a.piece) {
+      const int i = (int)(border - start), token = sorted[i] >> kPosBits;
+      auto is = [&](int j) { return j >= 0 && j < (int)n && (int)(sorted[j] >> kPosBits) == token; };
+      int cut = i;
+      if (is(i - 1) && !is(i - a.whole) && !is(i + a.whole)) {           // (else it has more than that many entries, or begins here)
+        int before = 1, behind = 0;                      // as many of its entries are ahead of the border for certain, and behind
+        for (int step = a.whole / 2; step; step /= 2) {
+          if (is(i - before - step)) before += step;
+          if (is(i + behind + step)) behind += step;
+        }
+        if (before + behind + 1 <= a.whole) cut = i + behind + 1;
+      }
+      a.cut[border / a.piece] = (int)start + cut;
+    }
+  };
+  typedef SIP_LDS uint32_t* Lds;
+  if (n <= kSortPairs) {
+    if (t < (int)n) {
+      const uint32_t mine = room[0][t];
+      uint32_t rank = 0;
+      for (uint32_t j = 0; j < n; ++j) rank += room[0][j] < mine;
+      room[1][rank] = mine;
+    }
+    __syncthreads();
+    finish((Lds)&room[1][0]);
+  } else if (in_lds) {
+    finish(sort_entries<Lds>((Lds)&room[0][0], (Lds)&room[1][0], (int)n, a.shift, at, wave_total));
+  } else {
+    finish(sort_entries<uint32_t*>(spare0, spare1, (int)n, a.shift, at, wave_total));
+  }
+}
+
+__device__ inline void embed_store(const EmbedGradArgs& a, long long at, f32x8 sum, const Eight* old) {
   sum *= a.scale;
-  const long long at = v * a.out_stride + c;
-  if (a.accumulate) sum += as_floats(load_eight(a.out, at, a.out_bf16), a.out_bf16);
+  if (old) sum += as_floats(*old, a.out_bf16);
   store_eight(a.out, at, a.out_bf16, sum);
 }
 
-// A lane: eight columns of one piece.
-template <bool BF16>
+// A lane: eight columns of one piece, eight rows under way at once, and where they are added to the rows of grad_weight that end there.
+constexpr int kSumAhead = 8;
+template <bool BF16, bool ADD>
 __global__ __launch_bounds__(256) void embed_sum_kernel(EmbedGradArgs a) {
-  const int per_row = a.D / 8, n = *a.live;
-  const long long u = blockIdx.x * 256ll + threadIdx.x;
-  const int piece = (int)(u / per_row), c = (int)(u - (long long)piece * per_row) * 8;
-  const long long first = (long long)piece * a.piece;
-  if (first >= n) return;
-  const int last = (int)min((long long)n, first + a.piece);
-  const uint32_t* key = a.key[0];
-  const uint32_t* pos = a.pos[0];
-  const f32x8 none = {0, 0, 0, 0, 0, 0, 0, 0};
-  f32x8 sum = none;
-  bool begun = first == 0 || key[first - 1] != key[first];             // the token's first entry is in this piece
-  for (int i = (int)first; i < last; ++i) {
-    sum += as_floats(load_eight(a.grad, pos[i] * a.grad_stride + c, BF16), BF16);
-    const bool ends = i + 1 == n || key[i + 1] != key[i];
-    if (!ends && i + 1 < last) continue;
-    if (begun && ends) embed_store(a, (int)key[i], c, sum);
-    else store_eight(a.part, ((long long)piece * 2 + begun) * a.D + c, false, sum);
-    sum = none;
-    begun = true;
+  const uint32_t per_row = a.D / 8, u = blockIdx.x * 256 + threadIdx.x;                     // (up to 2^28)
+  const int n = *a.live, piece = (int)(u / per_row), c = (int)(u - piece * per_row) * 8;
+  if ((long long)piece * a.piece >= n) return;
+  const int first = a.cut[piece], last = (piece + 1ll) * a.piece < n ? a.cut[piece + 1] : n;
+  if (first >= last) return;
+  f32x8 sum = {0, 0, 0, 0, 0, 0, 0, 0};
+  bool begun = first == 0 || a.key[first - 1] != a.key[first];         // the token's first entry is in this piece
+  struct __attribute__((packed, aligned(4))) Ahead { uint32_t x[kSumAhead]; };
+  Ahead next_key, next_pos;
+  uint32_t next_last;
+  auto look = [&](int i0) {                              // (what lies behind the last entry may be anything)
+    next_key = *reinterpret_cast<const Ahead*>(a.key + i0);
+    next_pos = *reinterpret_cast<const Ahead*>(a.pos + i0);
+    next_last = a.key[i0 + kSumAhead];
+  };
+  look(first);
+  for (int i0 = first; i0 < last; i0 += kSumAhead) {
+    uint32_t key[kSumAhead + 1], pos[kSumAhead];
+#pragma unroll
+    for (int j = 0; j < kSumAhead; ++j) {
+      key[j] = next_key.x[j];
+      pos[j] = next_pos.x[j];
+    }
+    key[kSumAhead] = next_last;
+    if (i0 + kSumAhead < last) look(i0 + kSumAhead);
+#pragma unroll
+    for (int j = 0; j <= kSumAhead; ++j)
+      if (i0 + j >= n) key[j] = 0xffffffffu;
+    Eight x[kSumAhead], old[kSumAhead];
+    bool fresh = begun;
+#pragma unroll
+    for (int j = 0; j < kSumAhead; ++j) {
+      x[j] = Eight{};
+      if (i0 + j < last) x[j] = load_eight(a.grad, pos[j] * a.grad_stride + c, BF16);
+      if constexpr (ADD) {
+        old[j] = Eight{};
+        if (i0 + j < last && key[j + 1] != key[j]) {
+          if (fresh) old[j] = load_eight(a.out, key[j] * a.out_stride + c, a.out_bf16);
+          fresh = true;
+        }
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < kSumAhead; ++j) {
+      if (i0 + j < last) {
+        sum += as_floats(x[j], BF16);
+        const bool ends = key[j + 1] != key[j];
+        if (ends || i0 + j + 1 == last) {
+          if (begun && ends) embed_store(a, key[j] * a.out_stride + c, sum, ADD ? &old[j] : nullptr);
+          else store_eight(a.part, ((long long)piece * 2 + begun) * a.D + c, false, sum);
+          sum = f32x8{0, 0, 0, 0, 0, 0, 0, 0};
+          begun = true;
+        }
+      }
+    }
   }
 }
 
-// The token that piece `blockIdx.x`'s right border cuts first, if it begins in that piece: sixteen lanes of eight columns, of which each
-// has sixteen workers that take every sixteenth of the pieces.
-__global__ __launch_bounds__(256) void embed_join_kernel(EmbedGradArgs a) {
-  __shared__ f32x8 sums[16][16];
-  const int n = *a.live, piece = blockIdx.x;
-  const long long border = (long long)(piece + 1) * a.piece;
-  if (border >= n) return;
-  const uint32_t* key = a.key[0];
-  const uint32_t v = key[border];
-  if (key[border - 1] != v) return;
-  const long long begin = (long long)piece * a.piece;
-  if (begin > 0 && key[begin] == v && key[begin - 1] == v) return;     // it began before
-  long long end = n;                                     // behind its last entry
-  for (long long low = border; low < end;) {
-    const long long mid = (low + end) / 2;
-    if (key[mid] > v) end = mid;
-    else low = mid + 1;
+// The tokens that begin in a piece and go on behind its right border: 64 lanes of eight columns, of which each has sixteen workers
+// that take every sixteenth of the token's pieces.  A workgroup looks at kJoinPieces of them.
+constexpr int kJoinPieces = 4;
+template <bool ADD>
+__global__ __launch_bounds__(1024) void embed_join_kernel(EmbedGradArgs a) {
+  __shared__ f32x8 sums[kSortWaves][64];
+  const int n = *a.live, worker = threadIdx.x >> 6, lane = threadIdx.x & 63, c = (blockIdx.y * 64 + lane) * 8, piece0 = blockIdx.x * kJoinPieces;
+  uint32_t token = 0;                                    // lane j: that of piece0 + j
+  bool cut = false;
+  if (lane < kJoinPieces && (piece0 + lane + 1ll) * a.piece < n) {
+    const int begin = a.cut[piece0 + lane], border = (piece0 + lane + 1) * a.piece;
+    if (a.cut[piece0 + lane + 1] == border && begin < border) {
+      token = a.key[border];
+      cut = a.key[border - 1] == token && (begin == 0 || a.key[begin - 1] != token);
+    }
   }
-  const int pieces = (int)((end - 1) / a.piece) - piece, worker = threadIdx.x >> 4, c = (blockIdx.y * 16 + (threadIdx.x & 15)) * 8;
-  f32x8 sum = {0, 0, 0, 0, 0, 0, 0, 0};
-  if (c < a.D)
-    for (int j = worker; j <= pieces; j += 16)
-      sum += as_floats(load_eight(a.part, ((long long)(piece + j) * 2 + (j == 0)) * a.D + c, false), false);
-  sums[worker][threadIdx.x & 15] = sum;
-  __syncthreads();
-  if (worker > 0 || c >= a.D) return;
-  for (int j = 1; j < 16; ++j) sum += sums[j][threadIdx.x & 15];
-  embed_store(a, (int)v, c, sum);
+  for (unsigned long long left = __ballot(cut); left; left &= left - 1) {
+    const int j0 = __builtin_ctzll(left), piece = piece0 + j0;
+    const uint32_t v = __builtin_amdgcn_readlane(token, j0);
+    int pieces = 1;                                      // behind this one, that begin with the token: 64 at a time
+    while (true) {
+      const long long at = (long long)(piece + pieces + 1 + lane) * a.piece;
+      const unsigned long long same = __ballot(at < n && a.key[min(at, (long long)n - 1)] == v);
+      pieces += __builtin_ctzll(~same | 1ull << 63);
+      if (~same) break;
+      ++pieces;                                          // (all 64: the count stopped at 63)
+    }
+    f32x8 sum = {0, 0, 0, 0, 0, 0, 0, 0};
+    Eight old = {};
+    if (c < a.D) {
+      if (ADD && worker == 0) old = load_eight(a.out, v * a.out_stride + c, a.out_bf16);
+#pragma unroll 4
+      for (int j = worker; j <= pieces; j += kSortWaves)
+        sum += as_floats(load_eight(a.part, ((long long)(piece + j) * 2 + (j == 0)) * a.D + c, false), false);
+    }
+    __syncthreads();
+    sums[worker][lane] = sum;
+    __syncthreads();
+    if (worker > 0 || c >= a.D) continue;
+    for (int j = 1; j < min(kSortWaves, pieces + 1); ++j) sum += sums[j][lane];
+    embed_store(a, v * a.out_stride + c, sum, ADD ? &old : nullptr);
+  }
 }
 
 }  // namespace sip

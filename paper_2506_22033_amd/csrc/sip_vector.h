@@ -28,27 +28,39 @@ sip::EmbedArgs embed_args(int32_t V, int32_t D, const int32_t* ids, int32_t N, f
 }
 dim3 embed_grid(int32_t N, int32_t D) { return dim3(std::min<long long>(tiles((long long)N * (D / 8), 256), 1 << 20)); }
 
-// Entries of a piece of the sorted tokens: 4 to 32, as many as leave every SIMD two waves.
-constexpr long long kEmbedLanes = kChip * 4 * 64 * 2;
+// Entries of a piece of the sorted tokens: 8 to 64, as many as leave every SIMD four waves.
+constexpr int kPieceLeast = sip::kSumAhead, kPieceMost = 64;
+constexpr long long kEmbedLanes = kChip * 4 * 64 * 4;
 int embed_piece(int32_t N, int32_t D) {
-  int piece = 4;
-  while (piece < 32 && (long long)N * (D / 8) >= 2 * piece * kEmbedLanes) piece *= 2;
+  int piece = kPieceLeast;
+  while (piece < kPieceMost && (long long)N * (D / 8) >= 2 * piece * kEmbedLanes) piece *= 2;
   return piece;
 }
 // The most pieces of N tokens or fewer.
 int embed_pieces_most(int32_t N, int32_t D) {
   int most = tiles(N, embed_piece(N, D));
-  for (int piece = 4; piece < embed_piece(N, D); piece *= 2)
+  for (int piece = kPieceLeast; piece < embed_piece(N, D); piece *= 2)
     most = std::max(most, tiles((2 * piece * kEmbedLanes - 1) / (D / 8), piece));
   return most;
 }
-struct EmbedPlan { int piece, pieces; size_t live, key[2], pos[2], part, bytes; };
-EmbedPlan embed_plan(int32_t N, int32_t D) {       // (of N tokens or fewer, but for `piece` and `pieces`)
+// Buckets of the vocabulary: up to 128, each a power of two wide.
+int embed_shift(int32_t V) {
+  int shift = 0;
+  while (tiles(V, 1 << shift) > 128) ++shift;
+  return shift;
+}
+static_assert(SIP_MAX_TOKENS <= 1 << sip::kPosBits && SIP_MAX_V <= 128 * sip::kBucketMost && sip::kBucketMost <= 1 << (32 - sip::kPosBits),
+              "an entry is 32 bits");
+struct EmbedPlan { int piece, pieces; size_t live, key, pos, cut, spare[2], part, bytes; };
+EmbedPlan embed_plan(int32_t N, int32_t D) {             // (room for N tokens or fewer)
   EmbedPlan p{};
   size_t at = 0;
   auto take = [&](size_t n) { const size_t here = at; at += head_align(n); return here; };
   p.live = take(4);
-  for (int i = 0; i < 2; ++i) { p.key[i] = take((size_t)N * 4); p.pos[i] = take((size_t)N * 4); }
+  p.key = take(((size_t)N + 2 * sip::kSumAhead) * 4);
+  p.pos = take(((size_t)N + 2 * sip::kSumAhead) * 4);
+  p.cut = take((size_t)N / kPieceLeast * 4 + 4);
+  for (size_t& s : p.spare) s = take((size_t)N * 4);
   p.piece = embed_piece(N, D);
   p.pieces = tiles(N, p.piece);
   p.part = take((size_t)embed_pieces_most(N, D) * 2 * D * 4);
@@ -129,24 +141,34 @@ sip_status sip_embed_backward(const void* grad_out, int64_t grad_out_stride, sip
   const EmbedPlan pl = embed_plan(std::max(N, 1), D);
   char* ws = static_cast<char*>(workspace);
   sip::EmbedGradArgs a{};
-  a.grad = grad_out; a.grad_stride = grad_out_stride; a.grad_bf16 = grad_out_dtype == SIP_BF16;
-  a.ids = ids; a.N = N; a.V = V; a.D = D; a.scale = scale; a.accumulate = accumulate != 0;
+  a.grad = grad_out; a.grad_stride = grad_out_stride;
+  a.ids = ids; a.N = N; a.V = V; a.D = D; a.scale = scale;
   a.out = grad_weight; a.out_stride = grad_weight_stride; a.out_bf16 = grad_weight_dtype == SIP_BF16;
+  a.shift = embed_shift(V);
+  a.buckets = N > 0 ? tiles(V, 1 << a.shift) : 0;
   a.piece = pl.piece;
+  a.whole = 2 * pl.piece;
   a.live = reinterpret_cast<int*>(ws + pl.live);
-  for (int i = 0; i < 2; ++i) {
-    a.key[i] = reinterpret_cast<uint32_t*>(ws + pl.key[i]);
-    a.pos[i] = reinterpret_cast<uint32_t*>(ws + pl.pos[i]);
-  }
+  a.key = reinterpret_cast<uint32_t*>(ws + pl.key);
+  a.pos = reinterpret_cast<uint32_t*>(ws + pl.pos);
+  a.cut = reinterpret_cast<int*>(ws + pl.cut);
+  for (int i = 0; i < 2; ++i) a.spare[i] = reinterpret_cast<uint32_t*>(ws + pl.spare[i]);
   a.part = reinterpret_cast<float*>(ws + pl.part);
   hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-  const int fill = accumulate ? 0 : (int)std::min<long long>(tiles((long long)V * (D / 8), sip::kSortThreads), 2 * kChip);
-  hipLaunchKernelGGL(sip::embed_sort_kernel, dim3(1 + fill), dim3(sip::kSortThreads), 0, stream, a);
+  const long long lines = (long long)V * D * dtype_bytes(grad_weight_dtype) / 16;
+  const dim3 sort_grid(a.buckets + (accumulate ? 0 : std::min(tiles(lines, sip::kSortThreads * 4), 16 * kChip)));
+  if (N <= 8192) hipLaunchKernelGGL(sip::embed_sort_kernel<8192>, sort_grid, dim3(sip::kSortThreads), 0, stream, a);
+  else hipLaunchKernelGGL(sip::embed_sort_kernel<16384>, sort_grid, dim3(sip::kSortThreads), 0, stream, a);
   if (N > 0) {
-    const dim3 grid(tiles((long long)pl.pieces * (D / 8), 256));
-    if (a.grad_bf16) hipLaunchKernelGGL(sip::embed_sum_kernel<true>, grid, dim3(256), 0, stream, a);
-    else hipLaunchKernelGGL(sip::embed_sum_kernel<false>, grid, dim3(256), 0, stream, a);
-    hipLaunchKernelGGL(sip::embed_join_kernel, dim3(pl.pieces, tiles(D, 128)), dim3(256), 0, stream, a);
+    const dim3 sum_grid(tiles((long long)pl.pieces * (D / 8), 256)), join_grid(tiles(pl.pieces, sip::kJoinPieces), tiles(D, 512));
+    auto launch = [&](auto in_add) {
+      constexpr bool kAdd = decltype(in_add)::value;
+      if (grad_out_dtype == SIP_BF16) hipLaunchKernelGGL((sip::embed_sum_kernel<true, kAdd>), sum_grid, dim3(256), 0, stream, a);
+      else hipLaunchKernelGGL((sip::embed_sum_kernel<false, kAdd>), sum_grid, dim3(256), 0, stream, a);
+      hipLaunchKernelGGL(sip::embed_join_kernel<kAdd>, join_grid, dim3(1024), 0, stream, a);
+    };
+    if (accumulate) launch(std::true_type{});
+    else launch(std::false_type{});
   }
   return launched();
 }
