@@ -3,27 +3,29 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
+#include "sip_gemm.h"
 #include "sip_state.h"
 
 namespace sip {
 
 // ---------------------------------------------------------------- selection
 // beam_chunk_kernel: a workgroup reads one chunk of a row once and leaves its maximum, its sum of exponentials and its n best
-// logits, in order.  beam_merge_kernel: a workgroup joins the lists of a group's rows.
+// logits, in order.  The merging kernels: a workgroup joins the lists of a group's rows.
 
-constexpr int kBeamThreads = 256;
-constexpr int kBeamEach = 32;                            // logits of a lane, in registers
-constexpr int kBeamChunk = kBeamThreads * kBeamEach;
+constexpr int kBeamThreads = 256, kBeamWaves = kBeamThreads / 64;
+constexpr int kBeamLoads = 8;                            // 16-byte loads of a lane: 32 fp32 logits, 64 bf16
 constexpr int kBeamList = 512;                           // entries that a chunk's list may have before it is ranked
-constexpr int kMergeThreads = 1024;
+inline __host__ __device__ int beam_chunk(bool bf16) { return kBeamThreads * kBeamLoads * (bf16 ? 8 : 4); }
 
-struct BeamPart { double sum; float max; float pad; };   // of a chunk: sum of 2^(c (z - max))
+struct BeamPart { double sum; float max, pad; };         // of a chunk: sum of 2^(c (z - max))
 
 struct BeamArgs {
   const void* logits; long long row_stride;
   int groups, width, V, n;
-  int chunks;                                            // of a row
-  float c_hi, c_lo;                                      // logit_scale * log2(e) = c_hi + c_lo, c_lo > 0
+  int chunks, chunk;                                     // of a row; logits of one
+  float c;                                               // logit_scale * log2(e)
   double scale;                                          // logit_scale
   const float* scores; const uint8_t* finished; const float* rank_scale;
   int end_token;
@@ -51,84 +53,252 @@ __device__ inline unsigned long long beam_key(float z, int token) {
 __device__ inline int key_token(unsigned long long key) { return (int)~(uint32_t)key; }
 __device__ inline float key_logit(unsigned long long key) { return unordered((uint32_t)(key >> 32)); }
 
+// A wave's sum, in lane 63.
+__device__ inline double wave_total(double x) {
+  auto step = [&](auto control, auto rows) {
+    const unsigned long long u = __builtin_bit_cast(unsigned long long, x);
+    const uint32_t lo = dpp_mov<decltype(control)::value, decltype(rows)::value>(0u, (uint32_t)u);
+    const uint32_t hi = dpp_mov<decltype(control)::value, decltype(rows)::value>(0u, (uint32_t)(u >> 32));
+    x += __builtin_bit_cast(double, (unsigned long long)hi << 32 | lo);
+  };
+  step(std::integral_constant<int, 0x111>(), std::integral_constant<int, 0xf>());        // row_shr 1, 2, 4, 8
+  step(std::integral_constant<int, 0x112>(), std::integral_constant<int, 0xf>());
+  step(std::integral_constant<int, 0x114>(), std::integral_constant<int, 0xf>());
+  step(std::integral_constant<int, 0x118>(), std::integral_constant<int, 0xf>());
+  step(std::integral_constant<int, 0x142>(), std::integral_constant<int, 0xa>());        // row_bcast 15, 31
+  step(std::integral_constant<int, 0x143>(), std::integral_constant<int, 0xc>());
+  return x;
+}
+
+// In a chunk's list an entry is a whole number below 2^46, the logit's and then its place from behind, as the double 2^52 + that:
+// these compare in one instruction.
+constexpr int kPlaceBits = 14;
+__device__ inline double list_entry(float z, int place) {
+  return __builtin_bit_cast(double, 0x4330000000000000ull | (unsigned long long)ordered(z) << kPlaceBits | (uint32_t)((1 << kPlaceBits) - 1 - place));
+}
+__device__ inline unsigned long long entry_key(double x, int first) {
+  const unsigned long long u = __builtin_bit_cast(unsigned long long, x);
+  return (u >> kPlaceBits & 0xffffffffu) << 32 | (uint32_t)~(first + (1 << kPlaceBits) - 1 - (int)(u & ((1u << kPlaceBits) - 1)));
+}
+static_assert(kBeamThreads * kBeamLoads * 8 <= 1 << kPlaceBits, "a place in the chunk");
+
 // What a row has: continuations from its logits, one at no cost, or none.
 enum BeamRow { kBeamNone, kBeamLive, kBeamFinished };
-__device__ inline BeamRow beam_row(const BeamArgs& a, int row) {
-  if (!isfinite(a.scores[row])) return kBeamNone;
-  if (a.rank_scale && !(a.rank_scale[row] > 0.0f && isfinite(a.rank_scale[row]))) return kBeamNone;
-  return a.finished && a.finished[row] ? kBeamFinished : kBeamLive;
+struct BeamRowInfo { float score, scale; int what; };
+__device__ inline BeamRowInfo beam_row(const BeamArgs& a, int row) {
+  const float score = a.scores[row], scale = a.rank_scale ? a.rank_scale[row] : 1.0f;
+  const uint8_t finished = a.finished ? a.finished[row] : 0;
+  const bool ok = isfinite(score) && isfinite(scale) && scale > 0.0f;
+  return {score, scale, !ok ? kBeamNone : finished ? kBeamFinished : kBeamLive};
+}
+
+// The logits of a lane's 16-byte loads: logit e of those is at place beam_place(e) behind the lane's first.
+template <int GROUP> constexpr int beam_place(int e) { return e / GROUP * (kBeamThreads * GROUP) + e % GROUP; }
+template <int GROUP>
+__device__ __forceinline__ float beam_logit(const u32x4 (&raw)[kBeamLoads], int e) {
+  const uint32_t u = raw[e / GROUP][e % GROUP * 4 / GROUP], bits = GROUP == 4 ? u : e & 1 ? u & 0xffff0000u : u << 16;
+  return __builtin_bit_cast(float, bits);
+}
+
+// A chunk with more than kBeamList logits from the bound on, nearly equal ones or a mask's many equal ones: its n first entries to the list
+// (any order).  The n-th largest logit is found, and among those that equal it the lowest tokens.
+template <int GROUP>
+__device__ __forceinline__ int select_apart(u32x4 (&raw)[kBeamLoads], double* list, int& count, int (&wave_n)[kBeamWaves], float from, int n) {
+  constexpr int kEach = kBeamLoads * GROUP;
+  const int t = threadIdx.x, lane = t & 63, w = t >> 6;
+  auto sum_of = [&](int mine) {                          // over the workgroup
+    for (int d = 32; d; d >>= 1) mine += __shfl_xor(mine, d);
+    __syncthreads();
+    if (lane == 0) wave_n[w] = mine;
+    __syncthreads();
+    return wave_n[0] + wave_n[1] + wave_n[2] + wave_n[3];
+  };
+  // f(e) of all logits, eight at a time
+  auto each = [&](auto f) {
+#pragma unroll
+    for (int i = 0; i < kBeamLoads; ++i) asm volatile("" : "+v"(raw[i]));        // (nothing of it is kept)
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) {
+      f(e);
+      if (e % 8 == 7) __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  // The smallest from the bound on: a mask's value, as a rule.
+  float low = INFINITY;
+  each([&](int e) { low = beam_logit<GROUP>(raw, e) >= from ? fminf(low, beam_logit<GROUP>(raw, e)) : low; });
+  for (int d = 32; d; d >>= 1) low = fminf(low, __shfl_xor(low, d));
+  __syncthreads();
+  if (lane == 0) wave_n[w] = __builtin_bit_cast(int, low);
+  __syncthreads();
+  for (int i = 0; i < kBeamWaves; ++i) low = fminf(low, __builtin_bit_cast(float, wave_n[i]));
+  int mine = 0;
+  each([&](int e) { mine += beam_logit<GROUP>(raw, e) > low; });
+  int above = sum_of(mine);
+  if (above >= n) {
+    // the n-th largest, bit by bit: the largest value that n logits reach
+    uint32_t at = 0;
+    for (int bit = 31; bit >= 0; --bit) {
+      const uint32_t up = at | 1u << bit;
+      if (up > 0xff800000u) continue;                    // (beyond +inf)
+      const float least = unordered(up);
+      mine = 0;
+      if (up >= 0x007fffffu) each([&](int e) { mine += beam_logit<GROUP>(raw, e) >= least; });
+      if (up < 0x007fffffu || sum_of(mine) >= n) at = up;
+    }
+    low = unordered(at);
+    mine = 0;
+    each([&](int e) { mine += beam_logit<GROUP>(raw, e) > low; });
+    above = sum_of(mine);
+  }
+  // of those that equal it, the n - above lowest: all below `end`
+  int end = 0;
+  for (int bit = kPlaceBits; bit >= 0; --bit) {
+    const int up = end | 1 << bit, mine_end = up - t * GROUP;
+    mine = 0;
+    each([&](int e) { mine += beam_logit<GROUP>(raw, e) == low && beam_place<GROUP>(e) < mine_end; });
+    if (sum_of(mine) <= n - above) end = up;
+  }
+  __syncthreads();
+  if (t == 0) count = 0;
+  __syncthreads();
+  const int mine_end = end - t * GROUP;
+  each([&](int e) {
+    const float z = beam_logit<GROUP>(raw, e);
+    if (z > low || (z == low && beam_place<GROUP>(e) < mine_end)) list[atomicAdd(&count, 1)] = list_entry(z, t * GROUP + beam_place<GROUP>(e));
+  });
+  __syncthreads();
+  return count;
 }
 
 template <bool BF16>
 __global__ __launch_bounds__(kBeamThreads) void beam_chunk_kernel(BeamArgs a) {
-  constexpr int kGroup = BF16 ? 8 : 4, kLoads = kBeamEach / kGroup;      // logits of a 16-byte load; loads of a lane
-  __shared__ __align__(16) uint32_t lane_max[kBeamThreads];
-  __shared__ __align__(16) unsigned long long list[kBeamList];
-  __shared__ double wave_sum[kBeamThreads / 64];
-  __shared__ float wave_max[kBeamThreads / 64], least;
-  __shared__ int count;
+  constexpr int kGroup = BF16 ? 8 : 4, kEach = kBeamLoads * kGroup;      // logits of a 16-byte load, of a lane
+  __shared__ __align__(16) double list[kBeamList];
+  __shared__ double wave_sum[kBeamWaves];
+  __shared__ float wave_max[kBeamWaves];
+  __shared__ uint32_t wave_least[kBeamWaves];
+  __shared__ int count, wave_n[kBeamWaves];
   const int row = blockIdx.x / a.chunks, chunk = blockIdx.x % a.chunks;
   const int t = threadIdx.x, lane = t & 63, w = t >> 6;
-  if (beam_row(a, row) != kBeamLive) return;
-  // logit j of load i is token first + i * 256 * kGroup + j
-  const int first = chunk * kBeamChunk + t * kGroup;
-  auto token = [&](int e) { return first + e / kGroup * (kBeamThreads * kGroup) + e % kGroup; };
+  if (beam_row(a, row).what != kBeamLive) return;
+  const int first = chunk * a.chunk + t * kGroup;        // my first token
   const char* z0 = static_cast<const char*>(a.logits) + ((long long)row * a.row_stride + first) * (BF16 ? 2 : 4);
-  float z[kBeamEach];
-  uint4 raw[kLoads];
+  u32x4 raw[kBeamLoads];
+  const uint32_t none = BF16 ? 0xff80ff80u : 0xff800000u;               // -inf
 #pragma unroll
-  for (int i = 0; i < kLoads; ++i)
-    if (token(i * kGroup + kGroup - 1) < a.V) raw[i] = *reinterpret_cast<const uint4*>(z0 + i * kBeamThreads * 16);
+  for (int i = 0; i < kBeamLoads; ++i) {
+    raw[i] = u32x4{none, none, none, none};
+    if (first + beam_place<kGroup>(i * kGroup) + kGroup <= a.V) raw[i] = *reinterpret_cast<const u32x4*>(z0 + i * kBeamThreads * 16);
+  }
+  if (chunk == a.chunks - 1 && a.V % kGroup != 0) {      // the row's last group, in part
 #pragma unroll
-  for (int i = 0; i < kLoads; ++i) {
-    const uint32_t u[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
+    for (int i = 0; i < kBeamLoads; ++i) {
+      const int left = a.V - (first + beam_place<kGroup>(i * kGroup));
+      if (left > 0 && left < kGroup) {
 #pragma unroll
-    for (int j = 0; j < kGroup; ++j) {
-      const int e = i * kGroup + j;
-      const uint32_t bits = BF16 ? (j & 1 ? u[j / 2] & 0xffff0000u : u[j / 2] << 16) : u[j];
-      z[e] = token(i * kGroup + kGroup - 1) < a.V ? __builtin_bit_cast(float, bits) : -INFINITY;
-    }
-    if (token(i * kGroup) < a.V && token(i * kGroup + kGroup - 1) >= a.V) {              // the row's last group, in part
-#pragma unroll
-      for (int j = 0; j < kGroup; ++j) {
-        const char* at = z0 + i * kBeamThreads * 16 + j * (BF16 ? 2 : 4);
-        if (token(i * kGroup + j) < a.V)
-          z[i * kGroup + j] = BF16 ? __builtin_bit_cast(float, (uint32_t)*reinterpret_cast<const uint16_t*>(at) << 16)
-                                   : *reinterpret_cast<const float*>(at);
+        for (int j = 0; j < kGroup; ++j)
+          if (j < left) {
+            const char* at = z0 + i * kBeamThreads * 16 + j * (BF16 ? 2 : 4);
+            if constexpr (BF16) raw[i][j / 2] = (raw[i][j / 2] & (j & 1 ? 0xffffu : 0xffff0000u)) | (uint32_t)*reinterpret_cast<const uint16_t*>(at) << (j & 1 ? 16 : 0);
+            else raw[i][j] = *reinterpret_cast<const uint32_t*>(at);
+          }
       }
     }
   }
-  float m = z[0];
+  auto value = [&](int e) { return beam_logit<kGroup>(raw, e); };
+  // (else the compiler keeps all logits unpacked from one pass to the next)
+  auto hide = [&]() {
 #pragma unroll
-  for (int e = 1; e < kBeamEach; ++e) m = fmaxf(m, z[e]);
-  lane_max[t] = ordered(fmaxf(m, -INFINITY));            // (a lane of NaNs alone)
-  for (int d = 32; d; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
-  if (lane == 0) wave_max[w] = fmaxf(m, -INFINITY);
+    for (int i = 0; i < kBeamLoads; ++i) asm volatile("" : "+v"(raw[i]));
+  };
+  // Each load's largest, and the lane's.  (fmaxf drops NaNs: they show in the sum.)
+  float best[kBeamLoads], m;
+#pragma unroll
+  for (int i = 0; i < kBeamLoads; ++i) {
+    best[i] = -INFINITY;
+    if constexpr (BF16) {
+      // Bits of bf16 from 0 on order like whole numbers, and any below 0 is less: two at a time.
+      s16x2 top = __builtin_bit_cast(s16x2, 0x80008000u);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const uint32_t two = raw[i][j];                  // (a bit_cast of raw[i][j] itself is one of raw[i][0])
+        top = __builtin_elementwise_max(top, __builtin_bit_cast(s16x2, two));
+      }
+      const int one = max((int)top[0], (int)top[1]);
+      best[i] = __builtin_bit_cast(float, (uint32_t)one << 16);
+      if (one < 0 || one > 0x7f80) {                     // nothing from 0 on, or a NaN
+        best[i] = -INFINITY;
+#pragma unroll
+        for (int j = 0; j < kGroup; ++j) best[i] = fmaxf(best[i], value(i * kGroup + j));
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < kGroup; ++j) best[i] = fmaxf(best[i], value(i * kGroup + j));
+    }
+    m = i ? fmaxf(m, best[i]) : best[i];
+  }
+  // The wave's n/4-th largest maximum of a lane, by its leading bits: of four waves, the smallest is at most the n-th largest logit.
+  const uint32_t lane_max = ordered(m);
+  uint32_t least_of_wave = 0;
+  const int wanted = (a.n + kBeamWaves - 1) / kBeamWaves;
+  for (int bit = 31; bit >= 16; --bit) {
+    const uint32_t up = least_of_wave | 1u << bit;
+    if (__popcll(__ballot(lane_max >= up)) >= wanted) least_of_wave = up;
+  }
+  const uint32_t largest = dpp_scan_max_u32(lane_max);
+  if (lane == 63) {
+    wave_max[w] = unordered(largest);
+    wave_least[w] = least_of_wave;
+  }
   if (t == 0) count = 0;
   __syncthreads();
-  // The n-th largest of the lanes' maxima is at most the n-th largest logit: by its leading bits, from wave 0 alone.
-  if (w == 0) {
-    const uint4 k = reinterpret_cast<const uint4*>(lane_max)[lane];
-    uint32_t at = 0;
-    for (int bit = 31; bit >= 12; --bit) {
-      const uint32_t up = at | 1u << bit;
-      const int n = __popcll(__ballot(k.x >= up)) + __popcll(__ballot(k.y >= up)) + __popcll(__ballot(k.z >= up)) +
-                    __popcll(__ballot(k.w >= up));
-      if (n >= a.n) at = up;
-    }
-    if (lane == 0) least = at < 0x00800000u ? -3.402823466e38f : unordered(at);          // (-inf is no continuation)
-  }
   m = fmaxf(fmaxf(wave_max[0], wave_max[1]), fmaxf(wave_max[2], wave_max[3]));
-  const float base = m == -INFINITY ? 0.0f : m;
-  float s[2] = {0.0f, 0.0f};
+  const uint32_t least = min(min(wave_least[0], wave_least[1]), min(wave_least[2], wave_least[3]));
+  const float from = least < 0x00800000u ? -3.402823466e38f : unordered(least);          // (-inf is no continuation)
+  // My logits from the bound on go to the list: counted first, so that nothing waits for a place.
+  int mine = 0;
 #pragma unroll
-  for (int e = 0; e < kBeamEach; ++e) {
-    const float d = z[e] - base;
-    s[e & 1] += __builtin_amdgcn_exp2f(__builtin_fmaf(d, a.c_lo, d * a.c_hi));
+  for (int i = 0; i < kBeamLoads; ++i)
+    if (best[i] >= from) {
+#pragma unroll
+      for (int j = 0; j < kGroup; ++j) mine += value(i * kGroup + j) >= from;
+    }
+  const int upto = (int)dpp_scan_add_u32((uint32_t)mine);
+  int place = 0;
+  if (lane == 63) place = atomicAdd(&count, upto);
+  // Meanwhile the sum.  2^(c z - c max) with c rounded to 24 bits, 2^-25 of the exponent off at most.
+  const float base = m == -INFINITY ? 0.0f : m, top = base * a.c;
+  float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+  hide();
+  if (fabsf(top) < 3e38f) {
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) {
+      s[e & 3] += __builtin_amdgcn_exp2f(__builtin_fmaf(value(e), a.c, -top));
+      if (e % 8 == 7) __builtin_amdgcn_sched_barrier(0);
+    }
+  } else {                                               // (a row of the lowest values, or +inf)
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) {
+      s[e & 3] += __builtin_amdgcn_exp2f((value(e) - base) * a.c);
+      if (e % 8 == 7) __builtin_amdgcn_sched_barrier(0);
+    }
   }
-  double sum = (double)s[0] + (double)s[1];
-  for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
-  if (lane == 0) wave_sum[w] = sum;
+  hide();
+  place = __builtin_amdgcn_readlane(place, 63) + upto - mine;
+#pragma unroll
+  for (int i = 0; i < kBeamLoads; ++i)
+    if (best[i] >= from) {
+#pragma unroll
+      for (int j = 0; j < kGroup; ++j) {
+        const int e = i * kGroup + j;
+        if (value(e) >= from) {
+          if (place < kBeamList) list[place] = list_entry(value(e), t * kGroup + beam_place<kGroup>(e));
+          ++place;
+        }
+      }
+    }
+  const double sum = wave_total(((double)s[0] + (double)s[1]) + ((double)s[2] + (double)s[3]));
+  if (lane == 63) wave_sum[w] = sum;
   __syncthreads();
   if (t == 0) {
     BeamPart p;
@@ -137,51 +307,21 @@ __global__ __launch_bounds__(kBeamThreads) void beam_chunk_kernel(BeamArgs a) {
     p.pad = 0.0f;
     a.part[blockIdx.x] = p;
   }
-  const float from = least;
-#pragma unroll
-  for (int e = 0; e < kBeamEach; ++e) {
-    if (z[e] >= from) {
-      const int at = atomicAdd(&count, 1);
-      if (at < kBeamList) list[at] = beam_key(z[e], token(e));
-    }
-  }
-  __syncthreads();
   int listed = count;
-  if (listed > kBeamList) {
-    // Thousands of nearly equal logits: the n-th largest key, bit by bit, over all of them.
-    unsigned long long at = 0;
-    for (int bit = 63; bit >= 0; --bit) {
-      const unsigned long long up = at | 1ull << bit;
-      int n = 0;
-#pragma unroll
-      for (int e = 0; e < kBeamEach; ++e) n += z[e] >= from && beam_key(z[e], token(e)) >= up;
-      for (int d = 32; d; d >>= 1) n += __shfl_xor(n, d);
-      __syncthreads();
-      if (lane == 0) lane_max[w] = n;
-      __syncthreads();
-      if ((int)(lane_max[0] + lane_max[1] + lane_max[2] + lane_max[3]) >= a.n) at = up;
-    }
-    __syncthreads();
-    if (t == 0) count = 0;
-    __syncthreads();
-#pragma unroll
-    for (int e = 0; e < kBeamEach; ++e)
-      if (z[e] >= from && beam_key(z[e], token(e)) >= at) list[atomicAdd(&count, 1)] = beam_key(z[e], token(e));
-    __syncthreads();
-    listed = count;
-  }
+  if (listed > kBeamList) listed = select_apart<kGroup>(raw, list, count, wave_n, from, a.n);
   unsigned long long* out = a.cand + (long long)blockIdx.x * a.n;
   for (int i = t; i < listed; i += kBeamThreads) {
-    const unsigned long long mine = list[i];
+    const double mine = list[i];
     int rank = 0;
+#pragma unroll 8
     for (int j = 0; j < listed; ++j) rank += list[j] > mine;
-    if (rank < a.n) out[rank] = mine;
+    if (rank < a.n) out[rank] = entry_key(mine, chunk * a.chunk);
   }
   for (int i = listed + t; i < a.n; i += kBeamThreads) out[i] = 0;
 }
 
 // A continuation among those of its group: the larger pair comes first.
-struct BeamRank { unsigned long long total, rest; };
+struct __align__(16) BeamRank { unsigned long long total, rest; };
 __device__ inline bool operator>(const BeamRank& x, const BeamRank& y) {
   return x.total > y.total || (x.total == y.total && x.rest > y.rest);
 }
@@ -193,122 +333,209 @@ __device__ inline int rest_token(unsigned long long rest) { return (int)(0xfffff
 __device__ inline float rest_logit(unsigned long long rest) { return unordered((uint32_t)(rest >> 20)); }
 static_assert(SIP_MAX_V <= 0xfffff && SIP_MAX_BEAMS <= 1 << 12, "beam_rest() holds a beam, a logit and a token");
 
-// Room for LISTS heads, and for what the selected lists hold at most: of the list with the r-th best head entries r + e < n.
-constexpr int merge_room(int lists, int n) { return lists > n * (n + 1) / 2 ? lists : n * (n + 1) / 2; }
+// The group's rows, in LDS.
+struct BeamGroup {
+  double lse[SIP_MAX_BEAMS];
+  float score[SIP_MAX_BEAMS], scale[SIP_MAX_BEAMS];
+  int what[SIP_MAX_BEAMS];
+};
+template <int THREADS>
+__device__ inline void load_group(const BeamArgs& a, BeamGroup& rows) {
+  const int t = threadIdx.x, lane = t & 63, w = t >> 6, K = a.width, S = a.chunks, row0 = blockIdx.x * K;
+  // As many rows a wave as have room for their chunks, a lane each.
+  int lanes = 1;
+  while (lanes < S) lanes *= 2;
+  const int at_once = 64 / lanes, mine = lane / lanes, chunk = lane % lanes;
+  for (int k0 = w * at_once; k0 < K; k0 += THREADS / 64 * at_once) {
+    const int k = k0 + mine;
+    BeamPart p = {0.0, -INFINITY, 0.0f};
+    BeamRowInfo row = {0.0f, 0.0f, kBeamNone};
+    if (k < K) {
+      if (chunk < S) p = a.part[(long long)(row0 + k) * S + chunk];       // (of a row that is not live: anything)
+      row = beam_row(a, row0 + k);
+    }
+    float top = p.max;
+    for (int d = 1; d < lanes; d <<= 1) top = fmaxf(top, __shfl_xor(top, d));
+    double s = p.max > -INFINITY ? p.sum * exp2(((double)p.max - (double)top) * (double)a.c) : p.sum;
+    for (int d = 1; d < lanes; d <<= 1) s += __shfl_xor(s, d);
+    if (k < K && chunk == 0) {
+      rows.lse[k] = (double)top * a.scale + log(s);
+      rows.score[k] = row.score;
+      rows.scale[k] = row.scale;
+      // (NaN or +inf somewhere, or nothing but -inf: no continuation)
+      rows.what[k] = row.what == kBeamLive && !(s > 0.0 && isfinite(s) && isfinite(top)) ? (int)kBeamNone : row.what;
+    }
+  }
+}
+__device__ inline double total_of(const BeamArgs& a, const BeamGroup& rows, int k, float z) {
+  return (double)rows.score[k] + ((double)z * a.scale - rows.lse[k]);
+}
+// Entry e of list l (of beam l / chunks), whose key is `key`; total 0: there is none.
+__device__ inline BeamRank rank_of(const BeamArgs& a, const BeamGroup& rows, int l, int e, unsigned long long key) {
+  const int k = l / a.chunks, what = rows.what[k];
+  if (what == kBeamLive && key) return {ordered64(total_of(a, rows, k, key_logit(key)) * (double)rows.scale[k]), beam_rest(k, key)};
+  if (what == kBeamFinished && l == k * a.chunks && e == 0)
+    return {ordered64((double)rows.score[k] * (double)rows.scale[k]), beam_rest(k, beam_key(0.0f, a.end_token))};
+  return {0, 0};
+}
 
-// One workgroup a group.  The lists are in order, so the n-th best of their heads bounds what can be selected, and a list whose
-// head is the r-th best can give its n - r first entries at most.
-template <int ROOM>
-__global__ __launch_bounds__(kMergeThreads) void beam_merge_kernel(BeamArgs a) {
-  __shared__ BeamRank found[ROOM];
-  __shared__ double lse[SIP_MAX_BEAMS];
-  __shared__ float score[SIP_MAX_BEAMS], scale[SIP_MAX_BEAMS];
-  __shared__ int what[SIP_MAX_BEAMS], chosen[SIP_MAX_CONTINUATIONS], wave_n[2][kMergeThreads / 64], count, lists_chosen;
-  const int g = blockIdx.x, t = threadIdx.x, lane = t & 63, w = t >> 6, K = a.width, S = a.chunks, n = a.n;
-  const int lists = K * S, row0 = g * K;
-  if (t < K) {
-    what[t] = beam_row(a, row0 + t);
-    score[t] = a.scores[row0 + t];
-    scale[t] = a.rank_scale ? a.rank_scale[row0 + t] : 1.0f;
-  }
-  if (t == 0) count = lists_chosen = 0;
-  __syncthreads();
-  for (int k = w; k < K; k += kMergeThreads / 64) {
-    if (what[k] != kBeamLive) continue;
-    const BeamPart* part = a.part + (long long)(row0 + k) * S;
-    float m = -INFINITY;
-    double s = 0.0;
-    if (lane < S) { m = part[lane].max; s = part[lane].sum; }
-    float top = m;
-    for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
-    if (m > -INFINITY) s *= exp2(((double)m - (double)top) * ((double)a.c_hi + (double)a.c_lo));
-    for (int d = 32; d; d >>= 1) s += __shfl_xor(s, d);
-    if (lane == 0) {
-      lse[k] = (double)top * a.scale + log(s);
-      if (!isfinite(s) || !(s > 0.0) || !isfinite(top)) what[k] = kBeamNone;     // NaN or +inf somewhere, or nothing but -inf
-    }
-  }
-  __syncthreads();
-  // Entry e of list l (of beam l / S); total = 0: there is none.
-  auto total_of = [&](int k, float z) { return (double)score[k] + ((double)z * a.scale - lse[k]); };
-  auto entry = [&](int l, int e) {
-    const int k = l / S;
-    BeamRank r = {0, 0};
-    if (what[k] == kBeamLive) {
-      const unsigned long long key = a.cand[((long long)row0 * S + l) * n + e];
-      if (key) r = {ordered64(total_of(k, key_logit(key)) * (double)scale[k]), beam_rest(k, key)};
-    } else if (what[k] == kBeamFinished && l == k * S && e == 0) {
-      r = {ordered64((double)score[k] * (double)scale[k]), beam_rest(k, beam_key(0.0f, a.end_token))};
-    }
-    return r;
-  };
-  constexpr int kHeads = SIP_MAX_BEAMS * 64 / kMergeThreads;
-  uint32_t head[kHeads];
+// The leading bits of the n-th largest of the workgroup's values, EACH a lane: two bits a turn, of which votes[turn] counts the values
+// that reach the three possibilities (zeros before; a barrier a turn).
+constexpr int kVoteTurns = 12;
+typedef int BeamVotes[kVoteTurns][4];
+template <int EACH>
+__device__ inline uint32_t nth_largest(const uint32_t (&x)[EACH], int n, BeamVotes& votes) {
+  const int lane = threadIdx.x & 63;
+  uint32_t from = 0;
+  for (int turn = 0; turn < kVoteTurns; ++turn) {
+    const int bit = 30 - 2 * turn;
+    int mine[3] = {0, 0, 0};
 #pragma unroll
-  for (int i = 0; i < kHeads; ++i) {
-    const int l = t + i * kMergeThreads;
-    head[i] = l < lists ? (uint32_t)(entry(l, 0).total >> 32) : 0;
-  }
-  uint32_t from = 0;                                     // the leading bits of the n-th best head
-  for (int bit = 31, side = 0; bit >= 8; --bit, side ^= 1) {
-    const uint32_t up = from | 1u << bit;
-    int mine = 0;
+    for (int i = 0; i < EACH; ++i)
 #pragma unroll
-    for (int i = 0; i < kHeads; ++i) mine += __popcll(__ballot(head[i] >= up));
-    if (lane == 0) wave_n[side][w] = mine;
+      for (int j = 0; j < 3; ++j) mine[j] += __popcll(__ballot(x[i] >= (from | (uint32_t)(j + 1) << bit)));
+    if (lane < 3 && mine[0]) atomicAdd(&votes[turn][lane], lane == 0 ? mine[0] : lane == 1 ? mine[1] : mine[2]);
     __syncthreads();
-    int all = 0;
-#pragma unroll
-    for (int j = 0; j < kMergeThreads / 64; ++j) all += wave_n[side][j];
-    if (all >= n) from = up;
-    if (all == n) break;
+    const int4 all = *reinterpret_cast<const int4*>(votes[turn]);
+    const int step = (all.x >= n) + (all.y >= n) + (all.z >= n);
+    from |= (uint32_t)step << bit;
+    if (step && (step == 1 ? all.x : step == 2 ? all.y : all.z) == n) break;
   }
-  if (from == 0) from = 1;                               // (fewer than n lists: every one that has an entry)
-  __syncthreads();
-#pragma unroll
-  for (int i = 0; i < kHeads; ++i) {
-    const int l = t + i * kMergeThreads;
-    if (head[i] >= from) found[atomicAdd(&count, 1)] = {entry(l, 0).total, entry(l, 0).rest};
-  }
-  __syncthreads();
-  const int heads = count;
-  // their order, and their lists' numbers by it
-  for (int i = t; i < heads; i += kMergeThreads) {
-    const BeamRank mine = found[i];
-    int rank = 0;
-    for (int j = 0; j < heads; ++j) rank += found[j] > mine;
-    if (rank < n) {
-      const int k = rest_beam(mine.rest);
-      chosen[rank] = k * S + (what[k] == kBeamFinished ? 0 : rest_token(mine.rest) / kBeamChunk);
-      atomicAdd(&lists_chosen, 1);
+  return from ? from : 1;                                // (fewer than n: all that there are)
+}
+
+// f(rank, i) for each of n entries, i's place among them; `ranks` for up to kRanked.  Begins and ends with the entries visible to all.
+constexpr int kRanked = 1024;
+template <int THREADS, class F>
+__device__ inline void rank_all(const BeamRank* found, int n, int* ranks, F f) {
+  const int t = threadIdx.x;
+  if (n <= kRanked / 2) {
+    // several threads an entry: each compares it with a part of the others
+    int wide = 32;
+    while (wide < n) wide *= 2;
+    const int parts = max(1, THREADS / wide), part = t / wide;   // (wide > THREADS: one part, several entries a thread)
+    for (int i = t; i < n; i += THREADS) ranks[i] = 0;
+    __syncthreads();
+    for (int i = t % wide; i < n; i += min(wide, THREADS)) {
+      const BeamRank mine = found[i];
+      int rank = 0;
+      for (int j = part; j < n; j += parts) rank += found[j] > mine;
+      if (rank) atomicAdd(&ranks[i], rank);
+    }
+    __syncthreads();
+    for (int i = t; i < n; i += THREADS) f(ranks[i], i);
+  } else {
+    for (int i = t; i < n; i += THREADS) {
+      const BeamRank mine = found[i];
+      int rank = 0;
+      for (int j = 0; j < n; ++j) rank += found[j] > mine;
+      f(rank, i);
     }
   }
   __syncthreads();
+}
+
+__device__ inline void store_selected(const BeamArgs& a, const BeamGroup& rows, const BeamRank& x, int rank) {
+  if (rank >= a.n) return;
+  const int k = rest_beam(x.rest), at = blockIdx.x * a.n + rank;
+  a.tokens[at] = rest_token(x.rest);
+  a.parents[at] = k;
+  a.out_scores[at] = rows.what[k] == kBeamFinished ? rows.score[k] : (float)total_of(a, rows, k, rest_logit(x.rest));
+}
+__device__ inline void store_missing(const BeamArgs& a, int kept) {
+  for (int i = kept + threadIdx.x; i < a.n; i += blockDim.x) {
+    const int at = blockIdx.x * a.n + i;
+    a.tokens[at] = a.parents[at] = -1;
+    a.out_scores[at] = -INFINITY;
+  }
+}
+
+// A group whose lists have up to kMergeFew entries together: all of them in registers.
+constexpr int kMergeFew = 1024;
+__global__ __launch_bounds__(256) void beam_merge_few_kernel(BeamArgs a) {
+  constexpr int kEach = kMergeFew / 256;
+  __shared__ BeamGroup rows;
+  __shared__ BeamRank found[kMergeFew];
+  __shared__ int ranks[kRanked], count;
+  __shared__ __align__(16) BeamVotes votes;
+  const int t = threadIdx.x, entries = a.width * a.chunks * a.n;
+  const unsigned long long* cand = a.cand + (long long)blockIdx.x * entries;
+  unsigned long long key[kEach];
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) key[i] = t + i * 256 < entries ? cand[t + i * 256] : 0;
+  if (t == 0) count = 0;
+  if (t < kVoteTurns * 4) votes[t / 4][t % 4] = 0;
+  load_group<256>(a, rows);
+  __syncthreads();
+  BeamRank x[kEach];
+  uint32_t lead[kEach];
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) {
+    const int at = t + i * 256;
+    x[i] = {0, 0};
+    if (at < entries) x[i] = rank_of(a, rows, at / a.n, at % a.n, key[i]);
+    lead[i] = (uint32_t)(x[i].total >> 32);
+  }
+  const uint32_t from = nth_largest(lead, a.n, votes);
+#pragma unroll
+  for (int i = 0; i < kEach; ++i)
+    if (lead[i] >= from) found[atomicAdd(&count, 1)] = x[i];
+  __syncthreads();
+  const int kept = count;
+  rank_all<256>(found, kept, ranks, [&](int rank, int i) { store_selected(a, rows, found[i], rank); });
+  store_missing(a, kept);
+}
+
+// Any group.  The lists are in order, so the n-th best of their heads bounds what can be selected, and a list whose head is the
+// r-th best can give its n - r first entries at most.
+constexpr int kMergeThreads = 1024;
+constexpr int kMergeLists = SIP_MAX_BEAMS * 64;
+constexpr int kMergeRoom = SIP_MAX_CONTINUATIONS * (SIP_MAX_CONTINUATIONS + 1) / 2;
+static_assert(kMergeRoom >= kMergeLists, "room for all heads");
+__global__ __launch_bounds__(kMergeThreads) void beam_merge_kernel(BeamArgs a) {
+  constexpr int kHeads = kMergeLists / kMergeThreads;
+  __shared__ BeamGroup rows;
+  __shared__ BeamRank found[kMergeRoom];
+  __shared__ int ranks[kRanked], chosen[SIP_MAX_CONTINUATIONS], count;
+  __shared__ __align__(16) BeamVotes votes;
+  const int t = threadIdx.x, S = a.chunks, n = a.n, lists = a.width * S;
+  const unsigned long long* cand = a.cand + (long long)blockIdx.x * lists * n;
+  unsigned long long key[kHeads];
+#pragma unroll
+  for (int i = 0; i < kHeads; ++i) key[i] = t + i * kMergeThreads < lists ? cand[(long long)(t + i * kMergeThreads) * n] : 0;
+  if (t == 0) count = 0;
+  if (t < kVoteTurns * 4) votes[t / 4][t % 4] = 0;
+  load_group<kMergeThreads>(a, rows);
+  __syncthreads();
+  uint32_t lead[kHeads];
+#pragma unroll
+  for (int i = 0; i < kHeads; ++i) {
+    const int l = t + i * kMergeThreads;
+    lead[i] = l < lists ? (uint32_t)(rank_of(a, rows, l, 0, key[i]).total >> 32) : 0;
+  }
+  const uint32_t from = nth_largest(lead, n, votes);
+#pragma unroll
+  for (int i = 0; i < kHeads; ++i)
+    if (lead[i] >= from) found[atomicAdd(&count, 1)] = rank_of(a, rows, t + i * kMergeThreads, 0, key[i]);
+  __syncthreads();
+  const int heads = count, selected = min(heads, n);
+  rank_all<kMergeThreads>(found, heads, ranks, [&](int rank, int i) {
+    const unsigned long long rest = found[i].rest;
+    const int k = rest_beam(rest);
+    if (rank < n) chosen[rank] = k * S + (rows.what[k] == kBeamFinished ? 0 : rest_token(rest) / a.chunk);
+  });
   if (t == 0) count = 0;
   __syncthreads();
-  const int pairs = lists_chosen * n;
-  for (int i = t; i < pairs; i += kMergeThreads) {
+  for (int i = t; i < selected * n; i += kMergeThreads) {
     const int r = i / n, e = i % n;
     if (r + e >= n) continue;
-    const BeamRank x = entry(chosen[r], e);
+    const BeamRank x = rank_of(a, rows, chosen[r], e, cand[(long long)chosen[r] * n + e]);
     if (x.total >> 32 >= from) found[atomicAdd(&count, 1)] = x;
   }
   __syncthreads();
   const int kept = count;
-  for (int i = t; i < kept; i += kMergeThreads) {
-    const BeamRank mine = found[i];
-    int rank = 0;
-    for (int j = 0; j < kept; ++j) rank += found[j] > mine;
-    if (rank >= n) continue;
-    const int k = rest_beam(mine.rest), at = g * n + rank;
-    a.tokens[at] = rest_token(mine.rest);
-    a.parents[at] = k;
-    a.out_scores[at] = what[k] == kBeamFinished ? score[k] : (float)total_of(k, rest_logit(mine.rest));
-  }
-  for (int i = kept + t; i < n; i += kMergeThreads) {
-    a.tokens[g * n + i] = a.parents[g * n + i] = -1;
-    a.out_scores[g * n + i] = -INFINITY;
-  }
+  rank_all<kMergeThreads>(found, kept, ranks, [&](int rank, int i) { store_selected(a, rows, found[i], rank); });
+  store_missing(a, kept);
 }
 
 // ---------------------------------------------------------------- reordering of a state
@@ -321,15 +548,23 @@ struct ReorderArgs {
   int token_blocks;                                      // of 4 KB of a slot's token row; the table has eight more
 };
 
-// Where row k of a group takes its history from: its own slot and its parent's (-1: an empty history).  to < 0: nothing moves.
+// Where a row takes its history from: its parent's slot (-1: an empty history) and its own.  to < 0: nothing moves.  For the first
+// a.width threads, a row each; `slot` is LDS that nobody uses until the next barrier.
 struct Move { int from, to; };
-__device__ inline Move move_of(const ReorderArgs& a, int row0, int k) {
-  const int p = a.parents[row0 + k], to = a.slot_of_row[row0 + k];
+__device__ inline Move move_of(const ReorderArgs& a, int group, int* slot) {
+  const int k = threadIdx.x, row = group * a.width + k;
+  int p = -1, to = -1;
+  if (k < a.width) {
+    p = a.parents[row];
+    to = a.slot_of_row[row];
+    slot[k] = to;
+  }
+  __syncthreads();
   if ((unsigned)p >= (unsigned)a.width || (unsigned)to >= (unsigned)a.slots) return {-1, -1};
-  for (int j = 0; j < k; ++j)
-    if (a.slot_of_row[row0 + j] == to) return {-1, -1};  // an earlier row's
-  const int from = a.slot_of_row[row0 + p];
-  return {(unsigned)from < (unsigned)a.slots ? from : -1, to};
+  bool taken = false;                                    // an earlier row's
+  for (int j = 0; j < k; ++j) taken |= slot[j] == to;
+  const int from = slot[p];
+  return {(unsigned)from < (unsigned)a.slots ? from : -1, taken ? -1 : to};
 }
 __device__ inline int length_of(const ReorderArgs& a, int slot) {
   return slot < 0 ? 0 : min(max(a.len[slot], 0), a.L_max);
@@ -345,14 +580,14 @@ constexpr int kReorderThreads = 256;
 template <int WIDTH>
 __global__ __launch_bounds__(kReorderThreads) void state_reorder_kernel(ReorderArgs a) {
   __shared__ Move move[WIDTH];
-  __shared__ int keep[WIDTH];                            // tokens that move; a valid table
+  __shared__ int slot[WIDTH], keep[WIDTH];               // tokens that move
   const int blocks = a.token_blocks + 8, g = blockIdx.x / blocks, block = blockIdx.x % blocks, t = threadIdx.x;
   const bool table = block >= a.token_blocks;
+  Move m = move_of(a, g, slot);
   if (t < a.width) {
-    Move m = move_of(a, g * a.width, t);
     if (m.from == m.to) m.to = -1;
     move[t] = m;
-    keep[t] = table ? (m.from < 0 || a.ndist[m.from] >= 0) : length_of(a, m.from);
+    if (!table) keep[t] = length_of(a, m.from);
   }
   __syncthreads();
   StateLine x[WIDTH];
@@ -361,40 +596,39 @@ __global__ __launch_bounds__(kReorderThreads) void state_reorder_kernel(ReorderA
   for (int k = 0; k < WIDTH; ++k) {
     if (k >= a.width || move[k].to < 0) continue;
     const long long from = move[k].from;
-    if (!table) {
-      if (column < keep[k]) x[k] = *reinterpret_cast<const StateLine*>(a.tokens + from * a.L_max + column);
-    } else if (keep[k]) {
+    if (table) {
       if (from >= 0) x[k] = *reinterpret_cast<const StateLine*>(a.table + from * (2 * kTableSlots) + column);
       else
         for (int j = 0; j < 4; ++j) x[k].w[j] = column < kTableSlots ? kTableEmpty : 0u;
+    } else if (column < keep[k]) {
+      x[k] = *reinterpret_cast<const StateLine*>(a.tokens + from * a.L_max + column);
     }
   }
 #pragma unroll
   for (int k = 0; k < WIDTH; ++k) {
     if (k >= a.width || move[k].to < 0) continue;
     const long long to = move[k].to;
-    if (!table) {
+    if (table) {
+      *reinterpret_cast<StateLine*>(a.table + to * (2 * kTableSlots) + column) = x[k];
+    } else {
       int* out = a.tokens + to * a.L_max + column;
       if (column + 4 <= keep[k]) *reinterpret_cast<StateLine*>(out) = x[k];
       else
         for (int j = 0; j < 4; ++j)
           if (column + j < keep[k]) out[j] = (int)x[k].w[j];
-    } else if (keep[k]) {
-      *reinterpret_cast<StateLine*>(a.table + to * (2 * kTableSlots) + column) = x[k];
     }
   }
 }
 
 // One wave a group, behind the copies: lengths and numbers of distinct tokens, all read before any is written, and the new tokens.
 __global__ __launch_bounds__(64) void state_reorder_append_kernel(ReorderArgs a) {
-  const int row0 = blockIdx.x * a.width, k = threadIdx.x;
-  Move m = {-1, -1};
-  int n = 0, nd = 0, token = -1;
-  if (k < a.width) {
-    m = move_of(a, row0, k);
+  __shared__ int slot[64];
+  const int token = (int)threadIdx.x < a.width && a.new_tokens ? a.new_tokens[blockIdx.x * a.width + threadIdx.x] : -1;
+  const Move m = move_of(a, blockIdx.x, slot);
+  int n = 0, nd = 0;
+  if (m.to >= 0 && m.from >= 0) {
     n = length_of(a, m.from);
-    if (m.from >= 0) nd = a.ndist[m.from];
-    if (a.new_tokens) token = a.new_tokens[row0 + k];
+    nd = a.ndist[m.from];
   }
   __syncthreads();
   if (m.to < 0) return;

@@ -21,7 +21,6 @@ struct CodesArgs {
 };
 
 // The largest of each half of `x` over the GROUP / 8 lanes of a group, by exchange of neighbours, pairs, quads and eights.
-typedef int16_t s16x2 __attribute__((ext_vector_type(2)));
 template <int GROUP>
 __device__ inline s16x2 group_max(s16x2 x) {
   auto with = [&](auto pattern) {

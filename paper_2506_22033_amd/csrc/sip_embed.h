@@ -50,34 +50,61 @@ struct EmbedArgs {
   const uint8_t* codes; long long codes_stride;          // nullptr: weight
   const void* scales; int scales_bf16;
   const uint8_t* zeros;
-  int group;
+  int group_shift;                                       // log2 of a group's entries
   int V, D, N;
   const int* ids;
   float scale;
   void* out; long long out_stride; int out_bf16;
 };
 
-// A lane takes eight neighbours of a row.
-template <bool CODES>
+// A lane takes eight neighbours of a row, or of kEmbedAhead rows, all under way at once.
+template <bool CODES, int kEmbedAhead>
 __global__ __launch_bounds__(256) void embed_kernel(EmbedArgs a) {
-  const long long per_row = a.D / 8, total = per_row * a.N;
-  for (long long u = blockIdx.x * 256ll + threadIdx.x; u < total; u += gridDim.x * 256ll) {
-    const int i = (int)(u / per_row), c = (int)(u - i * per_row) * 8, v = a.ids[i];
-    f32x8 f = {0, 0, 0, 0, 0, 0, 0, 0};
-    if ((unsigned)v < (unsigned)a.V) {
-      if constexpr (CODES) {
-        const uint32_t q = *reinterpret_cast<const uint32_t*>(a.codes + v * a.codes_stride + c / 2);
-        const long long at = (long long)v * (a.D / a.group) + c / a.group;
-        const float s = a.scales_bf16 ? (float)static_cast<const __bf16*>(a.scales)[at] : static_cast<const float*>(a.scales)[at];
-        const int zero = a.zeros ? a.zeros[at] : 8;
+  const uint32_t per_row = a.D / 8, total = per_row * (uint32_t)a.N;                        // (up to 2^31)
+  const uint32_t u0 = blockIdx.x * (kEmbedAhead * 256) + threadIdx.x;
+  int v[kEmbedAhead], c[kEmbedAhead];
+  long long to[kEmbedAhead];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) f[e] = (float)((int)(q >> 4 * e & 15) - zero) * s;
-      } else {
-        f = as_floats(load_eight(a.weight, v * a.weight_stride + c, a.weight_bf16), a.weight_bf16);
-      }
-      f *= a.scale;
+  for (int j = 0; j < kEmbedAhead; ++j) {
+    const uint32_t u = u0 + j * 256, i = u / per_row;
+    c[j] = (int)(u - i * per_row) * 8;
+    to[j] = u < total ? i * a.out_stride + c[j] : -1;
+    v[j] = u < total ? a.ids[i] : -1;
+  }
+  if constexpr (CODES) {
+    uint32_t q[kEmbedAhead];
+    float s[kEmbedAhead];
+    int zero[kEmbedAhead];
+#pragma unroll
+    for (int j = 0; j < kEmbedAhead; ++j) {
+      q[j] = 0; s[j] = 0.0f; zero[j] = 8;
+      if ((unsigned)v[j] >= (unsigned)a.V) continue;
+      const long long at = (long long)v[j] * (a.D >> a.group_shift) + (c[j] >> a.group_shift);
+      q[j] = *reinterpret_cast<const uint32_t*>(a.codes + v[j] * a.codes_stride + c[j] / 2);
+      s[j] = a.scales_bf16 ? (float)static_cast<const __bf16*>(a.scales)[at] : static_cast<const float*>(a.scales)[at];
+      if (a.zeros) zero[j] = a.zeros[at];
     }
-    store_eight(a.out, i * a.out_stride + c, a.out_bf16, f);
+#pragma unroll
+    for (int j = 0; j < kEmbedAhead; ++j) {
+      f32x8 f;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) f[e] = (float)((int)(q[j] >> 4 * e & 15) - zero[j]) * s[j] * a.scale;
+      if ((unsigned)v[j] >= (unsigned)a.V) f = f32x8{0, 0, 0, 0, 0, 0, 0, 0};
+      if (to[j] >= 0) store_eight(a.out, to[j], a.out_bf16, f);
+    }
+  } else {
+    Eight x[kEmbedAhead];
+#pragma unroll
+    for (int j = 0; j < kEmbedAhead; ++j) {
+      x[j] = Eight{};
+      if ((unsigned)v[j] < (unsigned)a.V) x[j] = load_eight(a.weight, v[j] * a.weight_stride + c[j], a.weight_bf16);
+    }
+#pragma unroll
+    for (int j = 0; j < kEmbedAhead; ++j) {
+      f32x8 f = as_floats(x[j], a.weight_bf16) * a.scale;
+      if ((unsigned)v[j] >= (unsigned)a.V) f = f32x8{0, 0, 0, 0, 0, 0, 0, 0};            // (whatever the scale)
+      if (to[j] >= 0) store_eight(a.out, to[j], a.out_bf16, f);
+    }
   }
 }
 

@@ -1,19 +1,17 @@
 // Host side of the entry points declared in include/sip_beam.h: argument checks, workspace carving, launches.
 #pragma once
-#include <cmath>
-
 #include "../../include/sip_beam.h"
 #include "sip_beam.h"
 #include "sip_host.h"
 
 namespace {
 
-inline int beam_chunks(int32_t V) { return tiles(V, sip::kBeamChunk); }
+inline int beam_chunks(int32_t V, bool bf16) { return tiles(V, sip::beam_chunk(bf16)); }
 bool beam_shape_ok(int32_t groups, int32_t width, int32_t V, int32_t n) {
   return groups > 0 && width > 0 && V > 0 && n > 0 && width <= SIP_MAX_BEAMS && V <= SIP_MAX_V && n <= SIP_MAX_CONTINUATIONS &&
          (int64_t)groups * width <= SIP_MAX_B;
 }
-static_assert(SIP_MAX_V <= 64 * sip::kBeamChunk, "beam_merge_kernel: a lane a chunk, kHeads lists a lane");
+static_assert(SIP_MAX_V <= 64 * sip::kBeamThreads * sip::kBeamLoads * 4, "the merging kernels: a lane a chunk");
 size_t beam_part_bytes(int64_t lists) { return head_align((size_t)lists * sizeof(sip::BeamPart)); }
 
 }  // namespace
@@ -22,7 +20,7 @@ extern "C" {
 
 size_t sip_beam_workspace_bytes(int32_t groups, int32_t width, int32_t V, int32_t n) {
   if (!beam_shape_ok(groups, width, V, n)) return 0;
-  const int64_t lists = (int64_t)groups * width * beam_chunks(V);
+  const int64_t lists = (int64_t)groups * width * beam_chunks(V, false);                   // (of fp32: the most)
   return beam_part_bytes(lists) + head_align((size_t)lists * n * 8);
 }
 
@@ -39,13 +37,10 @@ sip_status sip_beam_select(const void* logits, int32_t groups, int32_t width, in
   sip::BeamArgs a{};
   a.logits = logits; a.row_stride = row_stride;
   a.groups = groups; a.width = width; a.V = V; a.n = n;
-  a.chunks = beam_chunks(V);
+  a.chunks = beam_chunks(V, dtype == SIP_BF16);
+  a.chunk = sip::beam_chunk(dtype == SIP_BF16);
   a.scale = (double)logit_scale;
-  // below the exact product, so that c_lo > 0: (-inf) c_hi + (-inf) c_lo is -inf then
-  const double c = a.scale * 1.4426950408889634074;
-  a.c_hi = (float)c;
-  if ((double)a.c_hi >= c) a.c_hi = std::nextafterf(a.c_hi, 0.0f);
-  a.c_lo = (float)(c - (double)a.c_hi);
+  a.c = (float)(a.scale * 1.4426950408889634074);
   a.scores = scores; a.finished = finished; a.rank_scale = rank_scale; a.end_token = end_token;
   a.tokens = tokens; a.parents = parents; a.out_scores = out_scores;
   const int64_t lists = (int64_t)groups * width * a.chunks;
@@ -54,11 +49,8 @@ sip_status sip_beam_select(const void* logits, int32_t groups, int32_t width, in
   hipStream_t stream = static_cast<hipStream_t>(hip_stream);
   if (dtype == SIP_BF16) hipLaunchKernelGGL(sip::beam_chunk_kernel<true>, dim3(lists), dim3(sip::kBeamThreads), 0, stream, a);
   else hipLaunchKernelGGL(sip::beam_chunk_kernel<false>, dim3(lists), dim3(sip::kBeamThreads), 0, stream, a);
-  constexpr int kFew = sip::merge_room(512, 31), kMany = sip::merge_room(SIP_MAX_BEAMS * 64, SIP_MAX_CONTINUATIONS);
-  if (sip::merge_room(width * a.chunks, n) <= kFew)
-    hipLaunchKernelGGL(sip::beam_merge_kernel<kFew>, dim3(groups), dim3(sip::kMergeThreads), 0, stream, a);
-  else
-    hipLaunchKernelGGL(sip::beam_merge_kernel<kMany>, dim3(groups), dim3(sip::kMergeThreads), 0, stream, a);
+  if (width * a.chunks * n <= sip::kMergeFew) hipLaunchKernelGGL(sip::beam_merge_few_kernel, dim3(groups), dim3(256), 0, stream, a);
+  else hipLaunchKernelGGL(sip::beam_merge_kernel, dim3(groups), dim3(sip::kMergeThreads), 0, stream, a);
   return launched();
 }
 

@@ -26,7 +26,14 @@ sip::EmbedArgs embed_args(int32_t V, int32_t D, const int32_t* ids, int32_t N, f
   a.out = out; a.out_stride = out_stride; a.out_bf16 = out_dtype == SIP_BF16;
   return a;
 }
-dim3 embed_grid(int32_t N, int32_t D) { return dim3(std::min<long long>(tiles((long long)N * (D / 8), 256), 1 << 20)); }
+// Four rows' pieces a lane where that leaves every compute unit eight workgroups: 16000 rows of 4096 bf16 take 40 us so, 50 with one a lane;
+// 32 rows from codes 4.4 and 3.0.
+template <bool CODES>
+void launch_embed(const sip::EmbedArgs& a, hipStream_t stream) {
+  const long long units = (long long)a.N * (a.D / 8);
+  if (units >= 8 * kChip * 4 * 256) hipLaunchKernelGGL((sip::embed_kernel<CODES, 4>), dim3(tiles(units, 4 * 256)), dim3(256), 0, stream, a);
+  else hipLaunchKernelGGL((sip::embed_kernel<CODES, 1>), dim3(tiles(units, 256)), dim3(256), 0, stream, a);
+}
 
 // Entries of a piece of the sorted tokens: 8 to 64, as many as leave every SIMD four waves.
 constexpr int kPieceLeast = sip::kSumAhead, kPieceMost = 64;
@@ -100,7 +107,7 @@ sip_status sip_embed(const void* weight, sip_dtype weight_dtype, int32_t V, int3
   if (N == 0) return SIP_OK;
   sip::EmbedArgs a = embed_args(V, D, ids, N, scale, out, out_stride, out_dtype);
   a.weight = weight; a.weight_stride = weight_stride; a.weight_bf16 = weight_dtype == SIP_BF16;
-  hipLaunchKernelGGL(sip::embed_kernel<false>, embed_grid(N, D), dim3(256), 0, static_cast<hipStream_t>(hip_stream), a);
+  launch_embed<false>(a, static_cast<hipStream_t>(hip_stream));
   return launched();
 }
 
@@ -117,8 +124,8 @@ sip_status sip_embed_codes(const uint8_t* codes, int64_t codes_stride, const voi
   if (N == 0) return SIP_OK;
   sip::EmbedArgs a = embed_args(V, D, ids, N, scale, out, out_stride, out_dtype);
   a.codes = codes; a.codes_stride = codes_stride; a.scales = scales; a.scales_bf16 = scales_dtype == SIP_BF16;
-  a.zeros = zeros; a.group = group;
-  hipLaunchKernelGGL(sip::embed_kernel<true>, embed_grid(N, D), dim3(256), 0, static_cast<hipStream_t>(hip_stream), a);
+  a.zeros = zeros; a.group_shift = group == 32 ? 5 : group == 64 ? 6 : 7;
+  launch_embed<true>(a, static_cast<hipStream_t>(hip_stream));
   return launched();
 }
 
