@@ -23,7 +23,8 @@ struct AdaptArgs {
   int* count;                                            // batches
   int* rows;                                             // [B] rows that have an adapter, by adapter
   int4* batch;                                           // [B] first of a batch in `rows`, its size, its adapter
-  float* t;                                              // [batches][16][rank] scales[a] * down[a] hidden[b]
+  float* t;                                              // [parts][batches][16][rank] scales[a] * down[a] hidden[b], a part of the sum over D each
+  int parts, batches;
 };
 
 // One workgroup lists the rows by adapter, in batches.  (The order of an adapter's rows changes no result.)
@@ -107,8 +108,8 @@ __device__ inline Split split_of(f32x8 x) {
   return s;
 }
 
-// t of a batch, sixteen entries a workgroup: its waves share the sum over D and join their parts in order.
-constexpr int kDownWaves = 16;
+// t of a batch, sixteen entries a workgroup: its waves share a part of the sum over D and join what they have in order.
+constexpr int kDownWaves = 16, kDownParts = 4;
 template <bool BF16, bool DIRECT>
 __global__ __launch_bounds__(kDownWaves * 64) void adapt_down_kernel(AdaptArgs p) {
   __shared__ __align__(16) f32x4 sums[kDownWaves][64];
@@ -122,15 +123,16 @@ __global__ __launch_bounds__(kDownWaves * 64) void adapt_down_kernel(AdaptArgs p
   f32x4 acc = {0, 0, 0, 0};
   const bf16x8 none = {};
   constexpr int kAhead = BF16 ? 8 : 4;                   // steps whose loads are under way at once
-  for (int c0 = w * 32; c0 < p.D; c0 += kAhead * kDownWaves * 32) {
+  const int each = (p.D + p.parts * 32 - 1) / (p.parts * 32) * 32, begin = blockIdx.z * each, end = min(p.D, begin + each);
+  for (int c0 = begin + w * 32; c0 < end; c0 += kAhead * kDownWaves * 32) {
     bf16x8 a[kAhead];
     Eight h[kAhead];
 #pragma unroll
     for (int s = 0; s < kAhead; ++s) {
       const int c = c0 + s * kDownWaves * 32 + k;
-      a[s] = live && c < p.D ? *reinterpret_cast<const bf16x8*>(down + c) : none;
+      a[s] = live && c < end ? *reinterpret_cast<const bf16x8*>(down + c) : none;
       h[s] = Eight{};
-      if (x.row >= 0 && c < p.D) h[s] = load_eight(p.hidden, x.row * p.hidden_stride + c, BF16);
+      if (x.row >= 0 && c < end) h[s] = load_eight(p.hidden, x.row * p.hidden_stride + c, BF16);
     }
 #pragma unroll
     for (int s = 0; s < kAhead; ++s) {
@@ -149,13 +151,15 @@ __global__ __launch_bounds__(kDownWaves * 64) void adapt_down_kernel(AdaptArgs p
   for (int i = 1; i < kDownWaves; ++i) acc += sums[i][lane];
   const int j0 = blockIdx.y * 16 + acc_a(lane);
   if (x.row < 0 || j0 >= p.rank) return;
-  *reinterpret_cast<f32x4*>(p.t + ((long long)blockIdx.x * kAdaptRows + (lane & 15)) * p.rank + j0) = acc * scale;
+  const long long at = ((long long)blockIdx.z * p.batches + blockIdx.x) * kAdaptRows + (lane & 15);
+  *reinterpret_cast<f32x4*>(p.t + at * p.rank + j0) = acc * scale;
 }
 
 // The additions of one batch to `tiles` of kUpWaves * 16 logits each.  A wave's share of a tile is sixteen entries of the vocabulary, of
-// which a lane has four neighbours of one row.  VECTOR: logits are fp32 in rows that start at 16 bytes.
+// which a lane has four neighbours of one row.  VECTOR: logits are fp32 in rows that start at 16 bytes.  ONE: tiles = 1, and t may
+// be in parts.
 constexpr int kUpWaves = 4, kUpEntries = kUpWaves * 16;
-template <int STEPS, bool DIRECT, bool VECTOR>
+template <int STEPS, bool ONE, bool DIRECT, bool VECTOR>
 __global__ __launch_bounds__(kUpWaves * 64) void adapt_up_kernel(AdaptArgs p, int batches, int tiles) {
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, k = 8 * (lane >> 4);
   // batches of one adapter go through the same entries one after the other on one XCD, whose L2 then has them
@@ -163,47 +167,65 @@ __global__ __launch_bounds__(kUpWaves * 64) void adapt_up_kernel(AdaptArgs p, in
   if (v0 >= p.V) return;
   const Batch x = batch_of<DIRECT>(p, i);
   if (x.n == 0) return;
-  Split t[STEPS];
-#pragma unroll
-  for (int s = 0; s < STEPS; ++s) {
-    f32x8 f = {0, 0, 0, 0, 0, 0, 0, 0};
-    if (x.row >= 0 && 32 * s + k < p.rank)
-      f = as_floats(load_eight(p.t, ((long long)i * kAdaptRows + (lane & 15)) * p.rank + 32 * s + k, false), false);
-    t[s] = split_of(f);
-  }
   const uint16_t* up = p.up + (long long)x.adapter * p.V * p.rank;
   const bf16x8 none = {};
-  constexpr int kAhead = STEPS > 2 ? 2 : 4;              // tiles whose loads are under way at once
-  for (int tile0 = 0; tile0 < tiles; tile0 += kAhead) {
+  constexpr int kAhead = ONE ? 1 : STEPS > 2 ? 2 : 4;    // tiles whose loads are under way at once, while as many others are multiplied
+  constexpr int kParts = ONE ? kDownParts : 1;
+  struct Loads {
     bf16x8 a[kAhead][STEPS];
     f32x4 z[kAhead];
-    auto at_of = [&](int j) { return v0 + ((tile0 + j) * kUpWaves + w) * 16; };          // a tile's first entry; V: there is none
+  };
+  auto first_of = [&](int tile) { return tile < tiles ? v0 + (tile * kUpWaves + w) * 16 : p.V; };       // (V: there is none)
+  auto load = [&](Loads& l, int tile0) {
 #pragma unroll
     for (int j = 0; j < kAhead; ++j) {
-      const int v = tile0 + j < tiles ? at_of(j) : p.V, entry = v + (lane & 15), at = v + acc_a(lane);
+      const int v = first_of(tile0 + j), entry = v + (lane & 15), at = v + acc_a(lane);
 #pragma unroll
       for (int s = 0; s < STEPS; ++s)
-        a[j][s] = entry < p.V && 32 * s + k < p.rank ? *reinterpret_cast<const bf16x8*>(up + (long long)entry * p.rank + 32 * s + k) : none;
-      z[j] = f32x4{0, 0, 0, 0};
+        l.a[j][s] = entry < p.V && 32 * s + k < p.rank ? *reinterpret_cast<const bf16x8*>(up + (long long)entry * p.rank + 32 * s + k) : none;
+      l.z[j] = f32x4{0, 0, 0, 0};
       if (x.row < 0 || at >= p.V) continue;
       const long long z0 = x.row * p.logits_stride + at;
       if (VECTOR && at + 4 <= p.V) {
-        z[j] = *reinterpret_cast<const f32x4*>(static_cast<const float*>(p.logits) + z0);
+        l.z[j] = *reinterpret_cast<const f32x4*>(static_cast<const float*>(p.logits) + z0);
       } else {
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-          if (at + e < p.V) z[j][e] = p.logits_bf16 ? (float)static_cast<const __bf16*>(p.logits)[z0 + e] : static_cast<const float*>(p.logits)[z0 + e];
+          if (at + e < p.V) l.z[j][e] = p.logits_bf16 ? (float)static_cast<const __bf16*>(p.logits)[z0 + e] : static_cast<const float*>(p.logits)[z0 + e];
       }
     }
+  };
+  Eight t_part[STEPS][kParts];
+#pragma unroll
+  for (int s = 0; s < STEPS; ++s)
+#pragma unroll
+    for (int part = 0; part < kParts; ++part) {
+      t_part[s][part] = Eight{};
+      const long long at = (((long long)part * batches + i) * kAdaptRows + (lane & 15)) * p.rank + 32 * s + k;
+      if (part < p.parts && x.row >= 0 && 32 * s + k < p.rank) t_part[s][part] = load_eight(p.t, at, false);
+    }
+  Loads next;
+  load(next, 0);
+  Split t[STEPS];
+#pragma unroll
+  for (int s = 0; s < STEPS; ++s) {
+    f32x8 sum = as_floats(t_part[s][0], false);
+#pragma unroll
+    for (int part = 1; part < kParts; ++part) sum += as_floats(t_part[s][part], false);
+    t[s] = split_of(sum);
+  }
+  for (int tile0 = 0; tile0 < tiles; tile0 += kAhead) {
+    const Loads now = next;
+    if (tile0 + kAhead < tiles) load(next, tile0 + kAhead);
 #pragma unroll
     for (int j = 0; j < kAhead; ++j) {
-      const int at = (tile0 + j < tiles ? at_of(j) : p.V) + acc_a(lane);
+      const int at = first_of(tile0 + j) + acc_a(lane);
       f32x4 acc = {0, 0, 0, 0};
 #pragma unroll
       for (int part = 2; part >= 0; --part)
 #pragma unroll
-        for (int s = 0; s < STEPS; ++s) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[j][s], t[s].part[part], acc, 0, 0, 0);
-      acc += z[j];
+        for (int s = 0; s < STEPS; ++s) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(now.a[j][s], t[s].part[part], acc, 0, 0, 0);
+      acc += now.z[j];
       if (x.row < 0 || at >= p.V) continue;
       const long long z0 = x.row * p.logits_stride + at;
       if (VECTOR && at + 4 <= p.V) {

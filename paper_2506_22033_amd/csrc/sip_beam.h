@@ -380,7 +380,7 @@ __device__ inline BeamRank rank_of(const BeamArgs& a, const BeamGroup& rows, int
 }
 
 // The leading bits of the n-th largest of the workgroup's values, EACH a lane: two bits a turn, of which votes[turn] counts the values
-// that reach the three possibilities (zeros before; a barrier a turn).
+// that reach the three possibilities (zeros before; a barrier a turn).  0 if there are fewer than n.
 constexpr int kVoteTurns = 12;
 typedef int BeamVotes[kVoteTurns][4];
 template <int EACH>
@@ -401,29 +401,57 @@ __device__ inline uint32_t nth_largest(const uint32_t (&x)[EACH], int n, BeamVot
     from |= (uint32_t)step << bit;
     if (step && (step == 1 ? all.x : step == 2 ? all.y : all.z) == n) break;
   }
-  return from ? from : 1;                                // (fewer than n: all that there are)
+  return from;
 }
 
-// f(rank, i) for each of n entries, i's place among them; `ranks` for up to kRanked.  Begins and ends with the entries visible to all.
-constexpr int kRanked = 1024;
-template <int THREADS, class F>
-__device__ inline void rank_all(const BeamRank* found, int n, int* ranks, F f) {
+// The same bound from the lists' heads alone, one a thread, compared with one another (their last bits make them differ), four a read: 16
+// waves' reads of LDS are what it costs.  0 if there are fewer than n.
+constexpr int kHeadsMost = 256;
+template <int THREADS>
+__device__ inline uint32_t nth_head(uint32_t lead, int lists, int n, uint32_t (&heads)[kHeadsMost], int (&ranks)[THREADS], uint32_t& bound) {
+  constexpr uint32_t kLast = kHeadsMost - 1;
   const int t = threadIdx.x;
-  if (n <= kRanked / 2) {
+  if (t < kHeadsMost) heads[t] = t < lists ? (lead & ~kLast) | (kLast - t) : 0;
+  ranks[t] = 0;
+  if (t == 0) bound = 0;
+  __syncthreads();
+  int wide = 64;
+  while (wide < lists) wide *= 2;
+  const int parts = THREADS / wide, i = t % wide;
+  if (i < lists) {
+    const uint32_t mine = heads[i];
+    int rank = 0;
+    for (int j = t / wide * 4; j < lists; j += parts * 4) {
+      const uint4 four = *reinterpret_cast<const uint4*>(&heads[j]);
+      rank += (four.x > mine) + (four.y > mine) + (four.z > mine) + (four.w > mine);
+    }
+    if (rank) atomicAdd(&ranks[i], rank);
+  }
+  __syncthreads();
+  if (t < lists && ranks[t] == n - 1) bound = heads[t] & ~kLast;
+  __syncthreads();
+  return bound;
+}
+
+// f(rank, i) for each of n entries, i's place among them.  Begins and ends with the entries visible to all.
+template <int THREADS, class F>
+__device__ inline void rank_all(const BeamRank* found, int n, int (&ranks)[THREADS], F f) {
+  const int t = threadIdx.x;
+  if (n <= THREADS / 2) {
     // several threads an entry: each compares it with a part of the others
     int wide = 32;
     while (wide < n) wide *= 2;
-    const int parts = max(1, THREADS / wide), part = t / wide;   // (wide > THREADS: one part, several entries a thread)
-    for (int i = t; i < n; i += THREADS) ranks[i] = 0;
+    const int parts = THREADS / wide, i = t % wide;
+    ranks[t] = 0;
     __syncthreads();
-    for (int i = t % wide; i < n; i += min(wide, THREADS)) {
+    if (i < n) {
       const BeamRank mine = found[i];
       int rank = 0;
-      for (int j = part; j < n; j += parts) rank += found[j] > mine;
+      for (int j = t / wide; j < n; j += parts) rank += found[j] > mine;
       if (rank) atomicAdd(&ranks[i], rank);
     }
     __syncthreads();
-    for (int i = t; i < n; i += THREADS) f(ranks[i], i);
+    if (t < n) f(ranks[t], t);
   } else {
     for (int i = t; i < n; i += THREADS) {
       const BeamRank mine = found[i];
@@ -456,7 +484,9 @@ __global__ __launch_bounds__(256) void beam_merge_few_kernel(BeamArgs a) {
   constexpr int kEach = kMergeFew / 256;
   __shared__ BeamGroup rows;
   __shared__ BeamRank found[kMergeFew];
-  __shared__ int ranks[kRanked], count;
+  __shared__ int ranks[256], count;
+  __shared__ uint32_t first[kHeadsMost], bound;
+  __shared__ __align__(16) uint32_t heads[kHeadsMost];
   __shared__ __align__(16) BeamVotes votes;
   const int t = threadIdx.x, entries = a.width * a.chunks * a.n;
   const unsigned long long* cand = a.cand + (long long)blockIdx.x * entries;
@@ -476,7 +506,20 @@ __global__ __launch_bounds__(256) void beam_merge_few_kernel(BeamArgs a) {
     if (at < entries) x[i] = rank_of(a, rows, at / a.n, at % a.n, key[i]);
     lead[i] = (uint32_t)(x[i].total >> 32);
   }
-  const uint32_t from = nth_largest(lead, a.n, votes);
+  const int lists = a.width * a.chunks;
+  uint32_t from = 0;
+  if (entries <= 64) from = 0;                           // (so few are compared with one another at once)
+  else if (lists <= kHeadsMost) {
+    // entry 0 of list t is entry t * n of all
+#pragma unroll
+    for (int i = 0; i < kEach; ++i)
+      if (t + i * 256 < entries && (t + i * 256) % a.n == 0) first[(t + i * 256) / a.n] = lead[i];
+    __syncthreads();
+    from = nth_head<256>(t < lists ? first[t] : 0, lists, a.n, heads, ranks, bound);
+  } else {
+    from = nth_largest(lead, a.n, votes);
+  }
+  from = max(from, 1u);                                  // (0: there is none)
 #pragma unroll
   for (int i = 0; i < kEach; ++i)
     if (lead[i] >= from) found[atomicAdd(&count, 1)] = x[i];
@@ -496,10 +539,13 @@ __global__ __launch_bounds__(kMergeThreads) void beam_merge_kernel(BeamArgs a) {
   constexpr int kHeads = kMergeLists / kMergeThreads;
   __shared__ BeamGroup rows;
   __shared__ BeamRank found[kMergeRoom];
-  __shared__ int ranks[kRanked], chosen[SIP_MAX_CONTINUATIONS], count;
+  __shared__ int ranks[kMergeThreads], chosen[SIP_MAX_CONTINUATIONS], count;
+  __shared__ uint32_t bound;
+  __shared__ __align__(16) uint32_t leads[kHeadsMost];
   __shared__ __align__(16) BeamVotes votes;
   const int t = threadIdx.x, S = a.chunks, n = a.n, lists = a.width * S;
   const unsigned long long* cand = a.cand + (long long)blockIdx.x * lists * n;
+  static_assert(kHeads == 4, "and as many entries at once");
   unsigned long long key[kHeads];
 #pragma unroll
   for (int i = 0; i < kHeads; ++i) key[i] = t + i * kMergeThreads < lists ? cand[(long long)(t + i * kMergeThreads) * n] : 0;
@@ -513,7 +559,7 @@ __global__ __launch_bounds__(kMergeThreads) void beam_merge_kernel(BeamArgs a) {
     const int l = t + i * kMergeThreads;
     lead[i] = l < lists ? (uint32_t)(rank_of(a, rows, l, 0, key[i]).total >> 32) : 0;
   }
-  const uint32_t from = nth_largest(lead, n, votes);
+  const uint32_t from = max(lists <= kHeadsMost ? nth_head<kMergeThreads>(lead[0], lists, n, leads, ranks, bound) : nth_largest(lead, n, votes), 1u);
 #pragma unroll
   for (int i = 0; i < kHeads; ++i)
     if (lead[i] >= from) found[atomicAdd(&count, 1)] = rank_of(a, rows, t + i * kMergeThreads, 0, key[i]);
@@ -526,11 +572,22 @@ __global__ __launch_bounds__(kMergeThreads) void beam_merge_kernel(BeamArgs a) {
   });
   if (t == 0) count = 0;
   __syncthreads();
-  for (int i = t; i < selected * n; i += kMergeThreads) {
-    const int r = i / n, e = i % n;
-    if (r + e >= n) continue;
-    const BeamRank x = rank_of(a, rows, chosen[r], e, cand[(long long)chosen[r] * n + e]);
-    if (x.total >> 32 >= from) found[atomicAdd(&count, 1)] = x;
+  constexpr int kAhead = kHeads;                         // entries whose loads are under way at once
+  for (int i0 = t; i0 < selected * n; i0 += kAhead * kMergeThreads) {
+    int list[kAhead], e[kAhead];
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      const int i = i0 + j * kMergeThreads, r = i / n;
+      e[j] = i - r * n;
+      list[j] = i < selected * n && r + e[j] < n ? chosen[r] : -1;
+      key[j] = list[j] >= 0 ? cand[(long long)list[j] * n + e[j]] : 0;
+    }
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      if (list[j] < 0) continue;
+      const BeamRank x = rank_of(a, rows, list[j], e[j], key[j]);
+      if (x.total >> 32 >= from) found[atomicAdd(&count, 1)] = x;
+    }
   }
   __syncthreads();
   const int kept = count;

@@ -127,11 +127,11 @@ struct EmbedGradArgs {
   float scale;
   void* out; long long out_stride; int out_bf16;
   int shift, buckets;                                    // bucket of a token: its bits from `shift` on
-  int piece, whole;                                      // entries of a piece, and of a token that is not cut: powers of two
+  int pieces, piece, whole;                              // entries of a piece, and of a token that is not cut: powers of two
   // workspace
   int* live;                                             // entries that take part
   uint32_t* key; uint32_t* pos;                          // [N + 8] tokens and their positions, sorted
-  int* cut;                                              // [pieces] where a piece begins
+  int* cut;                                              // [pieces + 1] where a piece begins
   uint32_t* spare[2];                                    // [N] for buckets that LDS does not hold
   float* part;                                           // [pieces][2][D] sums of what crosses a border: on the left, on the right
 };
@@ -349,8 +349,10 @@ template <bool BF16, bool ADD>
 __global__ __launch_bounds__(256) void embed_sum_kernel(EmbedGradArgs a) {
   const uint32_t per_row = a.D / 8, u = blockIdx.x * 256 + threadIdx.x;                     // (up to 2^28)
   const int n = *a.live, piece = (int)(u / per_row), c = (int)(u - piece * per_row) * 8;
+  if (piece >= a.pieces) return;
+  const int first = a.cut[piece], end = a.cut[piece + 1];               // (from the last entry on: anything)
   if ((long long)piece * a.piece >= n) return;
-  const int first = a.cut[piece], last = (piece + 1ll) * a.piece < n ? a.cut[piece + 1] : n;
+  const int last = (piece + 1ll) * a.piece < n ? end : n;
   if (first >= last) return;
   f32x8 sum = {0, 0, 0, 0, 0, 0, 0, 0};
   bool begun = first == 0 || a.key[first - 1] != a.key[first];         // the token's first entry is in this piece
@@ -414,12 +416,12 @@ __global__ __launch_bounds__(1024) void embed_join_kernel(EmbedGradArgs a) {
   const int n = *a.live, worker = threadIdx.x >> 6, lane = threadIdx.x & 63, c = (blockIdx.y * 64 + lane) * 8, piece0 = blockIdx.x * kJoinPieces;
   uint32_t token = 0;                                    // lane j: that of piece0 + j
   bool cut = false;
-  if (lane < kJoinPieces && (piece0 + lane + 1ll) * a.piece < n) {
-    const int begin = a.cut[piece0 + lane], border = (piece0 + lane + 1) * a.piece;
-    if (a.cut[piece0 + lane + 1] == border && begin < border) {
-      token = a.key[border];
-      cut = a.key[border - 1] == token && (begin == 0 || a.key[begin - 1] != token);
-    }
+  if (lane < kJoinPieces && piece0 + lane + 1 < a.pieces) {
+    const int border = (piece0 + lane + 1) * a.piece;                    // (within the list: what lies behind the last entry may be anything)
+    const int begin = a.cut[piece0 + lane], moved = a.cut[piece0 + lane + 1];
+    token = a.key[border];
+    const uint32_t behind = a.key[border - 1];
+    if (border < n && moved == border && begin < border && behind == token) cut = begin == 0 || a.key[begin - 1] != token;
   }
   for (unsigned long long left = __ballot(cut); left; left &= left - 1) {
     const int j0 = __builtin_ctzll(left), piece = piece0 + j0;

@@ -66,7 +66,7 @@ EmbedPlan embed_plan(int32_t N, int32_t D) {             // (room for N tokens o
   p.live = take(4);
   p.key = take(((size_t)N + 2 * sip::kSumAhead) * 4);
   p.pos = take(((size_t)N + 2 * sip::kSumAhead) * 4);
-  p.cut = take((size_t)N / kPieceLeast * 4 + 4);
+  p.cut = take((size_t)N / kPieceLeast * 4 + 8);
   for (size_t& s : p.spare) s = take((size_t)N * 4);
   p.piece = embed_piece(N, D);
   p.pieces = tiles(N, p.piece);
@@ -77,6 +77,11 @@ EmbedPlan embed_plan(int32_t N, int32_t D) {             // (room for N tokens o
 
 // Batches of B rows at most: one for every adapter that a row has, and one more for every sixteen rows.
 int adapt_batches(int32_t B, int32_t adapters) { return std::min(B, adapters + B / sip::kAdaptRows); }
+// Into how many parts the sum over D is dealt out: as many as compute units are free, of 512 entries or more.  (One compute unit takes
+// 5 us for the 128 KB of an adapter of rank 16, D = 4096.)
+int adapt_parts(int batches, int32_t rank, int32_t D) {
+  return std::max(1, std::min({sip::kDownParts, D / 512, kChip / (batches * tiles(rank, 16))}));
+}
 struct AdaptPlan { size_t count, rows, batch, t, bytes; };
 AdaptPlan adapt_plan(int32_t B, int32_t adapters, int32_t rank) {
   AdaptPlan p{};
@@ -85,7 +90,7 @@ AdaptPlan adapt_plan(int32_t B, int32_t adapters, int32_t rank) {
   p.count = take(4);
   p.rows = take((size_t)B * 4);
   p.batch = take((size_t)B * 16);
-  p.t = take((size_t)adapt_batches(B, adapters) * sip::kAdaptRows * rank * 4);
+  p.t = take((size_t)std::max(adapt_batches(B, adapters), kChip) * sip::kAdaptRows * rank * 4);           // (batches of all parts)
   p.bytes = at;
   return p;
 }
@@ -153,6 +158,7 @@ sip_status sip_embed_backward(const void* grad_out, int64_t grad_out_stride, sip
   a.out = grad_weight; a.out_stride = grad_weight_stride; a.out_bf16 = grad_weight_dtype == SIP_BF16;
   a.shift = embed_shift(V);
   a.buckets = N > 0 ? tiles(V, 1 << a.shift) : 0;
+  a.pieces = pl.pieces;
   a.piece = pl.piece;
   a.whole = 2 * pl.piece;
   a.live = reinterpret_cast<int*>(ws + pl.live);
@@ -213,10 +219,12 @@ sip_status sip_head_adapt(const void* hidden, int32_t B, int32_t D, int64_t hidd
   hipStream_t stream = static_cast<hipStream_t>(hip_stream);
   const bool direct = B <= sip::kAdaptDirect;
   const int batches = adapt_batches(B, adapters), steps = tiles(rank, 32);
+  if (!direct) hipLaunchKernelGGL(sip::adapt_rows_kernel, dim3(1), dim3(1024), 0, stream, a);
   int each = 16;                                         // tiles of a workgroup: fewer where that leaves the chip half empty
   while (each > 1 && (long long)tiles(V, sip::kUpEntries * each) * batches < 8 * kChip) each /= 2;
-  if (!direct) hipLaunchKernelGGL(sip::adapt_rows_kernel, dim3(1), dim3(1024), 0, stream, a);
-  const dim3 down_grid(batches, tiles(rank, 16)), up_grid(tiles(tiles(V, sip::kUpEntries * each), 8) * 8 * batches);
+  a.parts = each == 1 ? adapt_parts(batches, rank, D) : 1;
+  a.batches = batches;
+  const dim3 down_grid(batches, tiles(rank, 16), a.parts), up_grid(tiles(tiles(V, sip::kUpEntries * each), 8) * 8 * batches);
   auto launch = [&](auto in_direct) {
     constexpr bool kDirect = decltype(in_direct)::value;
     if (hidden_dtype == SIP_BF16) hipLaunchKernelGGL((sip::adapt_down_kernel<true, kDirect>), down_grid, dim3(sip::kDownWaves * 64), 0, stream, a);
@@ -224,7 +232,8 @@ sip_status sip_head_adapt(const void* hidden, int32_t B, int32_t D, int64_t hidd
     auto add = [&](auto in_steps, auto in_vector) {
       constexpr int kSteps = decltype(in_steps)::value;
       constexpr bool kVector = decltype(in_vector)::value;
-      hipLaunchKernelGGL((sip::adapt_up_kernel<kSteps, kDirect, kVector>), up_grid, dim3(sip::kUpWaves * 64), 0, stream, a, batches, each);
+      if (each == 1) hipLaunchKernelGGL((sip::adapt_up_kernel<kSteps, true, kDirect, kVector>), up_grid, dim3(sip::kUpWaves * 64), 0, stream, a, batches, each);
+      else hipLaunchKernelGGL((sip::adapt_up_kernel<kSteps, false, kDirect, kVector>), up_grid, dim3(sip::kUpWaves * 64), 0, stream, a, batches, each);
     };
     auto add_steps = [&](auto in_vector) {
       if (steps == 1) add(std::integral_constant<int, 1>{}, in_vector);
