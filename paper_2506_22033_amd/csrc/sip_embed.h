@@ -214,24 +214,23 @@ __device__ inline void clear_rows(const EmbedGradArgs& a, uint32_t mine, uint32_
   }
 }
 
-// A workgroup a bucket of the vocabulary: it reads all tokens, lists those of its bucket in order, counts those of the buckets before, and
-// sorts its own.  The workgroups behind fill grad_weight with zeros meanwhile, unless it is added to.  ROOM: entries of a bucket
-// that LDS holds, twice; larger buckets are sorted in the workspace.
 struct __attribute__((packed, aligned(4))) FourIds { uint32_t x[4]; };
-template <int ROOM>
-__global__ __launch_bounds__(kSortThreads) void embed_sort_kernel(EmbedGradArgs a) {
-  __shared__ uint32_t room[2][ROOM];
-  __shared__ SortCounters at;
-  __shared__ uint32_t wave_total[kSortWaves], wave_before[kSortWaves];
+struct BucketShared {
+  SortCounters at;
+  uint32_t wave_total[kSortWaves], wave_before[kSortWaves];
+};
+// What a workgroup finds of its bucket of the vocabulary: how many entries, how many are in the buckets before.
+struct Bucket { uint32_t low, size, n, start; };
+// It reads all tokens, lists those of its bucket in order -- put(place, bucket, entry) -- and counts those of the buckets before.
+template <class F>
+__device__ inline Bucket list_bucket(const EmbedGradArgs& a, int bucket, BucketShared& s, F put) {
   const int t = threadIdx.x, lane = t & 63, w = t >> 6;
-  if ((int)blockIdx.x >= a.buckets) {
-    clear_rows(a, (blockIdx.x - a.buckets) * kSortThreads + t, (gridDim.x - a.buckets) * kSortThreads);
-    return;
-  }
   // A wave's run of ids, four neighbours a lane, kQuads loads under way at once.
   constexpr int kQuads = 4;
-  const int bucket = blockIdx.x, run = (a.N + kSortThreads * 4 - 1) / (kSortThreads * 4) * 256, first = w * run, last = min(a.N, first + run);
-  const uint32_t low = (uint32_t)bucket << a.shift, size = min((uint32_t)a.V - low, 1u << a.shift);
+  const int run = (a.N + kSortThreads * 4 - 1) / (kSortThreads * 4) * 256, first = w * run, last = min(a.N, first + run);
+  Bucket b;
+  b.low = (uint32_t)bucket << a.shift;
+  b.size = min((uint32_t)a.V - b.low, 1u << a.shift);
   FourIds id[kQuads];
   auto load = [&](int i0) {
 #pragma unroll
@@ -251,26 +250,21 @@ __global__ __launch_bounds__(kSortThreads) void embed_sort_kernel(EmbedGradArgs 
     for (int j = 0; j < kQuads; ++j)
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        n += __popcll(__ballot(id[j].x[e] - low < size));
-        before += __popcll(__ballot(id[j].x[e] < low));
+        n += __popcll(__ballot(id[j].x[e] - b.low < b.size));
+        before += __popcll(__ballot(id[j].x[e] < b.low));
       }
   }
-  if (lane == 0) { wave_total[w] = n; wave_before[w] = before; }
+  if (lane == 0) { s.wave_total[w] = n; s.wave_before[w] = before; }
   __syncthreads();
-  uint32_t mine_n = lane < kSortWaves ? wave_total[lane] : 0, base = lane < w ? mine_n : 0, start = lane < kSortWaves ? wave_before[lane] : 0;
-  for (int s = 1; s < kSortWaves; s <<= 1) {
-    mine_n += __shfl_xor(mine_n, s);
-    base += __shfl_xor(base, s);
-    start += __shfl_xor(start, s);
+  uint32_t all = lane < kSortWaves ? s.wave_total[lane] : 0, base = lane < w ? all : 0, start = lane < kSortWaves ? s.wave_before[lane] : 0;
+  for (int d = 1; d < kSortWaves; d <<= 1) {
+    all += __shfl_xor(all, d);
+    base += __shfl_xor(base, d);
+    start += __shfl_xor(start, d);
   }
-  n = __shfl(mine_n, 0);
+  b.n = __shfl(all, 0);
+  b.start = __shfl(start, 0);
   base = __shfl(base, 0);
-  start = __shfl(start, 0);
-  if (bucket == a.buckets - 1 && t == 0) *a.live = (int)(start + n);
-  if (n == 0) return;
-  const bool in_lds = n <= ROOM;
-  uint32_t* spare0 = a.spare[0] + start;
-  uint32_t* spare1 = a.spare[1] + start;
   const unsigned long long below = (1ull << lane) - 1;
   for (int i0 = first; i0 < last; i0 += kQuads * 256) {
     if (run > kQuads * 256) load(i0);
@@ -278,7 +272,7 @@ __global__ __launch_bounds__(kSortThreads) void embed_sort_kernel(EmbedGradArgs 
     for (int j = 0; j < kQuads; ++j) {
       unsigned long long mine[4];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) mine[e] = __ballot(id[j].x[e] - low < size);
+      for (int e = 0; e < 4; ++e) mine[e] = __ballot(id[j].x[e] - b.low < b.size);
       if (mine[0] | mine[1] | mine[2] | mine[3]) {
         uint32_t to = base;
 #pragma unroll
@@ -288,16 +282,45 @@ __global__ __launch_bounds__(kSortThreads) void embed_sort_kernel(EmbedGradArgs 
         }
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-          if (mine[e] >> lane & 1) {
-            const uint32_t entry = (id[j].x[e] - low) << kPosBits | (uint32_t)(i0 + j * 256 + lane * 4 + e);
-            if (in_lds) room[0][to] = entry;
-            else spare0[to] = entry;
-            ++to;
-          }
+          if (mine[e] >> lane & 1) put(to++, b, (id[j].x[e] - b.low) << kPosBits | (uint32_t)(i0 + j * 256 + lane * 4 + e));
       }
     }
   }
   __syncthreads();
+  return b;
+}
+// The n entries in `from`, sorted: there or in `to` (LDS).
+typedef SIP_LDS uint32_t* LdsEntries;
+__device__ inline LdsEntries sort_bucket(const EmbedGradArgs& a, LdsEntries from, LdsEntries to, int n, BucketShared& s) {
+  if (n > kSortPairs) return sort_entries<LdsEntries>(from, to, n, a.shift, s.at, s.wave_total);
+  if ((int)threadIdx.x < n) {
+    const uint32_t mine = from[threadIdx.x];
+    uint32_t rank = 0;
+    for (int j = 0; j < n; ++j) rank += from[j] < mine;
+    to[rank] = mine;
+  }
+  __syncthreads();
+  return to;
+}
+
+// A workgroup a bucket.  The workgroups behind fill grad_weight with zeros meanwhile, unless it is added to.  ROOM: entries of a bucket
+// that LDS holds, twice; larger buckets are sorted in the workspace.
+template <int ROOM>
+__global__ __launch_bounds__(kSortThreads) void embed_sort_kernel(EmbedGradArgs a) {
+  __shared__ uint32_t room[2][ROOM];
+  __shared__ BucketShared shared;
+  const int t = threadIdx.x;
+  if ((int)blockIdx.x >= a.buckets) {
+    clear_rows(a, (blockIdx.x - a.buckets) * kSortThreads + t, (gridDim.x - a.buckets) * kSortThreads);
+    return;
+  }
+  const int bucket = blockIdx.x;
+  const Bucket b = list_bucket(a, bucket, shared, [&](uint32_t to, const Bucket& b, uint32_t entry) {
+    if (b.n <= ROOM) room[0][to] = entry;
+    else a.spare[0][b.start + to] = entry;
+  });
+  const uint32_t n = b.n, start = b.start;
+  if (bucket == a.buckets - 1 && t == 0) *a.live = (int)(start + n);
   // what is sorted goes out, and where the pieces' borders among it lie
   auto finish = [&](auto sorted) {
     for (uint32_t i = t; i < n; i += kSortThreads) {
@@ -320,21 +343,8 @@ __global__ __launch_bounds__(kSortThreads) void embed_sort_kernel(EmbedGradArgs 
       a.cut[border / a.piece] = (int)start + cut;
     }
   };
-  typedef SIP_LDS uint32_t* Lds;
-  if (n <= kSortPairs) {
-    if (t < (int)n) {
-      const uint32_t mine = room[0][t];
-      uint32_t rank = 0;
-      for (uint32_t j = 0; j < n; ++j) rank += room[0][j] < mine;
-      room[1][rank] = mine;
-    }
-    __syncthreads();
-    finish((Lds)&room[1][0]);
-  } else if (in_lds) {
-    finish(sort_entries<Lds>((Lds)&room[0][0], (Lds)&room[1][0], (int)n, a.shift, at, wave_total));
-  } else {
-    finish(sort_entries<uint32_t*>(spare0, spare1, (int)n, a.shift, at, wave_total));
-  }
+  if (n <= ROOM) finish(sort_bucket(a, (LdsEntries)&room[0][0], (LdsEntries)&room[1][0], (int)n, shared));
+  else finish(sort_entries<uint32_t*>(a.spare[0] + start, a.spare[1] + start, (int)n, a.shift, shared.at, shared.wave_total));
 }
 
 __device__ inline void embed_store(const EmbedGradArgs& a, long long at, f32x8 sum, const Eight* old) {
@@ -405,6 +415,81 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(EmbedGradArgs a) {
       }
     }
   }
+}
+
+// A small gradient in one launch: a workgroup a bucket, which sums its tokens' rows itself and clears the bucket's others.  The sorted
+// entries go to groups of waves that cover a row each, a run of entries a group; what crosses the end of a run goes through LDS.
+constexpr int kSmallTokens = 1024, kSmallWidth = kSortWaves * 512;
+template <bool BF16, bool ADD>
+__global__ __launch_bounds__(kSortThreads) void embed_small_kernel(EmbedGradArgs a) {
+  __shared__ uint32_t room[2][kSmallTokens];
+  __shared__ BucketShared shared;
+  __shared__ __align__(16) uint8_t hit[kBucketMost];
+  __shared__ f32x8 part[2][kSortThreads];                // of a group's run: what begins before it, what goes on behind it
+  const int t = threadIdx.x;
+  reinterpret_cast<uint32_t*>(hit)[t] = 0;
+  static_assert(kBucketMost == 4 * kSortThreads, "four a thread");
+  const Bucket b = list_bucket(a, blockIdx.x, shared, [&](uint32_t to, const Bucket&, uint32_t entry) {
+    room[0][to] = entry;
+    hit[entry >> kPosBits] = 1;
+  });
+  if constexpr (!ADD) {
+    const uint32_t per_row = a.D * (a.out_bf16 ? 2 : 4) / 16;
+    const long long pitch = a.out_stride * (a.out_bf16 ? 2 : 4) / 16;
+    u32x4* out = static_cast<u32x4*>(a.out) + b.low * pitch;
+    for (uint32_t u = t; u < b.size * per_row; u += kSortThreads) {
+      const uint32_t v = u / per_row;
+      if (!hit[v]) out[v * pitch + (u - v * per_row)] = u32x4{0, 0, 0, 0};
+    }
+  }
+  const int n = (int)b.n;
+  if (n == 0) return;
+  const LdsEntries sorted = sort_bucket(a, (LdsEntries)&room[0][0], (LdsEntries)&room[1][0], n, shared);
+  const int waves = (a.D + 511) / 512, groups = kSortWaves / waves, group = (t >> 6) / waves, c = (t - group * waves * 64) * 8;
+  const int run = (n + groups - 1) / groups, first = group * run, last = min(n, first + run);
+  auto token = [&](int i) { return sorted[i] >> kPosBits; };
+  const f32x8 none = {0, 0, 0, 0, 0, 0, 0, 0};
+  f32x8 sum = none;
+  constexpr int kAhead = ADD ? 4 : kSumAhead;            // (128 registers a lane)
+  if (c < a.D && first < last) {
+    bool begun = first == 0 || token(first - 1) != token(first);
+    for (int i0 = first; i0 < last; i0 += kAhead) {
+      Eight x[kAhead], old[kAhead];
+      bool fresh = begun;
+#pragma unroll
+      for (int j = 0; j < kAhead; ++j) {
+        x[j] = old[j] = Eight{};
+        if (i0 + j >= last) continue;
+        x[j] = load_eight(a.grad, (sorted[i0 + j] & ((1u << kPosBits) - 1)) * a.grad_stride + c, BF16);
+        if (ADD && (i0 + j + 1 == n || token(i0 + j + 1) != token(i0 + j))) {
+          if (fresh) old[j] = load_eight(a.out, (b.low + token(i0 + j)) * a.out_stride + c, a.out_bf16);
+          fresh = true;
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < kAhead; ++j) {
+        if (i0 + j >= last) continue;
+        sum += as_floats(x[j], BF16);
+        const bool ends = i0 + j + 1 == n || token(i0 + j + 1) != token(i0 + j);
+        if (!ends && i0 + j + 1 < last) continue;
+        if (begun && ends) embed_store(a, (b.low + token(i0 + j)) * a.out_stride + c, sum, ADD ? &old[j] : nullptr);
+        else part[begun][t] = sum;
+        sum = none;
+        begun = true;
+      }
+    }
+  }
+  __syncthreads();
+  // the token that goes on behind the run, if it begins in it
+  if (c >= a.D || first >= last || last == n) return;
+  const uint32_t v = token(last);
+  if (token(last - 1) != v || (first > 0 && token(first - 1) == v)) return;
+  sum = part[1][t];
+  for (int at = last, there = t + waves * 64; at < n && token(at) == v; at += run, there += waves * 64) sum += part[0][there];
+  Eight old = {};
+  const long long to = (b.low + v) * a.out_stride + c;
+  if (ADD) old = load_eight(a.out, to, a.out_bf16);
+  embed_store(a, to, sum, ADD ? &old : nullptr);
 }
 
 // The tokens that begin in a piece and go on behind its right border: 64 lanes of eight columns, of which each has sixteen workers

@@ -152,6 +152,29 @@ def test_frequent_tokens(N, D, V):
     _check_gradient(sip.sip_embed_backward(grad, ids, V, 1.0, dtype=F32), grad, ids, V, 1.0)
 
 
+@pytest.mark.parametrize("accumulate", [False, True])
+@pytest.mark.parametrize("gt", [F32, BF16])
+@pytest.mark.parametrize("N,D,V", [(8192, 64, 300), (1000, 512, 4096), (700, 600, 33), (60, 8192, 20), (333, 1544, 129), (17, 4096, 2000)])
+def test_frequent_tokens_of_small_calls(N, D, V, gt, accumulate):
+    """Runs of one token that cross the workgroup's shares, in one launch."""
+    g = _gen(N + D)
+    grad = torch.randn(N, D, generator=g, device=DEV).to(gt)
+    start = torch.randn(V, D, generator=g, device=DEV)
+    for kind in range(3):
+        ids = (torch.rand(N, generator=g, device=DEV).pow(6) * V).to(torch.int32)
+        if kind == 1:
+            ids[:] = V // 2
+        if kind == 2:
+            ids = torch.arange(N, dtype=torch.int32, device=DEV) % 2 + V - 2
+            ids[::7] = -1
+        gw = start.clone()
+        sip.sip_embed_backward(grad, ids, V, 1.0, grad_weight=gw, accumulate=accumulate)
+        _check_gradient(gw, grad, ids, V, 1.0, start if accumulate else None)
+        again = start.clone()
+        sip.sip_embed_backward(grad, ids, V, 1.0, grad_weight=again, accumulate=accumulate)
+        assert torch.equal(gw, again)
+
+
 def test_the_largest_vocabulary():
     V, D, N = sip.SIP_MAX_V, 8, 3000
     g = _gen(1)
