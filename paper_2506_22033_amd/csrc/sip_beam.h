@@ -630,71 +630,69 @@ __device__ inline int length_of(const ReorderArgs& a, int slot) {
 // Sixteen bytes that are aligned to four.
 struct __attribute__((packed, aligned(4))) StateLine { uint32_t w[4]; };
 
-constexpr int kReorderThreads = 256;
+constexpr int kReorderThreads = 256;                     // of a workgroup that copies 4 KB of every slot of a group
 
-// A lane takes the same 16 bytes of every slot of a group: it reads them all before it writes any, and nobody else touches
-// them, so that the slots change places without room beside them.
+// The moves of a group, for all threads of a workgroup of at least WIDTH.
 template <int WIDTH>
-__global__ __launch_bounds__(kReorderThreads) void state_reorder_kernel(ReorderArgs a) {
-  __shared__ Move move[WIDTH];
-  __shared__ int slot[WIDTH], keep[WIDTH];               // tokens that move
-  const int blocks = a.token_blocks + 8, g = blockIdx.x / blocks, block = blockIdx.x % blocks, t = threadIdx.x;
-  const bool table = block >= a.token_blocks;
-  Move m = move_of(a, g, slot);
-  if (t < a.width) {
-    if (m.from == m.to) m.to = -1;
-    move[t] = m;
-    if (!table) keep[t] = length_of(a, m.from);
+struct Moves {
+  Move move[WIDTH];                                      // to < 0: nothing to copy
+  int slot[WIDTH], length[WIDTH];                        // (length: of what moves)
+};
+template <int WIDTH>
+__device__ inline Move find_moves(const ReorderArgs& a, int group, Moves<WIDTH>& s, bool lengths) {
+  const Move m = move_of(a, group, s.slot);
+  if ((int)threadIdx.x < a.width) {
+    s.move[threadIdx.x] = {m.from, m.from == m.to ? -1 : m.to};
+    if (lengths) s.length[threadIdx.x] = length_of(a, m.from);
   }
   __syncthreads();
-  StateLine x[WIDTH];
-  const int column = ((table ? block - a.token_blocks : block) * kReorderThreads + t) * 4;
-#pragma unroll
-  for (int k = 0; k < WIDTH; ++k) {
-    if (k >= a.width || move[k].to < 0) continue;
-    const long long from = move[k].from;
-    if (table) {
-      if (from >= 0) x[k] = *reinterpret_cast<const StateLine*>(a.table + from * (2 * kTableSlots) + column);
-      else
-        for (int j = 0; j < 4; ++j) x[k].w[j] = column < kTableSlots ? kTableEmpty : 0u;
-    } else if (column < keep[k]) {
-      x[k] = *reinterpret_cast<const StateLine*>(a.tokens + from * a.L_max + column);
-    }
-  }
-#pragma unroll
-  for (int k = 0; k < WIDTH; ++k) {
-    if (k >= a.width || move[k].to < 0) continue;
-    const long long to = move[k].to;
-    if (table) {
-      *reinterpret_cast<StateLine*>(a.table + to * (2 * kTableSlots) + column) = x[k];
-    } else {
-      int* out = a.tokens + to * a.L_max + column;
-      if (column + 4 <= keep[k]) *reinterpret_cast<StateLine*>(out) = x[k];
-      else
-        for (int j = 0; j < 4; ++j)
-          if (column + j < keep[k]) out[j] = (int)x[k].w[j];
-    }
-  }
+  return m;
 }
 
-// One wave a group, behind the copies: lengths and numbers of distinct tokens, all read before any is written, and the new tokens.
-__global__ __launch_bounds__(64) void state_reorder_append_kernel(ReorderArgs a) {
-  __shared__ int slot[64];
-  const int token = (int)threadIdx.x < a.width && a.new_tokens ? a.new_tokens[blockIdx.x * a.width + threadIdx.x] : -1;
-  const Move m = move_of(a, blockIdx.x, slot);
-  int n = 0, nd = 0;
-  if (m.to >= 0 && m.from >= 0) {
-    n = length_of(a, m.from);
-    nd = a.ndist[m.from];
+// A lane takes the same 16 bytes of every slot of a group, a bucket of the tables or four tokens: it reads them all before it writes any, and
+// nobody else touches them, so that the slots change places without room beside them.
+template <int WIDTH>
+__device__ inline void move_table(const ReorderArgs& a, const Moves<WIDTH>& s, int column) {
+  u32x4 x[WIDTH];
+#pragma unroll
+  for (int k = 0; k < WIDTH; ++k) {
+    if (k >= a.width || s.move[k].to < 0) continue;
+    const uint32_t empty = column < kTableSlots ? kTableEmpty : 0u;
+    x[k] = u32x4{empty, empty, empty, empty};
+    if (s.move[k].from >= 0) x[k] = *reinterpret_cast<const u32x4*>(a.table + (long long)s.move[k].from * (2 * kTableSlots) + column);
   }
-  __syncthreads();
-  if (m.to < 0) return;
+#pragma unroll
+  for (int k = 0; k < WIDTH; ++k) {
+    if (k >= a.width || s.move[k].to < 0) continue;
+    *reinterpret_cast<u32x4*>(a.table + (long long)s.move[k].to * (2 * kTableSlots) + column) = x[k];
+  }
+}
+template <int WIDTH>
+__device__ inline void move_tokens(const ReorderArgs& a, const Moves<WIDTH>& s, int column) {
+  StateLine x[WIDTH];
+#pragma unroll
+  for (int k = 0; k < WIDTH; ++k) {
+    if (k >= a.width || s.move[k].to < 0 || column >= s.length[k]) continue;
+    x[k] = *reinterpret_cast<const StateLine*>(a.tokens + (long long)s.move[k].from * a.L_max + column);
+  }
+#pragma unroll
+  for (int k = 0; k < WIDTH; ++k) {
+    if (k >= a.width || s.move[k].to < 0 || column >= s.length[k]) continue;
+    int* out = a.tokens + (long long)s.move[k].to * a.L_max + column;
+    if (column + 4 <= s.length[k]) *reinterpret_cast<StateLine*>(out) = x[k];
+    else
+      for (int j = 0; j < 3; ++j)
+        if (column + j < s.length[k]) out[j] = (int)x[k].w[j];
+  }
+}
+// Row threadIdx.x's length and number of distinct tokens (`n`, `nd` as its parent had them), and its new token, once the copies are there.
+__device__ inline void append_token(const ReorderArgs& a, int to, int n, int nd, int token) {
   if (token >= 0) {
     if (n < a.L_max) {
-      a.tokens[(long long)m.to * a.L_max + n] = token;
+      a.tokens[(long long)to * a.L_max + n] = token;
       ++n;
       if (nd >= 0) {
-        uint32_t* key = a.table + (long long)m.to * (2 * kTableSlots);
+        uint32_t* key = a.table + (long long)to * (2 * kTableSlots);
         const int r = table_insert_single(key, key + kTableSlots, (uint32_t)token);
         nd = r < 0 ? -1 : nd + r;
         if (nd > kTableMaxDistinct) nd = -1;
@@ -703,8 +701,54 @@ __global__ __launch_bounds__(64) void state_reorder_append_kernel(ReorderArgs a)
       atomicAdd(&a.head->overflow, 1u);
     }
   }
-  a.len[m.to] = n;
-  a.ndist[m.to] = nd;
+  a.len[to] = n;
+  a.ndist[to] = nd;
+}
+struct Appended { int n, nd, token; };
+__device__ inline Appended appended_of(const ReorderArgs& a, int group, const Move& m) {
+  Appended x = {0, 0, -1};
+  if ((int)threadIdx.x >= a.width || m.to < 0) return x;
+  if (m.from >= 0) {
+    x.n = length_of(a, m.from);
+    x.nd = a.ndist[m.from];
+  }
+  if (a.new_tokens) x.token = a.new_tokens[group * a.width + threadIdx.x];
+  return x;
+}
+
+// A workgroup a group, and all in one launch.
+constexpr int kGroupThreads = 1024, kGroupWidth = 8;
+static_assert(kGroupThreads * 4 == kTableSlots, "a bucket a thread");
+__global__ __launch_bounds__(kGroupThreads) void state_reorder_group_kernel(ReorderArgs a) {
+  __shared__ Moves<kGroupWidth> s;
+  const int t = threadIdx.x;
+  const Move m = find_moves(a, blockIdx.x, s, true);
+  const Appended x = appended_of(a, blockIdx.x, m);
+  move_table(a, s, t * 4);
+  move_table(a, s, kTableSlots + t * 4);
+  for (int column = t * 4; column < a.L_max; column += kGroupThreads * 4) move_tokens(a, s, column);
+  __syncthreads();                                       // (everybody has read, and written)
+  if (t < a.width && m.to >= 0) append_token(a, m.to, x.n, x.nd, x.token);
+}
+
+// Wide groups and long rows: 4 KB of a group's slots a workgroup ...
+template <int WIDTH>
+__global__ __launch_bounds__(kReorderThreads) void state_reorder_kernel(ReorderArgs a) {
+  __shared__ Moves<WIDTH> s;
+  const int blocks = a.token_blocks + 8, g = blockIdx.x / blocks, block = blockIdx.x % blocks, t = threadIdx.x;
+  const bool table = block >= a.token_blocks;
+  find_moves(a, g, s, !table);
+  if (table) move_table(a, s, ((block - a.token_blocks) * kReorderThreads + t) * 4);
+  else move_tokens(a, s, (block * kReorderThreads + t) * 4);
+}
+// ... and behind the copies one wave a group for the rest: lengths and numbers of distinct tokens, all read before any is written, and
+// the new tokens.
+__global__ __launch_bounds__(64) void state_reorder_append_kernel(ReorderArgs a) {
+  __shared__ int slot[64];
+  const Move m = move_of(a, blockIdx.x, slot);
+  const Appended x = appended_of(a, blockIdx.x, m);
+  __syncthreads();
+  if (m.to >= 0) append_token(a, m.to, x.n, x.nd, x.token);
 }
 
 }  // namespace sip
