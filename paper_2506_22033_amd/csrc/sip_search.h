@@ -41,7 +41,7 @@ sip_status sip_beam_select(const void* logits, int32_t groups, int32_t width, in
   if (!workspace_ok(workspace, workspace_bytes, sip_beam_workspace_bytes(groups, width, V, n))) return SIP_ERR_WORKSPACE;
   sip::BeamArgs a{};
   a.logits = logits; a.row_stride = row_stride;
-  a.groups = groups; a.width = width; a.V = V; a.n = n;
+  a.width = width; a.V = V; a.n = n;
   a.chunks = beam_chunks(V, dtype == SIP_BF16);
   a.chunk = sip::beam_chunk(dtype == SIP_BF16);
   a.scale = (double)logit_scale;
@@ -69,7 +69,7 @@ sip_status sip_state_reorder(void* state, size_t state_bytes, int32_t slots, int
   const sip::StateView v = sip::state_view(state, slots, L_max);
   sip::ReorderArgs a{};
   a.head = v.head; a.len = v.len; a.ndist = v.ndist; a.tokens = v.tokens; a.table = v.table;
-  a.slots = slots; a.L_max = L_max; a.groups = groups; a.width = width;
+  a.slots = slots; a.L_max = L_max; a.width = width;
   a.slot_of_row = slot_of_row; a.parents = parents; a.new_tokens = tokens;
   a.token_blocks = tiles(L_max, sip::kReorderThreads * 4);
   hipStream_t stream = static_cast<hipStream_t>(hip_stream);
@@ -77,7 +77,7 @@ sip_status sip_state_reorder(void* state, size_t state_bytes, int32_t slots, int
     hipLaunchKernelGGL(sip::state_reorder_group_kernel, dim3(groups), dim3(sip::kGroupThreads), 0, stream, a);
     return launched();
   }
-  const dim3 grid((unsigned)groups * (unsigned)(a.token_blocks + 8)), threads(sip::kReorderThreads);
+  const dim3 grid(groups, a.token_blocks + 8), threads(sip::kReorderThreads);             // (of all along x, more than a launch can have)
   if (width <= 8) hipLaunchKernelGGL(sip::state_reorder_kernel<8>, grid, threads, 0, stream, a);
   else if (width <= 32) hipLaunchKernelGGL(sip::state_reorder_kernel<32>, grid, threads, 0, stream, a);
   else hipLaunchKernelGGL(sip::state_reorder_kernel<64>, grid, threads, 0, stream, a);
