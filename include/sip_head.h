@@ -168,7 +168,8 @@ sip_status sip_head_logits(const void* hidden, int32_t B, int32_t D, int64_t hid
  *  logits    [B, logits_stride] fp32 or bf16, aligned to its element; only the first V entries of a row are read or written.
  *  workspace 256-byte aligned, at least sip_head_adapt_workspace_bytes(B, adapters, rank, D) bytes.  What is enough for B
  *            rows is enough for fewer.
- * Products and sums are fp32, t is kept in fp32; the new logit is rounded once.
+ * Products and sums are fp32, t is kept in fp32; the new logit is rounded once.  A row with an entry of t that is not finite (or beyond the
+ * largest bf16), or with such an entry in an fp32 hidden state, has logits of NaN; other rows are not affected.
  */
 size_t sip_head_adapt_workspace_bytes(int32_t B, int32_t adapters, int32_t rank, int32_t D);
 sip_status sip_head_adapt(const void* hidden, int32_t B, int32_t D, int64_t hidden_stride, sip_dtype hidden_dtype,

@@ -11,8 +11,10 @@
 namespace sip {
 
 // ---------------------------------------------------------------- selection
-// beam_chunk_kernel: a workgroup reads one chunk of a row once and leaves its maximum, its sum of exponentials and its n best
-// logits, in order.  The merging kernels: a workgroup joins the lists of a group's rows.
+// total(k, v) = score_k + (c z_kv - lse_k) grows with z within a row, so that the n best logits of every row hold a group's n best
+// continuations: one pass over the logits, lse and candidates together.  beam_chunk_kernel: a workgroup reads one chunk of a row once and leaves
+// its maximum, its sum of exponentials and its n best logits, in order.  The merging kernels: a workgroup joins the lists of a group's
+// rows, in fp64: two continuations may lie as near to one another as fp32's rounding of a sum of exponentials lets them.
 
 constexpr int kBeamThreads = 256, kBeamWaves = kBeamThreads / 64;
 constexpr int kBeamLoads = 8;                            // 16-byte loads of a lane: 32 fp32 logits, 64 bf16
@@ -23,7 +25,7 @@ struct BeamPart { double sum; float max, pad; };         // of a chunk: sum of 2
 
 struct BeamArgs {
   const void* logits; long long row_stride;
-  int groups, width, V, n;
+  int width, V, n;
   int chunks, chunk;                                     // of a row; logits of one
   float c;                                               // logit_scale * log2(e)
   double scale;                                          // logit_scale
@@ -150,26 +152,44 @@ __device__ __forceinline__ int select_apart(u32x4 (&raw)[kBeamLoads], double* li
     each([&](int e) { mine += beam_logit<GROUP>(raw, e) > low; });
     above = sum_of(mine);
   }
-  // of those that equal it, the n - above lowest: all below `end`
-  int end = 0;
-  for (int bit = kPlaceBits; bit >= 0; --bit) {
-    const int up = end | 1 << bit, mine_end = up - t * GROUP;
-    mine = 0;
-    each([&](int e) { mine += beam_logit<GROUP>(raw, e) == low && beam_place<GROUP>(e) < mine_end; });
-    if (sum_of(mine) <= n - above) end = up;
-  }
   __syncthreads();
   if (t == 0) count = 0;
   __syncthreads();
-  const int mine_end = end - t * GROUP;
   each([&](int e) {
-    const float z = beam_logit<GROUP>(raw, e);
-    if (z > low || (z == low && beam_place<GROUP>(e) < mine_end)) list[atomicAdd(&count, 1)] = list_entry(z, t * GROUP + beam_place<GROUP>(e));
+    if (beam_logit<GROUP>(raw, e) > low) list[atomicAdd(&count, 1)] = list_entry(beam_logit<GROUP>(raw, e), t * GROUP + beam_place<GROUP>(e));
   });
+  // Of those that equal it the n - above lowest tokens: a load after the other, whose places go by lane.  Of a mask, the first.
+  int found = above;
+#pragma unroll
+  for (int i = 0; i < kBeamLoads; ++i)
+    if (found < n) {
+      mine = 0;
+#pragma unroll
+      for (int j = 0; j < GROUP; ++j) mine += beam_logit<GROUP>(raw, i * GROUP + j) == low;
+      const int upto = (int)dpp_scan_add_u32((uint32_t)mine);
+      __syncthreads();
+      if (lane == 63) wave_n[w] = upto;
+      __syncthreads();
+      int place = found + upto - mine;
+      for (int j = 0; j < kBeamWaves; ++j) {
+        place += j < w ? wave_n[j] : 0;
+        found += wave_n[j];
+      }
+#pragma unroll
+      for (int j = 0; j < GROUP; ++j)
+        if (beam_logit<GROUP>(raw, i * GROUP + j) == low) {
+          if (place < n) list[place] = list_entry(low, t * GROUP + beam_place<GROUP>(i * GROUP + j));
+          ++place;
+        }
+    }
   __syncthreads();
-  return count;
+  return min(found, n);
 }
 
+// The chunk stays in registers: its maxima give the bound from which on logits can be among the n best -- n of the 256 lanes' maxima reach it,
+// and few logits more --, its sum follows, and what reaches the bound is ranked in LDS.
+// fp32 is bound by reading: 256 rows of V = 152064, a tenth of them finished, n = 8 28.8 us, 4.9 TB/s.  bf16 by vector instructions: 224 rows of
+// 151643 20 us for n = 1 (floor 13), 26 for n = 64, of which they are busy for 17.5: unpacking, an exponential's four passes, the ranks.
 template <bool BF16>
 __global__ __launch_bounds__(kBeamThreads) void beam_chunk_kernel(BeamArgs a) {
   constexpr int kGroup = BF16 ? 8 : 4, kEach = kBeamLoads * kGroup;      // logits of a 16-byte load, of a lane
@@ -478,7 +498,8 @@ __device__ inline void store_missing(const BeamArgs& a, int kept) {
   }
 }
 
-// A group whose lists have up to kMergeFew entries together: all of them in registers.
+// A group whose lists have up to kMergeFew entries together: all of them in registers.  Latency, of the loads and a dozen barriers: 64 groups
+// with 608 entries 6.5 us, one with 64 4.1.
 constexpr int kMergeFew = 1024;
 __global__ __launch_bounds__(256) void beam_merge_few_kernel(BeamArgs a) {
   constexpr int kEach = kMergeFew / 256;
@@ -530,7 +551,7 @@ __global__ __launch_bounds__(256) void beam_merge_few_kernel(BeamArgs a) {
 }
 
 // Any group.  The lists are in order, so the n-th best of their heads bounds what can be selected, and a list whose head is the
-// r-th best can give its n - r first entries at most.
+// r-th best can give its n - r first entries at most.  7 groups of 32 beams, 320 lists of 64 each: 15.7 us, latency too.
 constexpr int kMergeThreads = 1024;
 constexpr int kMergeLists = SIP_MAX_BEAMS * 64;
 constexpr int kMergeRoom = SIP_MAX_CONTINUATIONS * (SIP_MAX_CONTINUATIONS + 1) / 2;
@@ -600,7 +621,7 @@ __global__ __launch_bounds__(kMergeThreads) void beam_merge_kernel(BeamArgs a) {
 struct ReorderArgs {
   StateHeader* head;
   int* len; int* ndist; int* tokens; uint32_t* table;
-  int slots, L_max, groups, width;
+  int slots, L_max, width;
   const int* slot_of_row; const int* parents; const int* new_tokens;
   int token_blocks;                                      // of 4 KB of a slot's token row; the table has eight more
 };
@@ -716,7 +737,7 @@ __device__ inline Appended appended_of(const ReorderArgs& a, int group, const Mo
   return x;
 }
 
-// A workgroup a group, and all in one launch.
+// A workgroup a group, and all in one launch.  (sip_search.h has the figures of both ways.)
 constexpr int kGroupThreads = 1024, kGroupWidth = 8;
 static_assert(kGroupThreads * 4 == kTableSlots, "a bucket a thread");
 __global__ __launch_bounds__(kGroupThreads) void state_reorder_group_kernel(ReorderArgs a) {
@@ -731,11 +752,12 @@ __global__ __launch_bounds__(kGroupThreads) void state_reorder_group_kernel(Reor
   if (t < a.width && m.to >= 0) append_token(a, m.to, x.n, x.nd, x.token);
 }
 
-// Wide groups and long rows: 4 KB of a group's slots a workgroup ...
+// Wide groups and long rows: 4 KB of a group's slots a workgroup ...  64 groups of 8 slots with 3000 tokens each: 9 to 13 us for 33 MB read and
+// written, latency: slots, then lengths, then the loads, then the stores.
 template <int WIDTH>
 __global__ __launch_bounds__(kReorderThreads) void state_reorder_kernel(ReorderArgs a) {
   __shared__ Moves<WIDTH> s;
-  const int blocks = a.token_blocks + 8, g = blockIdx.x / blocks, block = blockIdx.x % blocks, t = threadIdx.x;
+  const int g = blockIdx.x, block = blockIdx.y, t = threadIdx.x;
   const bool table = block >= a.token_blocks;
   find_moves(a, g, s, !table);
   if (table) move_table(a, s, ((block - a.token_blocks) * kReorderThreads + t) * 4);
