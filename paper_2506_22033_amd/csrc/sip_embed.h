@@ -57,7 +57,8 @@ struct EmbedArgs {
   void* out; long long out_stride; int out_bf16;
 };
 
-// A lane takes eight neighbours of a row, or of kEmbedAhead rows, all under way at once.
+// A lane takes eight neighbours of a row, or of kEmbedAhead rows, all under way at once.  Bound by memory: 16000 tokens of 4096 bf16 40 us, 4.5 TB/s
+// of the distinct rows and what is written; a few tokens by a launch and two reads, 2.9 us.
 template <bool CODES, int kEmbedAhead>
 __global__ __launch_bounds__(256) void embed_kernel(EmbedArgs a) {
   const uint32_t per_row = a.D / 8, total = per_row * (uint32_t)a.N;                        // (up to 2^31)
@@ -303,8 +304,11 @@ __device__ inline LdsEntries sort_bucket(const EmbedGradArgs& a, LdsEntries from
   return to;
 }
 
-// A workgroup a bucket.  The workgroups behind fill grad_weight with zeros meanwhile, unless it is added to.  ROOM: entries of a bucket
-// that LDS holds, twice; larger buckets are sorted in the workspace.
+// A workgroup a bucket, up to 128 of them, each of which reads all tokens: no counts are exchanged, and none waits for another.  The
+// workgroups behind fill grad_weight with zeros meanwhile, unless it is added to.  ROOM: entries of a bucket that LDS holds, twice; larger buckets
+// are sorted in the workspace.
+// 8192 tokens 10 us, 65536 21, and 41 where one token is an eighth of them: reading, and the largest bucket.  Beside 1.24 GB of zeros
+// that is hidden: 211 us, 5.9 TB/s.
 template <int ROOM>
 __global__ __launch_bounds__(kSortThreads) void embed_sort_kernel(EmbedGradArgs a) {
   __shared__ uint32_t room[2][ROOM];
@@ -354,6 +358,8 @@ __device__ inline void embed_store(const EmbedGradArgs& a, long long at, f32x8 s
 }
 
 // A lane: eight columns of one piece, eight rows under way at once, and where they are added to the rows of grad_weight that end there.
+// Bound by memory: 8192 rows of 4096 bf16, a tenth masked, added to 3500 rows of bf16 26.5 us, 4.4 TB/s; 65536 of 2048 to as many rows of fp32 275 us,
+// 4.9 TB/s.
 constexpr int kSumAhead = 8;
 template <bool BF16, bool ADD>
 __global__ __launch_bounds__(256) void embed_sum_kernel(EmbedGradArgs a) {
@@ -419,6 +425,7 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(EmbedGradArgs a) {
 
 // A small gradient in one launch: a workgroup a bucket, which sums its tokens' rows itself and clears the bucket's others.  The sorted
 // entries go to groups of waves that cover a row each, a run of entries a group; what crosses the end of a run goes through LDS.
+// 384 tokens, 4096 x 512 fp32: 8.9 us instead of the three kernels' 16.
 constexpr int kSmallTokens = 1024, kSmallWidth = kSortWaves * 512;
 template <bool BF16, bool ADD>
 __global__ __launch_bounds__(kSortThreads) void embed_small_kernel(EmbedGradArgs a) {
@@ -493,7 +500,8 @@ __global__ __launch_bounds__(kSortThreads) void embed_small_kernel(EmbedGradArgs
 }
 
 // The tokens that begin in a piece and go on behind its right border: 64 lanes of eight columns, of which each has sixteen workers
-// that take every sixteenth of the token's pieces.  A workgroup looks at kJoinPieces of them.
+// that take every sixteenth of the token's pieces.  A workgroup looks at kJoinPieces of them.  Latency, 2 us where there is nothing to join
+// and 8.5 for the 18 most frequent tokens of 8192.
 constexpr int kJoinPieces = 4;
 template <bool ADD>
 __global__ __launch_bounds__(1024) void embed_join_kernel(EmbedGradArgs a) {
