@@ -21,7 +21,7 @@ constexpr int kBeamLoads = 8;                            // 16-byte loads of a l
 constexpr int kBeamList = 512;                           // entries that a chunk's list may have before it is ranked
 inline __host__ __device__ int beam_chunk(bool bf16) { return kBeamThreads * kBeamLoads * (bf16 ? 8 : 4); }
 
-struct BeamPart { double sum; float max, pad; };         // of a chunk: sum of 2^(c (z - max))
+struct BeamPart { double sum; float max, off; };         // of a chunk: sum of 2^(c (z - max) + off)
 
 struct BeamArgs {
   const void* logits; long long row_stride;
@@ -103,10 +103,9 @@ __device__ __forceinline__ float beam_logit(const u32x4 (&raw)[kBeamLoads], int 
 }
 
 // A chunk with more than kBeamList logits from the bound on, nearly equal ones or a mask's many equal ones: its n first entries to the list
-// (any order).  The n-th largest logit is found, and among those that equal it the lowest tokens.
+// (any order).  m is the largest; the chunk has `left` places.  The n-th largest logit is found, and among those that equal it the lowest tokens.
 template <int GROUP>
-__device__ __forceinline__ int select_apart(u32x4 (&raw)[kBeamLoads], double* list, int& count, int (&wave_n)[kBeamWaves], float from, int n) {
-  constexpr int kEach = kBeamLoads * GROUP;
+__device__ __forceinline__ int select_apart(u32x4 (&raw)[kBeamLoads], double* list, int& count, int (&wave_n)[kBeamWaves], float from, float m, int n, int left) {
   const int t = threadIdx.x, lane = t & 63, w = t >> 6;
   auto sum_of = [&](int mine) {                          // over the workgroup
     for (int d = 32; d; d >>= 1) mine += __shfl_xor(mine, d);
@@ -115,15 +114,16 @@ __device__ __forceinline__ int select_apart(u32x4 (&raw)[kBeamLoads], double* li
     __syncthreads();
     return wave_n[0] + wave_n[1] + wave_n[2] + wave_n[3];
   };
-  // f(e) of all logits, eight at a time
+  // f(e) of all logits, a load at a time
   auto each = [&](auto f) {
 #pragma unroll
     for (int i = 0; i < kBeamLoads; ++i) asm volatile("" : "+v"(raw[i]));        // (nothing of it is kept)
 #pragma unroll
-    for (int e = 0; e < kEach; ++e) {
-      f(e);
-      if (e % 8 == 7) __builtin_amdgcn_sched_barrier(0);
-    }
+    for (int i = 0; i < kBeamLoads; ++i)
+      if (i * kBeamThreads * GROUP < left) {
+#pragma unroll
+        for (int j = 0; j < GROUP; ++j) f(i * GROUP + j);
+      }
   };
   // The smallest from the bound on: a mask's value, as a rule.
   float low = INFINITY;
@@ -137,9 +137,10 @@ __device__ __forceinline__ int select_apart(u32x4 (&raw)[kBeamLoads], double* li
   each([&](int e) { mine += beam_logit<GROUP>(raw, e) > low; });
   int above = sum_of(mine);
   if (above >= n) {
-    // the n-th largest, bit by bit: the largest value that n logits reach
-    uint32_t at = 0;
-    for (int bit = 31; bit >= 0; --bit) {
+    // the n-th largest, bit by bit from the first one on in which the smallest and the largest differ: the largest value that n logits reach
+    const int first = 31 - __builtin_clz(ordered(low) ^ ordered(m));
+    uint32_t at = ordered(low) & ~((2ull << first) - 1);
+    for (int bit = first; bit >= (GROUP == 8 ? 16 : 0); --bit) {         // (bf16 has sixteen)
       const uint32_t up = at | 1u << bit;
       if (up > 0xff800000u) continue;                    // (beyond +inf)
       const float least = unordered(up);
@@ -147,6 +148,7 @@ __device__ __forceinline__ int select_apart(u32x4 (&raw)[kBeamLoads], double* li
       if (up >= 0x007fffffu) each([&](int e) { mine += beam_logit<GROUP>(raw, e) >= least; });
       if (up < 0x007fffffu || sum_of(mine) >= n) at = up;
     }
+    if (GROUP == 8 && !(at & 0x80000000u)) at |= 0xffffu;                // (those below 0 end in ones)
     low = unordered(at);
     mine = 0;
     each([&](int e) { mine += beam_logit<GROUP>(raw, e) > low; });
@@ -260,7 +262,9 @@ __global__ __launch_bounds__(kBeamThreads) void beam_chunk_kernel(BeamArgs a) {
   // The wave's n/4-th largest maximum of a lane, by its leading bits: of four waves, the smallest is at most the n-th largest logit.
   const uint32_t lane_max = ordered(m);
   uint32_t least_of_wave = 0;
-  const int wanted = (a.n + kBeamWaves - 1) / kBeamWaves;
+  int wanted = (a.n + kBeamWaves - 1) / kBeamWaves;
+  const int lanes = (a.V - chunk * a.chunk + kGroup - 1) / kGroup, live = min(max(lanes - w * 64, 0), 64);
+  if (lanes < kBeamThreads) wanted = (a.n * live + lanes - 1) / lanes;  // (a short chunk: of each wave by the lanes that have logits)
   for (int bit = 31; bit >= 16; --bit) {
     const uint32_t up = least_of_wave | 1u << bit;
     if (__popcll(__ballot(lane_max >= up)) >= wanted) least_of_wave = up;
@@ -268,7 +272,7 @@ __global__ __launch_bounds__(kBeamThreads) void beam_chunk_kernel(BeamArgs a) {
   const uint32_t largest = dpp_scan_max_u32(lane_max);
   if (lane == 63) {
     wave_max[w] = unordered(largest);
-    wave_least[w] = least_of_wave;
+    wave_least[w] = live > 0 ? least_of_wave : 0xffffffffu;
   }
   if (t == 0) count = 0;
   __syncthreads();
@@ -286,17 +290,19 @@ __global__ __launch_bounds__(kBeamThreads) void beam_chunk_kernel(BeamArgs a) {
   const int upto = (int)dpp_scan_add_u32((uint32_t)mine);
   int place = 0;
   if (lane == 63) place = atomicAdd(&count, upto);
-  // Meanwhile the sum.  2^(c z - c max) with c rounded to 24 bits, 2^-25 of the exponent off at most.
+  // Meanwhile the sum.  2^(c z - c max) with c rounded to 24 bits, 2^-25 of the exponent off at most; what the product c max is rounded by is
+  // kept beside it.
   const float base = m == -INFINITY ? 0.0f : m, top = base * a.c;
+  const bool near = fabsf(top) < 1e6f;
   float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
   hide();
-  if (fabsf(top) < 3e38f) {
+  if (near) {
 #pragma unroll
     for (int e = 0; e < kEach; ++e) {
       s[e & 3] += __builtin_amdgcn_exp2f(__builtin_fmaf(value(e), a.c, -top));
       if (e % 8 == 7) __builtin_amdgcn_sched_barrier(0);
     }
-  } else {                                               // (a row of the lowest values, or +inf)
+  } else {                                               // (a row of a mask's values, or +inf)
 #pragma unroll
     for (int e = 0; e < kEach; ++e) {
       s[e & 3] += __builtin_amdgcn_exp2f((value(e) - base) * a.c);
@@ -324,11 +330,11 @@ __global__ __launch_bounds__(kBeamThreads) void beam_chunk_kernel(BeamArgs a) {
     BeamPart p;
     p.sum = (wave_sum[0] + wave_sum[1]) + (wave_sum[2] + wave_sum[3]);
     p.max = m;
-    p.pad = 0.0f;
+    p.off = near ? __builtin_fmaf(base, a.c, -top) : 0.0f;
     a.part[blockIdx.x] = p;
   }
   int listed = count;
-  if (listed > kBeamList) listed = select_apart<kGroup>(raw, list, count, wave_n, from, a.n);
+  if (listed > kBeamList) listed = select_apart<kGroup>(raw, list, count, wave_n, from, m, a.n, a.V - chunk * a.chunk);
   unsigned long long* out = a.cand + (long long)blockIdx.x * a.n;
   for (int i = t; i < listed; i += kBeamThreads) {
     const double mine = list[i];
@@ -353,10 +359,10 @@ __device__ inline int rest_token(unsigned long long rest) { return (int)(0xfffff
 __device__ inline float rest_logit(unsigned long long rest) { return unordered((uint32_t)(rest >> 20)); }
 static_assert(SIP_MAX_V <= 0xfffff && SIP_MAX_BEAMS <= 1 << 12, "beam_rest() holds a beam, a logit and a token");
 
-// The group's rows, in LDS.
+// The group's rows, in LDS.  Logits count from a row's largest on, lse with them: a mask's value may be any.
 struct BeamGroup {
   double lse[SIP_MAX_BEAMS];
-  float score[SIP_MAX_BEAMS], scale[SIP_MAX_BEAMS];
+  float top[SIP_MAX_BEAMS], score[SIP_MAX_BEAMS], scale[SIP_MAX_BEAMS];
   int what[SIP_MAX_BEAMS];
 };
 template <int THREADS>
@@ -376,10 +382,11 @@ __device__ inline void load_group(const BeamArgs& a, BeamGroup& rows) {
     }
     float top = p.max;
     for (int d = 1; d < lanes; d <<= 1) top = fmaxf(top, __shfl_xor(top, d));
-    double s = p.max > -INFINITY ? p.sum * exp2(((double)p.max - (double)top) * (double)a.c) : p.sum;
+    double s = p.max > -INFINITY ? p.sum * exp2(((double)p.max - (double)top) * (double)a.c - (double)p.off) : p.sum;
     for (int d = 1; d < lanes; d <<= 1) s += __shfl_xor(s, d);
     if (k < K && chunk == 0) {
-      rows.lse[k] = (double)top * a.scale + log(s);
+      rows.lse[k] = log(s);
+      rows.top[k] = top;
       rows.score[k] = row.score;
       rows.scale[k] = row.scale;
       // (NaN or +inf somewhere, or nothing but -inf: no continuation)
@@ -388,7 +395,7 @@ __device__ inline void load_group(const BeamArgs& a, BeamGroup& rows) {
   }
 }
 __device__ inline double total_of(const BeamArgs& a, const BeamGroup& rows, int k, float z) {
-  return (double)rows.score[k] + ((double)z * a.scale - rows.lse[k]);
+  return (double)rows.score[k] + (((double)z - (double)rows.top[k]) * a.scale - rows.lse[k]);
 }
 // Entry e of list l (of beam l / chunks), whose key is `key`; total 0: there is none.
 __device__ inline BeamRank rank_of(const BeamArgs& a, const BeamGroup& rows, int l, int e, unsigned long long key) {
@@ -400,14 +407,15 @@ __device__ inline BeamRank rank_of(const BeamArgs& a, const BeamGroup& rows, int
 }
 
 // The leading bits of the n-th largest of the workgroup's values, EACH a lane: two bits a turn, of which votes[turn] counts the values
-// that reach the three possibilities (zeros before; a barrier a turn).  0 if there are fewer than n.
-constexpr int kVoteTurns = 12;
+// that reach the three possibilities (zeros before; a barrier a turn).  `reach` says how many reach it, before: of how many; no more than `enough` end
+// the search.  0 if there are fewer than n.
+constexpr int kVoteTurns = 16;
 typedef int BeamVotes[kVoteTurns][4];
 template <int EACH>
-__device__ inline uint32_t nth_largest(const uint32_t (&x)[EACH], int n, BeamVotes& votes) {
+__device__ inline uint32_t nth_largest(const uint32_t (&x)[EACH], int n, int enough, int& reach, BeamVotes& votes) {
   const int lane = threadIdx.x & 63;
   uint32_t from = 0;
-  for (int turn = 0; turn < kVoteTurns; ++turn) {
+  for (int turn = 0; turn < kVoteTurns && reach > enough; ++turn) {
     const int bit = 30 - 2 * turn;
     int mine[3] = {0, 0, 0};
 #pragma unroll
@@ -419,7 +427,7 @@ __device__ inline uint32_t nth_largest(const uint32_t (&x)[EACH], int n, BeamVot
     const int4 all = *reinterpret_cast<const int4*>(votes[turn]);
     const int step = (all.x >= n) + (all.y >= n) + (all.z >= n);
     from |= (uint32_t)step << bit;
-    if (step && (step == 1 ? all.x : step == 2 ? all.y : all.z) == n) break;
+    if (step) reach = step == 1 ? all.x : step == 2 ? all.y : all.z;
   }
   return from;
 }
@@ -451,6 +459,56 @@ __device__ inline uint32_t nth_head(uint32_t lead, int lists, int n, uint32_t (&
   if (t < lists && ranks[t] == n - 1) bound = heads[t] & ~kLast;
   __syncthreads();
   return bound;
+}
+
+// Of m entries the n largest and few more, up to `enough` in all; m > enough >= n.  By the leading word of their ranks, and where that is equal
+// by the next.  What it saves: ranking 8000 entries among one another takes 2 ms.
+template <int THREADS, int ROOM>
+__device__ inline int keep_largest(BeamRank* found, int m, int n, int enough, BeamVotes& votes, int& count) {
+  constexpr int kEach = (ROOM + THREADS - 1) / THREADS;
+  const int t = threadIdx.x;
+  BeamRank x[kEach];
+  bool open[kEach], kept[kEach];                         // equal to the bound so far; above it
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) {
+    open[i] = t + i * THREADS < m;
+    kept[i] = false;
+    x[i] = open[i] ? found[t + i * THREADS] : BeamRank{0, 0};
+  }
+  int above = 0, reach = m;
+  __syncthreads();                                       // (everybody has read `count`)
+  for (int w = 0; w < 4; ++w) {
+    uint32_t word[kEach];
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) word[i] = open[i] ? (uint32_t)((w < 2 ? x[i].total : x[i].rest) >> (w & 1 ? 0 : 32)) : 0;
+    if (t < kVoteTurns * 4) votes[t / 4][t % 4] = 0;
+    if (t == 0) count = 0;
+    __syncthreads();
+    const uint32_t from = nth_largest(word, n - above, enough - above, reach, votes);
+    const bool last = above + reach <= enough;           // (else `from` is the n-th largest word, all of it)
+    int mine = 0;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      const bool up = open[i] && (last ? word[i] >= from : word[i] > from);
+      kept[i] |= up;
+      mine += up;
+      open[i] &= word[i] == from;
+    }
+    if (last) break;
+    if (mine) atomicAdd(&count, mine);
+    __syncthreads();
+    above += count;
+    reach -= count;
+    __syncthreads();
+  }
+  __syncthreads();
+  if (t == 0) count = 0;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < kEach; ++i)
+    if (kept[i]) found[atomicAdd(&count, 1)] = x[i];
+  __syncthreads();
+  return count;
 }
 
 // f(rank, i) for each of n entries, i's place among them.  Begins and ends with the entries visible to all.
@@ -500,7 +558,8 @@ __device__ inline void store_missing(const BeamArgs& a, int kept) {
 
 // A group whose lists have up to kMergeFew entries together: all of them in registers.  Latency, of the loads and a dozen barriers: 64 groups
 // with 608 entries 6.5 us, one with 64 4.1.
-constexpr int kMergeFew = 1024;
+constexpr int kMergeFew = 1024, kRankFew = 192;           // (entries that are ranked among one another at most)
+static_assert(kRankFew >= SIP_MAX_CONTINUATIONS, "all that are selected");
 __global__ __launch_bounds__(256) void beam_merge_few_kernel(BeamArgs a) {
   constexpr int kEach = kMergeFew / 256;
   __shared__ BeamGroup rows;
@@ -530,7 +589,7 @@ __global__ __launch_bounds__(256) void beam_merge_few_kernel(BeamArgs a) {
   const int lists = a.width * a.chunks;
   uint32_t from = 0;
   if (entries <= 64) from = 0;                           // (so few are compared with one another at once)
-  else if (lists <= kHeadsMost) {
+  else if (lists >= a.n && lists <= kHeadsMost) {
     // entry 0 of list t is entry t * n of all
 #pragma unroll
     for (int i = 0; i < kEach; ++i)
@@ -538,21 +597,23 @@ __global__ __launch_bounds__(256) void beam_merge_few_kernel(BeamArgs a) {
     __syncthreads();
     from = nth_head<256>(t < lists ? first[t] : 0, lists, a.n, heads, ranks, bound);
   } else {
-    from = nth_largest(lead, a.n, votes);
+    int reach = entries;
+    from = nth_largest(lead, a.n, max(a.n, 64), reach, votes);
   }
   from = max(from, 1u);                                  // (0: there is none)
 #pragma unroll
   for (int i = 0; i < kEach; ++i)
     if (lead[i] >= from) found[atomicAdd(&count, 1)] = x[i];
   __syncthreads();
-  const int kept = count;
+  int kept = count;
+  if (kept > kRankFew) kept = keep_largest<256, kMergeFew>(found, kept, a.n, kRankFew, votes, count);
   rank_all<256>(found, kept, ranks, [&](int rank, int i) { store_selected(a, rows, found[i], rank); });
   store_missing(a, kept);
 }
 
 // Any group.  The lists are in order, so the n-th best of their heads bounds what can be selected, and a list whose head is the
 // r-th best can give its n - r first entries at most.  7 groups of 32 beams, 320 lists of 64 each: 15.7 us, latency too.
-constexpr int kMergeThreads = 1024;
+constexpr int kMergeThreads = 1024, kRankMost = 256;
 constexpr int kMergeLists = SIP_MAX_BEAMS * 64;
 constexpr int kMergeRoom = SIP_MAX_CONTINUATIONS * (SIP_MAX_CONTINUATIONS + 1) / 2;
 static_assert(kMergeRoom >= kMergeLists, "room for all heads");
@@ -580,12 +641,15 @@ __global__ __launch_bounds__(kMergeThreads) void beam_merge_kernel(BeamArgs a) {
     const int l = t + i * kMergeThreads;
     lead[i] = l < lists ? (uint32_t)(rank_of(a, rows, l, 0, key[i]).total >> 32) : 0;
   }
-  const uint32_t from = max(lists <= kHeadsMost ? nth_head<kMergeThreads>(lead[0], lists, n, leads, ranks, bound) : nth_largest(lead, n, votes), 1u);
+  int reach = lists;
+  const uint32_t from = max(lists < n ? 0 : lists <= kHeadsMost ? nth_head<kMergeThreads>(lead[0], lists, n, leads, ranks, bound) : nth_largest(lead, n, n, reach, votes), 1u);
 #pragma unroll
   for (int i = 0; i < kHeads; ++i)
     if (lead[i] >= from) found[atomicAdd(&count, 1)] = rank_of(a, rows, t + i * kMergeThreads, 0, key[i]);
   __syncthreads();
-  const int heads = count, selected = min(heads, n);
+  int heads = count;
+  if (heads > kRankMost) heads = keep_largest<kMergeThreads, kMergeLists>(found, heads, n, kRankMost, votes, count);
+  const int selected = min(heads, n);
   rank_all<kMergeThreads>(found, heads, ranks, [&](int rank, int i) {
     const unsigned long long rest = found[i].rest;
     const int k = rest_beam(rest);
@@ -611,7 +675,8 @@ __global__ __launch_bounds__(kMergeThreads) void beam_merge_kernel(BeamArgs a) {
     }
   }
   __syncthreads();
-  const int kept = count;
+  int kept = count;
+  if (kept > kRankMost) kept = keep_largest<kMergeThreads, kMergeRoom>(found, kept, n, kRankMost, votes, count);
   rank_all<kMergeThreads>(found, kept, ranks, [&](int rank, int i) { store_selected(a, rows, found[i], rank); });
   store_missing(a, kept);
 }

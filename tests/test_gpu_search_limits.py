@@ -4,6 +4,7 @@ import pytest
 import torch
 
 import paper_2506_22033_amd as sip
+from tests.test_gpu_beam import _check, _rows
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -30,6 +31,47 @@ def test_equal_logits_by_the_lower_token(dtype, low, share, n):
     assert parents.cpu().tolist() == [[0] * n] * 2
     want = torch.sort(z.to(dtype).float() + 0.0, dim=1, descending=True, stable=True).indices[:, :n]
     assert torch.equal(tokens.cpu().long(), want)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("groups,width,V,n", [(2, 64, 1481, 128), (1, 64, 70000, 128), (3, 20, 1116, 40), (2, 54, 1575, 54), (1, 9, 700, 60),
+                                              (2, 2, 115984, 2), (1, 30, 9000, 31), (1, 16, 1023, 64), (1, 64, 33, 128), (2, 31, 2100, 100)])
+def test_wide_groups_of_few_lists_and_short_chunks(groups, width, V, n, dtype):
+    logits, g = _rows(groups * width, V, dtype, V * n)
+    scores = -torch.rand(groups * width, generator=g, device=DEV) * 0.5
+    _check(logits, scores, width, n, sip.sip_beam_select(logits, scores, width, n))
+
+
+@pytest.mark.parametrize("width,V,n", [(64, 9000, 128), (64, 40000, 100), (8, 3000, 16), (64, 100, 3), (1, 50000, 128)])
+def test_equal_rows_of_equal_logits_by_beam_and_token(width, V, n):
+    # Every continuation of every beam has the same total: the first beam's lowest tokens, then the next one's.
+    logits = torch.zeros(width, (V + 7) // 8 * 8, device=DEV)[:, :V]
+    tokens, parents, _ = sip.sip_beam_select(logits, torch.zeros(width, device=DEV), width, n)
+    want = torch.arange(n)
+    assert torch.equal(parents[0].cpu().long(), want // V) and torch.equal(tokens[0].cpu().long(), want % V)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("scale,at", [(1e-3, 1.0), (1e-3, -1.0), (0.05, -300.0), (1.0, 0.0)])
+def test_many_logits_near_one_another(dtype, scale, at):
+    # More than a chunk's list holds reach the bound: few distinct values, above and below 0.
+    logits, g = _rows(12, 20000, F32, 5)
+    logits = torch.round(logits.clamp(-2, 2) * 2) / 2 * scale + at
+    room = torch.empty(12, 20000, dtype=dtype, device=DEV)
+    room.copy_(logits)
+    scores = -torch.arange(12, device=DEV).float() * 0.25
+    _check(room, scores, 4, 100, sip.sip_beam_select(room, scores, 4, 100))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("low", [-1e30, -1e10, 1e10, 1e35, 3e6, -2e5, 777.0])
+def test_rows_of_large_values(low, dtype):
+    # Equal logits: the total is -ln V beside the score, whatever they are.  Three of a row are lower by a quarter of it.
+    V = 20000
+    logits = torch.full((2, V), low, device=DEV).to(dtype)
+    logits[1, 5:8] = torch.tensor(low - abs(low) / 4, device=DEV).to(dtype)
+    scores = torch.tensor([-0.5, 0.0], device=DEV)
+    _check(logits, scores, 2, 9, sip.sip_beam_select(logits, scores, 2, 9))
 
 
 def test_reorder_of_more_work_than_lanes_along_a_grid():
