@@ -18,7 +18,7 @@ struct AdaptArgs {
   int B, D, V, rank, adapters;
   const uint16_t* down; const uint16_t* up;
   const int* adapter_of_row; const float* scales;
-  void* logits; long long logits_stride; int logits_bf16;
+  void* logits; long long logits_stride;
   // workspace
   int* count;                                            // batches
   int* rows;                                             // [B] rows that have an adapter, by adapter
@@ -157,12 +157,40 @@ __global__ __launch_bounds__(kDownWaves * 64) void adapt_down_kernel(AdaptArgs p
 }
 
 // The additions of one batch to `tiles` of kUpWaves * 16 logits each.  A wave's share of a tile is sixteen entries of the vocabulary, of
-// which a lane has four neighbours of one row.  VECTOR: logits are fp32 in rows that start at 16 bytes.  ONE: tiles = 1, and t may
+// which a lane has four neighbours of one row, loaded and stored at once wherever they lie.  ONE: tiles = 1, and t may
 // be in parts.
 // t enters as three bf16 parts, which hold its 24 bits: the products are exact, the matrix cores hardly busy.  Bound by memory: 224 rows, 32
 // adapters of rank 64, V = 128256, 760 MB, 165 us, 4.6 TB/s (558 us with a lane an entry of the vocabulary and fp32 products).
 constexpr int kUpWaves = 4, kUpEntries = kUpWaves * 16;
-template <int STEPS, bool ONE, bool DIRECT, bool VECTOR>
+struct __attribute__((packed, aligned(4))) FourF32 { f32x4 x; };         // four logits as they may lie: aligned to one
+struct __attribute__((packed, aligned(2))) FourBf16 { uint32_t w[2]; };
+template <bool BF16>
+__device__ inline f32x4 load_logits(const void* logits, long long at) {
+  if constexpr (!BF16) return reinterpret_cast<const FourF32*>(static_cast<const float*>(logits) + at)->x;
+  const FourBf16 z = *reinterpret_cast<const FourBf16*>(static_cast<const uint16_t*>(logits) + at);
+  f32x4 x;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const uint32_t w = e & 1 ? z.w[e / 2] & 0xffff0000u : z.w[e / 2] << 16;
+    x[e] = __builtin_bit_cast(float, w);
+  }
+  return x;
+}
+template <bool BF16>
+__device__ inline void store_logits(void* logits, long long at, const f32x4& x) {
+  if constexpr (!BF16) {
+    *reinterpret_cast<FourF32*>(static_cast<float*>(logits) + at) = FourF32{x};
+  } else {
+    FourBf16 z;
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const float lo = x[2 * e], hi = x[2 * e + 1];
+      z.w[e] = __builtin_bit_cast(uint16_t, (__bf16)lo) | (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)hi) << 16;
+    }
+    *reinterpret_cast<FourBf16*>(static_cast<uint16_t*>(logits) + at) = z;
+  }
+}
+template <int STEPS, bool ONE, bool DIRECT, bool BF16>
 __global__ __launch_bounds__(kUpWaves * 64) void adapt_up_kernel(AdaptArgs p, int batches, int tiles) {
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, k = 8 * (lane >> 4);
   // batches of one adapter go through the same entries one after the other on one XCD, whose L2 then has them
@@ -189,12 +217,12 @@ __global__ __launch_bounds__(kUpWaves * 64) void adapt_up_kernel(AdaptArgs p, in
       l.z[j] = f32x4{0, 0, 0, 0};
       if (x.row < 0 || at >= p.V) continue;
       const long long z0 = x.row * p.logits_stride + at;
-      if (VECTOR && at + 4 <= p.V) {
-        l.z[j] = *reinterpret_cast<const f32x4*>(static_cast<const float*>(p.logits) + z0);
+      if (at + 4 <= p.V) {
+        l.z[j] = load_logits<BF16>(p.logits, z0);
       } else {
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (at + e < p.V) l.z[j][e] = p.logits_bf16 ? (float)static_cast<const __bf16*>(p.logits)[z0 + e] : static_cast<const float*>(p.logits)[z0 + e];
+        for (int e = 0; e < 3; ++e)
+          if (at + e < p.V) l.z[j][e] = BF16 ? (float)static_cast<const __bf16*>(p.logits)[z0 + e] : static_cast<const float*>(p.logits)[z0 + e];
       }
     }
   };
@@ -231,13 +259,13 @@ __global__ __launch_bounds__(kUpWaves * 64) void adapt_up_kernel(AdaptArgs p, in
       acc += now.z[j];
       if (x.row < 0 || at >= p.V) continue;
       const long long z0 = x.row * p.logits_stride + at;
-      if (VECTOR && at + 4 <= p.V) {
-        *reinterpret_cast<f32x4*>(static_cast<float*>(p.logits) + z0) = acc;
+      if (at + 4 <= p.V) {
+        store_logits<BF16>(p.logits, z0, acc);
       } else {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
+        for (int e = 0; e < 3; ++e) {
           if (at + e >= p.V) break;
-          if (p.logits_bf16) static_cast<__bf16*>(p.logits)[z0 + e] = (__bf16)acc[e];
+          if (BF16) static_cast<__bf16*>(p.logits)[z0 + e] = (__bf16)acc[e];
           else static_cast<float*>(p.logits)[z0 + e] = acc[e];
         }
       }

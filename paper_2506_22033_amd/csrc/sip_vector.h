@@ -226,12 +226,11 @@ sip_status sip_head_adapt(const void* hidden, int32_t B, int32_t D, int64_t hidd
   a.B = B; a.D = D; a.V = V; a.rank = rank; a.adapters = adapters;
   a.down = static_cast<const uint16_t*>(down); a.up = static_cast<const uint16_t*>(up);
   a.adapter_of_row = adapter_of_row; a.scales = scales;
-  a.logits = logits; a.logits_stride = logits_stride; a.logits_bf16 = logits_dtype == SIP_BF16;
+  a.logits = logits; a.logits_stride = logits_stride;
   a.count = reinterpret_cast<int*>(ws + pl.count);
   a.rows = reinterpret_cast<int*>(ws + pl.rows);
   a.batch = reinterpret_cast<int4*>(ws + pl.batch);
   a.t = reinterpret_cast<float*>(ws + pl.t);
-  const bool vector = logits_dtype == SIP_F32 && aligned16(logits) && logits_stride % 4 == 0;
   hipStream_t stream = static_cast<hipStream_t>(hip_stream);
   const bool direct = B <= sip::kAdaptDirect;
   const int batches = adapt_batches(B, adapters), steps = tiles(rank, 32);
@@ -245,19 +244,19 @@ sip_status sip_head_adapt(const void* hidden, int32_t B, int32_t D, int64_t hidd
     constexpr bool kDirect = decltype(in_direct)::value;
     if (hidden_dtype == SIP_BF16) hipLaunchKernelGGL((sip::adapt_down_kernel<true, kDirect>), down_grid, dim3(sip::kDownWaves * 64), 0, stream, a);
     else hipLaunchKernelGGL((sip::adapt_down_kernel<false, kDirect>), down_grid, dim3(sip::kDownWaves * 64), 0, stream, a);
-    auto add = [&](auto in_steps, auto in_vector) {
+    auto add = [&](auto in_steps, auto in_bf16) {
       constexpr int kSteps = decltype(in_steps)::value;
-      constexpr bool kVector = decltype(in_vector)::value;
-      if (each == 1) hipLaunchKernelGGL((sip::adapt_up_kernel<kSteps, true, kDirect, kVector>), up_grid, dim3(sip::kUpWaves * 64), 0, stream, a, batches, each);
-      else hipLaunchKernelGGL((sip::adapt_up_kernel<kSteps, false, kDirect, kVector>), up_grid, dim3(sip::kUpWaves * 64), 0, stream, a, batches, each);
+      constexpr bool kBf16 = decltype(in_bf16)::value;
+      if (each == 1) hipLaunchKernelGGL((sip::adapt_up_kernel<kSteps, true, kDirect, kBf16>), up_grid, dim3(sip::kUpWaves * 64), 0, stream, a, batches, each);
+      else hipLaunchKernelGGL((sip::adapt_up_kernel<kSteps, false, kDirect, kBf16>), up_grid, dim3(sip::kUpWaves * 64), 0, stream, a, batches, each);
     };
-    auto add_steps = [&](auto in_vector) {
-      if (steps == 1) add(std::integral_constant<int, 1>{}, in_vector);
-      else if (steps == 2) add(std::integral_constant<int, 2>{}, in_vector);
-      else if (steps == 3) add(std::integral_constant<int, 3>{}, in_vector);
-      else add(std::integral_constant<int, 4>{}, in_vector);
+    auto add_steps = [&](auto in_bf16) {
+      if (steps == 1) add(std::integral_constant<int, 1>{}, in_bf16);
+      else if (steps == 2) add(std::integral_constant<int, 2>{}, in_bf16);
+      else if (steps == 3) add(std::integral_constant<int, 3>{}, in_bf16);
+      else add(std::integral_constant<int, 4>{}, in_bf16);
     };
-    if (vector) add_steps(std::true_type{});
+    if (logits_dtype == SIP_BF16) add_steps(std::true_type{});
     else add_steps(std::false_type{});
   };
   if (direct) launch(std::true_type{});
