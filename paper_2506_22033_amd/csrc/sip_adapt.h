@@ -156,38 +156,37 @@ __global__ __launch_bounds__(kDownWaves * 64) void adapt_down_kernel(AdaptArgs p
   *reinterpret_cast<f32x4*>(p.t + at * p.rank + j0) = acc * scale;
 }
 
-// The additions of one batch to `tiles` of kUpWaves * 16 logits each.  A wave's share of a tile is sixteen entries of the vocabulary, of
-// which a lane has four neighbours of one row, loaded and stored at once wherever they lie.  ONE: tiles = 1, and t may
-// be in parts.
+// The additions of one batch to `tiles` of kUpWaves * 32 logits each.  A wave's share of a tile is 32 entries of the vocabulary, of
+// which a lane has eight neighbours of one row, loaded and stored wherever they lie: two matrix products, one for the first four of every
+// eight, one for the others (four a lane are 32 bytes of a bf16 row at once: 219 rows, 40 adapters of rank 8, V = 214517 140 us in all instead of 92).  ONE: tiles = 1, and t may be in parts.
 // t enters as three bf16 parts, which hold its 24 bits: the products are exact, the matrix cores hardly busy.  Bound by memory: 224 rows, 32
-// adapters of rank 64, V = 128256, 760 MB, 165 us, 4.6 TB/s (558 us with a lane an entry of the vocabulary and fp32 products).
-constexpr int kUpWaves = 4, kUpEntries = kUpWaves * 16;
-struct __attribute__((packed, aligned(4))) FourF32 { f32x4 x; };         // four logits as they may lie: aligned to one
-struct __attribute__((packed, aligned(2))) FourBf16 { uint32_t w[2]; };
+// adapters of rank 64, V = 128256, 760 MB, 162 us, 4.7 TB/s (558 us with a lane an entry of the vocabulary and fp32 products).
+constexpr int kUpWaves = 4, kUpEntries = kUpWaves * 32;
+struct __attribute__((packed, aligned(4))) FourF32 { f32x4 x; };        // four logits as they may lie: aligned to one
+struct __attribute__((packed, aligned(2))) EightBf16 { u32x4 x; };
 template <bool BF16>
-__device__ inline f32x4 load_logits(const void* logits, long long at) {
-  if constexpr (!BF16) return reinterpret_cast<const FourF32*>(static_cast<const float*>(logits) + at)->x;
-  const FourBf16 z = *reinterpret_cast<const FourBf16*>(static_cast<const uint16_t*>(logits) + at);
-  f32x4 x;
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    const uint32_t w = e & 1 ? z.w[e / 2] & 0xffff0000u : z.w[e / 2] << 16;
-    x[e] = __builtin_bit_cast(float, w);
+__device__ inline f32x8 load_logits(const void* logits, long long at) {
+  Eight x;
+  if constexpr (BF16) {
+    x.w[0] = reinterpret_cast<const EightBf16*>(static_cast<const uint16_t*>(logits) + at)->x;
+  } else {
+    const FourF32* p = reinterpret_cast<const FourF32*>(static_cast<const float*>(logits) + at);
+    x.w[0] = __builtin_bit_cast(u32x4, p[0]);
+    x.w[1] = __builtin_bit_cast(u32x4, p[1]);
   }
-  return x;
+  return as_floats(x, BF16);
 }
 template <bool BF16>
-__device__ inline void store_logits(void* logits, long long at, const f32x4& x) {
-  if constexpr (!BF16) {
-    *reinterpret_cast<FourF32*>(static_cast<float*>(logits) + at) = FourF32{x};
-  } else {
-    FourBf16 z;
+__device__ inline void store_logits(void* logits, long long at, const f32x8& x) {
+  if constexpr (BF16) {
+    u32x4 w;
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      const float lo = x[2 * e], hi = x[2 * e + 1];
-      z.w[e] = __builtin_bit_cast(uint16_t, (__bf16)lo) | (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)hi) << 16;
-    }
-    *reinterpret_cast<FourBf16*>(static_cast<uint16_t*>(logits) + at) = z;
+    for (int e = 0; e < 4; ++e) w[e] = __builtin_bit_cast(uint16_t, (__bf16)x[2 * e]) | (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)x[2 * e + 1]) << 16;
+    *reinterpret_cast<EightBf16*>(static_cast<uint16_t*>(logits) + at) = EightBf16{w};
+  } else {
+    FourF32* p = reinterpret_cast<FourF32*>(static_cast<float*>(logits) + at);
+    p[0] = FourF32{__builtin_shufflevector(x, x, 0, 1, 2, 3)};
+    p[1] = FourF32{__builtin_shufflevector(x, x, 4, 5, 6, 7)};
   }
 }
 template <int STEPS, bool ONE, bool DIRECT, bool BF16>
@@ -200,28 +199,37 @@ __global__ __launch_bounds__(kUpWaves * 64) void adapt_up_kernel(AdaptArgs p, in
   if (x.n == 0) return;
   const uint16_t* up = p.up + (long long)x.adapter * p.V * p.rank;
   const bf16x8 none = {};
-  constexpr int kAhead = ONE ? 1 : STEPS > 2 ? 2 : 4;    // tiles whose loads are under way at once, while as many others are multiplied
+  // Tiles whose loads are under way at once, kEarly while as many others are multiplied.  More waves do better where their loads are short: rank
+  // 8 as above 92 us, kEarly 98, and with two tiles 119, four 170; rank 64 as above 1 % less with two, rank 112 2 % less kEarly.
+  constexpr bool kEarly = ONE || STEPS > 1;
+  constexpr int kAhead = ONE || STEPS != 2 ? 1 : 2;
   constexpr int kParts = ONE ? kDownParts : 1;
   struct Loads {
-    bf16x8 a[kAhead][STEPS];
-    f32x4 z[kAhead];
+    bf16x8 a[kAhead][2][STEPS];
+    f32x8 z[kAhead];
   };
-  auto first_of = [&](int tile) { return tile < tiles ? v0 + (tile * kUpWaves + w) * 16 : p.V; };       // (V: there is none)
+  auto first_of = [&](int tile) { return tile < tiles ? v0 + (tile * kUpWaves + w) * 32 : p.V; };       // (V: there is none)
+  // row r of a product is entry 8 (r / 4) + r % 4, and that plus 4 of the second one: lane l then has 8 (l / 16) and what follows of row l % 16
+  const int entry0 = 8 * ((lane & 15) >> 2) + (lane & 3), at0 = 8 * (lane >> 4);
   auto load = [&](Loads& l, int tile0) {
 #pragma unroll
     for (int j = 0; j < kAhead; ++j) {
-      const int v = first_of(tile0 + j), entry = v + (lane & 15), at = v + acc_a(lane);
+      const int v = first_of(tile0 + j), at = v + at0;
 #pragma unroll
-      for (int s = 0; s < STEPS; ++s)
-        l.a[j][s] = entry < p.V && 32 * s + k < p.rank ? *reinterpret_cast<const bf16x8*>(up + (long long)entry * p.rank + 32 * s + k) : none;
-      l.z[j] = f32x4{0, 0, 0, 0};
+      for (int half = 0; half < 2; ++half) {
+        const int entry = v + entry0 + 4 * half;
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s)
+          l.a[j][half][s] = entry < p.V && 32 * s + k < p.rank ? *reinterpret_cast<const bf16x8*>(up + (long long)entry * p.rank + 32 * s + k) : none;
+      }
+      l.z[j] = f32x8{0, 0, 0, 0, 0, 0, 0, 0};
       if (x.row < 0 || at >= p.V) continue;
       const long long z0 = x.row * p.logits_stride + at;
-      if (at + 4 <= p.V) {
+      if (at + 8 <= p.V) {
         l.z[j] = load_logits<BF16>(p.logits, z0);
       } else {
 #pragma unroll
-        for (int e = 0; e < 3; ++e)
+        for (int e = 0; e < 7; ++e)
           if (at + e < p.V) l.z[j][e] = BF16 ? (float)static_cast<const __bf16*>(p.logits)[z0 + e] : static_cast<const float*>(p.logits)[z0 + e];
       }
     }
@@ -236,7 +244,7 @@ __global__ __launch_bounds__(kUpWaves * 64) void adapt_up_kernel(AdaptArgs p, in
       if (part < p.parts && x.row >= 0 && 32 * s + k < p.rank) t_part[s][part] = load_eight(p.t, at, false);
     }
   Loads next;
-  load(next, 0);
+  if (kEarly) load(next, 0);
   Split t[STEPS];
 #pragma unroll
   for (int s = 0; s < STEPS; ++s) {
@@ -246,27 +254,32 @@ __global__ __launch_bounds__(kUpWaves * 64) void adapt_up_kernel(AdaptArgs p, in
     t[s] = split_of(sum);
   }
   for (int tile0 = 0; tile0 < tiles; tile0 += kAhead) {
+    if (!kEarly) load(next, tile0);
     const Loads now = next;
-    if (tile0 + kAhead < tiles) load(next, tile0 + kAhead);
+    if (kEarly && tile0 + kAhead < tiles) load(next, tile0 + kAhead);
 #pragma unroll
     for (int j = 0; j < kAhead; ++j) {
-      const int at = first_of(tile0 + j) + acc_a(lane);
-      f32x4 acc = {0, 0, 0, 0};
+      const int at = first_of(tile0 + j) + at0;
+      f32x4 acc[2];
 #pragma unroll
-      for (int part = 2; part >= 0; --part)
+      for (int half = 0; half < 2; ++half) {
+        acc[half] = f32x4{0, 0, 0, 0};
 #pragma unroll
-        for (int s = 0; s < STEPS; ++s) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(now.a[j][s], t[s].part[part], acc, 0, 0, 0);
-      acc += now.z[j];
+        for (int part = 2; part >= 0; --part)
+#pragma unroll
+          for (int s = 0; s < STEPS; ++s) acc[half] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(now.a[j][half][s], t[s].part[part], acc[half], 0, 0, 0);
+      }
+      const f32x8 sum = __builtin_shufflevector(acc[0], acc[1], 0, 1, 2, 3, 4, 5, 6, 7) + now.z[j];
       if (x.row < 0 || at >= p.V) continue;
       const long long z0 = x.row * p.logits_stride + at;
-      if (at + 4 <= p.V) {
-        store_logits<BF16>(p.logits, z0, acc);
+      if (at + 8 <= p.V) {
+        store_logits<BF16>(p.logits, z0, sum);
       } else {
 #pragma unroll
-        for (int e = 0; e < 3; ++e) {
+        for (int e = 0; e < 7; ++e) {
           if (at + e >= p.V) break;
-          if (BF16) static_cast<__bf16*>(p.logits)[z0 + e] = (__bf16)acc[e];
-          else static_cast<float*>(p.logits)[z0 + e] = acc[e];
+          if (BF16) static_cast<__bf16*>(p.logits)[z0 + e] = (__bf16)sum[e];
+          else static_cast<float*>(p.logits)[z0 + e] = sum[e];
         }
       }
     }
