@@ -688,90 +688,80 @@ struct ReorderArgs {
   int* len; int* ndist; int* tokens; uint32_t* table;
   int slots, L_max, width;
   const int* slot_of_row; const int* parents; const int* new_tokens;
-  int token_blocks;                                      // of 4 KB of a slot's token row; the table has eight more
 };
 
-// Where a row takes its history from: its parent's slot (-1: an empty history) and its own.  to < 0: nothing moves.  For the first
-// a.width threads, a row each; `slot` is LDS that nobody uses until the next barrier.
-struct Move { int from, to; };
-__device__ inline Move move_of(const ReorderArgs& a, int group, int* slot) {
-  const int k = threadIdx.x, row = group * a.width + k;
+// Where the rows of a group take their histories from, lane k row k's: its parent's slot (-1: an empty history), its own, and how long that history
+// is.  to < 0: nothing is appended, nor moved; a row whose parent is itself moves nothing.  For a whole wave.
+struct Move { int from, to, length; };
+__device__ inline int length_of(const ReorderArgs& a, int slot) {
+  return slot < 0 ? 0 : min(max(a.len[slot], 0), a.L_max);
+}
+__device__ inline Move move_of(const ReorderArgs& a, int group, bool lengths) {
+  const int k = threadIdx.x & 63, row = group * a.width + k;
   int p = -1, to = -1;
   if (k < a.width) {
     p = a.parents[row];
     to = a.slot_of_row[row];
-    slot[k] = to;
   }
-  __syncthreads();
-  if ((unsigned)p >= (unsigned)a.width || (unsigned)to >= (unsigned)a.slots) return {-1, -1};
-  bool taken = false;                                    // an earlier row's
-  for (int j = 0; j < k; ++j) taken |= slot[j] == to;
-  const int from = slot[p];
-  return {(unsigned)from < (unsigned)a.slots ? from : -1, taken ? -1 : to};
-}
-__device__ inline int length_of(const ReorderArgs& a, int slot) {
-  return slot < 0 ? 0 : min(max(a.len[slot], 0), a.L_max);
+  const int from = __shfl(to, p & 63);
+  unsigned long long same = __ballot((unsigned)to < (unsigned)a.slots);                    // the rows of my slot, by its bits
+  for (int b = 0; (a.slots - 1) >> b; ++b) {
+    const unsigned long long set = __ballot(to >> b & 1);
+    same &= to >> b & 1 ? set : ~set;
+  }
+  const bool taken = same & ((1ull << k) - 1);           // an earlier one's
+  Move m = {-1, -1, 0};
+  if ((unsigned)p >= (unsigned)a.width || (unsigned)to >= (unsigned)a.slots) return m;
+  m.from = (unsigned)from < (unsigned)a.slots ? from : -1;
+  m.to = taken ? -1 : to;
+  if (lengths) m.length = length_of(a, m.from);
+  return m;
 }
 
 // Sixteen bytes that are aligned to four.
 struct __attribute__((packed, aligned(4))) StateLine { uint32_t w[4]; };
 
-constexpr int kReorderThreads = 256;                     // of a workgroup that copies 4 KB of every slot of a group
-
-// The moves of a group, for all threads of a workgroup of at least WIDTH.
-template <int WIDTH>
-struct Moves {
-  Move move[WIDTH];                                      // to < 0: nothing to copy
-  int slot[WIDTH], length[WIDTH];                        // (length: of what moves)
-};
-template <int WIDTH>
-__device__ inline Move find_moves(const ReorderArgs& a, int group, Moves<WIDTH>& s, bool lengths) {
-  const Move m = move_of(a, group, s.slot);
-  if ((int)threadIdx.x < a.width) {
-    s.move[threadIdx.x] = {m.from, m.from == m.to ? -1 : m.to};
-    if (lengths) s.length[threadIdx.x] = length_of(a, m.from);
-  }
-  __syncthreads();
-  return m;
-}
-
-// A lane takes the same 16 bytes of every slot of a group, a bucket of the tables or four tokens: it reads them all before it writes any, and
-// nobody else touches them, so that the slots change places without room beside them.
-template <int WIDTH>
-__device__ inline void move_table(const ReorderArgs& a, const Moves<WIDTH>& s, int column) {
-  u32x4 x[WIDTH];
+// A lane takes the same 16 bytes of every slot of a group of up to kGroupWidth, of the tables or of the tokens: it reads them all before it writes any,
+// and nobody else touches them, so that the slots change places without room beside them.  The moves come from the wave's lanes, as scalars.
+constexpr int kGroupWidth = 8;
+__device__ inline void move_table(const ReorderArgs& a, const Move& m, int column) {
+  const int to = m.to == m.from ? -1 : m.to;
+  StateLine x[kGroupWidth];
 #pragma unroll
-  for (int k = 0; k < WIDTH; ++k) {
-    if (k >= a.width || s.move[k].to < 0) continue;
+  for (int k = 0; k < kGroupWidth; ++k) {
+    const int from = __builtin_amdgcn_readlane(m.from, k);
+    if (__builtin_amdgcn_readlane(to, k) < 0) continue;
     const uint32_t empty = column < kTableSlots ? kTableEmpty : 0u;
-    x[k] = u32x4{empty, empty, empty, empty};
-    if (s.move[k].from >= 0) x[k] = *reinterpret_cast<const u32x4*>(a.table + (long long)s.move[k].from * (2 * kTableSlots) + column);
+    x[k] = StateLine{{empty, empty, empty, empty}};
+    if (from >= 0) x[k] = *reinterpret_cast<const StateLine*>(a.table + (long long)from * (2 * kTableSlots) + column);
   }
 #pragma unroll
-  for (int k = 0; k < WIDTH; ++k) {
-    if (k >= a.width || s.move[k].to < 0) continue;
-    *reinterpret_cast<u32x4*>(a.table + (long long)s.move[k].to * (2 * kTableSlots) + column) = x[k];
+  for (int k = 0; k < kGroupWidth; ++k) {
+    const int slot = __builtin_amdgcn_readlane(to, k);
+    if (slot >= 0) *reinterpret_cast<StateLine*>(a.table + (long long)slot * (2 * kTableSlots) + column) = x[k];
   }
 }
-template <int WIDTH>
-__device__ inline void move_tokens(const ReorderArgs& a, const Moves<WIDTH>& s, int column) {
-  StateLine x[WIDTH];
+__device__ inline void move_tokens(const ReorderArgs& a, const Move& m, int column) {
+  const int to = m.to == m.from ? -1 : m.to;
+  StateLine x[kGroupWidth];
 #pragma unroll
-  for (int k = 0; k < WIDTH; ++k) {
-    if (k >= a.width || s.move[k].to < 0 || column >= s.length[k]) continue;
-    x[k] = *reinterpret_cast<const StateLine*>(a.tokens + (long long)s.move[k].from * a.L_max + column);
+  for (int k = 0; k < kGroupWidth; ++k) {
+    const int from = __builtin_amdgcn_readlane(m.from, k), length = __builtin_amdgcn_readlane(m.length, k);
+    if (__builtin_amdgcn_readlane(to, k) < 0 || column >= length) continue;
+    x[k] = *reinterpret_cast<const StateLine*>(a.tokens + (long long)from * a.L_max + column);
   }
 #pragma unroll
-  for (int k = 0; k < WIDTH; ++k) {
-    if (k >= a.width || s.move[k].to < 0 || column >= s.length[k]) continue;
-    int* out = a.tokens + (long long)s.move[k].to * a.L_max + column;
-    if (column + 4 <= s.length[k]) *reinterpret_cast<StateLine*>(out) = x[k];
+  for (int k = 0; k < kGroupWidth; ++k) {
+    const int slot = __builtin_amdgcn_readlane(to, k), length = __builtin_amdgcn_readlane(m.length, k);
+    if (slot < 0 || column >= length) continue;
+    int* out = a.tokens + (long long)slot * a.L_max + column;
+    if (column + 4 <= length) *reinterpret_cast<StateLine*>(out) = x[k];
     else
       for (int j = 0; j < 3; ++j)
-        if (column + j < s.length[k]) out[j] = (int)x[k].w[j];
+        if (column + j < length) out[j] = (int)x[k].w[j];
   }
 }
-// Row threadIdx.x's length and number of distinct tokens (`n`, `nd` as its parent had them), and its new token, once the copies are there.
+// A row's length and number of distinct tokens (`n`, `nd` as its parent had them), and its new token, once the copies are there.
 __device__ inline void append_token(const ReorderArgs& a, int to, int n, int nd, int token) {
   if (token >= 0) {
     if (n < a.L_max) {
@@ -790,52 +780,81 @@ __device__ inline void append_token(const ReorderArgs& a, int to, int n, int nd,
   a.len[to] = n;
   a.ndist[to] = nd;
 }
-struct Appended { int n, nd, token; };
+struct Appended { int nd, token; };
 __device__ inline Appended appended_of(const ReorderArgs& a, int group, const Move& m) {
-  Appended x = {0, 0, -1};
+  Appended x = {0, -1};
   if ((int)threadIdx.x >= a.width || m.to < 0) return x;
-  if (m.from >= 0) {
-    x.n = length_of(a, m.from);
-    x.nd = a.ndist[m.from];
-  }
+  if (m.from >= 0) x.nd = a.ndist[m.from];
   if (a.new_tokens) x.token = a.new_tokens[group * a.width + threadIdx.x];
   return x;
 }
 
 // A workgroup a group, and all in one launch.  (sip_search.h has the figures of both ways.)
-constexpr int kGroupThreads = 1024, kGroupWidth = 8;
-static_assert(kGroupThreads * 4 == kTableSlots, "a bucket a thread");
+constexpr int kGroupThreads = 1024;
+static_assert(kGroupThreads * 4 == kTableSlots, "four entries of a table a thread");
 __global__ __launch_bounds__(kGroupThreads) void state_reorder_group_kernel(ReorderArgs a) {
-  __shared__ Moves<kGroupWidth> s;
   const int t = threadIdx.x;
-  const Move m = find_moves(a, blockIdx.x, s, true);
+  const Move m = move_of(a, blockIdx.x, true);
   const Appended x = appended_of(a, blockIdx.x, m);
-  move_table(a, s, t * 4);
-  move_table(a, s, kTableSlots + t * 4);
-  for (int column = t * 4; column < a.L_max; column += kGroupThreads * 4) move_tokens(a, s, column);
+  move_table(a, m, t * 4);
+  move_table(a, m, kTableSlots + t * 4);
+  for (int column = t * 4; column < a.L_max; column += kGroupThreads * 4) move_tokens(a, m, column);
   __syncthreads();                                       // (everybody has read, and written)
-  if (t < a.width && m.to >= 0) append_token(a, m.to, x.n, x.nd, x.token);
+  if (t < a.width && m.to >= 0) append_token(a, m.to, m.length, x.nd, x.token);
 }
 
-// Wide groups and long rows: 4 KB of a group's slots a workgroup ...  64 groups of 8 slots with 3000 tokens each: 9 to 13 us for 33 MB read and
-// written, latency: slots, then lengths, then the loads, then the stores.
-template <int WIDTH>
-__global__ __launch_bounds__(kReorderThreads) void state_reorder_kernel(ReorderArgs a) {
-  __shared__ Moves<WIDTH> s;
-  const int g = blockIdx.x, block = blockIdx.y, t = threadIdx.x;
-  const bool table = block >= a.token_blocks;
-  find_moves(a, g, s, !table);
-  if (table) move_table(a, s, ((block - a.token_blocks) * kReorderThreads + t) * 4);
-  else move_tokens(a, s, (block * kReorderThreads + t) * 4);
+// The same in many workgroups, 4 KB of a group's slots each, without the new tokens.  Latency: slots, then lengths, then the loads, then the stores.  64
+// groups of 8 slots with 3000 tokens each: 9.2 us for 33 MB read and written.
+constexpr int kReorderThreads = 256, kReorderTables = 2 * kTableSlots / (kReorderThreads * 4);
+__global__ __launch_bounds__(kReorderThreads) void state_reorder_few_kernel(ReorderArgs a) {
+  const int block = blockIdx.y - kReorderTables;         // (below 0: of the tables)
+  const Move m = move_of(a, blockIdx.x, block >= 0);
+  const int column = ((block < 0 ? blockIdx.y : block) * kReorderThreads + threadIdx.x) * 4;
+  if (block < 0) move_table(a, m, column);
+  else move_tokens(a, m, column);
 }
-// ... and behind the copies one wave a group for the rest: lengths and numbers of distinct tokens, all read before any is written, and
+
+// Wider groups: a workgroup takes 1 KB of a group's slots, a wave that of kReorderEach of them, and all are read before any is written.  2 groups
+// of 64 slots 6.6 us; 20 with all slots in every lane's registers: the instructions of so many are what costs.  64 groups of 8 11 us.
+constexpr int kReorderEach = 4, kReorderWords = 64 * 4;
+constexpr int kReorderTableBlocks = 2 * kTableSlots / kReorderWords;
+__global__ __launch_bounds__(SIP_MAX_BEAMS / kReorderEach * 64) void state_reorder_kernel(ReorderArgs a) {
+  const int w = threadIdx.x >> 6, lane = threadIdx.x & 63, block = blockIdx.y - kReorderTableBlocks;       // (below 0: of the tables)
+  const bool table = block < 0;
+  const Move m = move_of(a, blockIdx.x, !table);
+  const int column = (table ? blockIdx.y : block) * kReorderWords + lane * 4;
+  uint32_t* rows = table ? a.table : reinterpret_cast<uint32_t*>(a.tokens);
+  const long long pitch = table ? 2 * kTableSlots : a.L_max;
+  const uint32_t empty = column < kTableSlots ? kTableEmpty : 0u;
+  StateLine x[kReorderEach];
+  int to[kReorderEach], left[kReorderEach];              // words from mine on that move
+#pragma unroll
+  for (int j = 0; j < kReorderEach; ++j) {
+    const int k = w * kReorderEach + j, from = __builtin_amdgcn_readlane(m.from, k);
+    to[j] = __builtin_amdgcn_readlane(m.to, k);
+    left[j] = to[j] < 0 || to[j] == from ? 0 : table ? 4 : __builtin_amdgcn_readlane(m.length, k) - column;
+    x[j] = StateLine{{empty, empty, empty, empty}};
+    if (left[j] > 0 && from >= 0) x[j] = *reinterpret_cast<const StateLine*>(rows + from * pitch + column);
+  }
+#pragma unroll
+  for (int j = 0; j < kReorderEach; ++j) asm volatile("" : "+v"(x[j].w[0]), "+v"(x[j].w[1]), "+v"(x[j].w[2]), "+v"(x[j].w[3]) :: "memory");      // (they are here)
+  __syncthreads();
+#pragma unroll
+  for (int j = 0; j < kReorderEach; ++j) {
+    uint32_t* out = rows + to[j] * pitch + column;
+    if (left[j] >= 4) *reinterpret_cast<StateLine*>(out) = x[j];
+    else
+      for (int i = 0; i < 3; ++i)
+        if (i < left[j]) out[i] = x[j].w[i];
+  }
+}
+// And behind either one wave a group for the rest: lengths and numbers of distinct tokens, all read before any is written, and
 // the new tokens.
 __global__ __launch_bounds__(64) void state_reorder_append_kernel(ReorderArgs a) {
-  __shared__ int slot[64];
-  const Move m = move_of(a, blockIdx.x, slot);
+  const Move m = move_of(a, blockIdx.x, true);
   const Appended x = appended_of(a, blockIdx.x, m);
   __syncthreads();
-  if (m.to >= 0) append_token(a, m.to, x.n, x.nd, x.token);
+  if (m.to >= 0) append_token(a, m.to, m.length, x.nd, x.token);
 }
 
 }  // namespace sip

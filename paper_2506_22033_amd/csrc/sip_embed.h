@@ -499,14 +499,15 @@ __global__ __launch_bounds__(kSortThreads) void embed_small_kernel(EmbedGradArgs
   embed_store(a, to, sum, ADD ? &old : nullptr);
 }
 
-// The tokens that begin in a piece and go on behind its right border: 64 lanes of eight columns, of which each has sixteen workers
-// that take every sixteenth of the token's pieces.  A workgroup looks at kJoinPieces of them.  Latency, 2 us where there is nothing to join
-// and 8.5 for the 18 most frequent tokens of 8192.
-constexpr int kJoinPieces = 4;
+// The tokens that begin in a piece and go on behind its right border.  A workgroup looks at kJoinPieces of them, kJoinLanes lanes of eight
+// columns, of which each has kJoinWorkers workers that take every sixteenth of the token's pieces: one that is a fifth of all tokens has a thousand.
+// Latency, 4 us where there is nothing to join, 8 for the 18 most frequent tokens of 8192, and 24 where 50000 tokens of 568 columns are drawn with
+// 1 / rank^1.2 (64 lanes, 1024 threads: 8.5 and 54; 8 lanes: 13 and 26).
+constexpr int kJoinPieces = 4, kJoinThreads = 256, kJoinLanes = 16, kJoinWorkers = kJoinThreads / kJoinLanes;
 template <bool ADD>
-__global__ __launch_bounds__(1024) void embed_join_kernel(EmbedGradArgs a) {
-  __shared__ f32x8 sums[kSortWaves][64];
-  const int n = *a.live, worker = threadIdx.x >> 6, lane = threadIdx.x & 63, c = (blockIdx.y * 64 + lane) * 8, piece0 = blockIdx.x * kJoinPieces;
+__global__ __launch_bounds__(kJoinThreads) void embed_join_kernel(EmbedGradArgs a) {
+  __shared__ f32x8 sums[kJoinThreads / 64][kJoinLanes];
+  const int t = threadIdx.x, lane = t & 63, n = *a.live, worker = t / kJoinLanes, c = (blockIdx.y * kJoinLanes + t % kJoinLanes) * 8, piece0 = blockIdx.x * kJoinPieces;
   uint32_t token = 0;                                    // lane j: that of piece0 + j
   bool cut = false;
   if (lane < kJoinPieces && piece0 + lane + 1 < a.pieces) {
@@ -519,27 +520,46 @@ __global__ __launch_bounds__(1024) void embed_join_kernel(EmbedGradArgs a) {
   for (unsigned long long left = __ballot(cut); left; left &= left - 1) {
     const int j0 = __builtin_ctzll(left), piece = piece0 + j0;
     const uint32_t v = __builtin_amdgcn_readlane(token, j0);
-    int pieces = 1;                                      // behind this one, that begin with the token: 64 at a time
-    while (true) {
-      const long long at = (long long)(piece + pieces + 1 + lane) * a.piece;
-      const unsigned long long same = __ballot(at < n && a.key[min(at, (long long)n - 1)] == v);
-      pieces += __builtin_ctzll(~same | 1ull << 63);
-      if (~same) break;
-      ++pieces;                                          // (all 64: the count stopped at 63)
+    // Pieces behind this one that begin with the token: 64 at a time by every one, 4096 by every 64th.
+    int pieces = 1;
+    auto same = [&](int step) {
+      const long long at = (long long)(piece + pieces + (lane + 1) * step) * a.piece;
+      return __ballot(at < n && a.key[min(at, (long long)n - 1)] == v);
+    };
+    auto count = [](unsigned long long same) { return ~same ? __builtin_ctzll(~same) : 64; };
+    unsigned long long next = same(1), far = same(64);
+    if (!~next) {
+      while (far) {
+        const int more = count(far);
+        pieces += more * 64;
+        if (more < 64) break;
+        far = same(64);
+      }
+      next = same(1);
     }
+    pieces += count(next);
     f32x8 sum = {0, 0, 0, 0, 0, 0, 0, 0};
     Eight old = {};
     if (c < a.D) {
       if (ADD && worker == 0) old = load_eight(a.out, v * a.out_stride + c, a.out_bf16);
-#pragma unroll 4
-      for (int j = worker; j <= pieces; j += kSortWaves)
+#pragma unroll 8
+      for (int j = worker; j <= pieces; j += kJoinWorkers)
         sum += as_floats(load_eight(a.part, ((long long)(piece + j) * 2 + (j == 0)) * a.D + c, false), false);
     }
+    for (int d = kJoinLanes; d < 64; d <<= 1) {
+      f32x8 other;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float x = sum[e];
+        other[e] = __shfl_xor(x, d);
+      }
+      sum += other;
+    }
     __syncthreads();
-    sums[worker][lane] = sum;
+    if (lane < kJoinLanes) sums[t >> 6][lane] = sum;
     __syncthreads();
-    if (worker > 0 || c >= a.D) continue;
-    for (int j = 1; j < min(kSortWaves, pieces + 1); ++j) sum += sums[j][lane];
+    if (t >= kJoinLanes || c >= a.D) continue;
+    for (int j = 1; j < kJoinThreads / 64; ++j) sum += sums[j][lane];
     embed_store(a, v * a.out_stride + c, sum, ADD ? &old : nullptr);
   }
 }

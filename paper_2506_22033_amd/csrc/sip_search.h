@@ -15,7 +15,7 @@ static_assert(SIP_MAX_V <= 64 * sip::kBeamThreads * sip::kBeamLoads * 4, "the me
 size_t beam_part_bytes(int64_t lists) { return head_align((size_t)lists * sizeof(sip::BeamPart)); }
 
 // Up to so many words a group's slots are moved by one workgroup, in one launch instead of two.  Kernels in us, one and two: a group of 4 beams,
-// L_max = 512, 5.8 and 3.4 + 2.6; 128 groups of 4, 2048, 9.5 and 6.5 + 3.6; but 64 of 8, 4096, 14.8 and 9.1 + 3.8, one of 16, 4096, 20 and 7.8 + 3.0.
+// L_max = 512, 5.3 and 3.4 + 2.6; 128 groups of 4, 2048, 9.5 and 6.5 + 3.6; but 64 of 8, 4096, 14.8 and 9.4 + 4.0.
 constexpr long long kGroupWords = 48 << 10;
 static_assert(kGroupWords < (sip::kGroupWidth + 1) * 2 * sip::kTableSlots, "no wider groups");
 
@@ -71,16 +71,19 @@ sip_status sip_state_reorder(void* state, size_t state_bytes, int32_t slots, int
   a.head = v.head; a.len = v.len; a.ndist = v.ndist; a.tokens = v.tokens; a.table = v.table;
   a.slots = slots; a.L_max = L_max; a.width = width;
   a.slot_of_row = slot_of_row; a.parents = parents; a.new_tokens = tokens;
-  a.token_blocks = tiles(L_max, sip::kReorderThreads * 4);
   hipStream_t stream = static_cast<hipStream_t>(hip_stream);
   if ((long long)width * (L_max + 2 * sip::kTableSlots) <= kGroupWords) {
     hipLaunchKernelGGL(sip::state_reorder_group_kernel, dim3(groups), dim3(sip::kGroupThreads), 0, stream, a);
     return launched();
   }
-  const dim3 grid(groups, a.token_blocks + 8), threads(sip::kReorderThreads);             // (of all along x, more than a launch can have)
-  if (width <= 8) hipLaunchKernelGGL(sip::state_reorder_kernel<8>, grid, threads, 0, stream, a);
-  else if (width <= 32) hipLaunchKernelGGL(sip::state_reorder_kernel<32>, grid, threads, 0, stream, a);
-  else hipLaunchKernelGGL(sip::state_reorder_kernel<64>, grid, threads, 0, stream, a);
+  // (groups along x: of both along it, more than a launch can have)
+  if (width <= sip::kGroupWidth) {
+    const dim3 grid(groups, sip::kReorderTables + tiles(L_max, sip::kReorderThreads * 4));
+    hipLaunchKernelGGL(sip::state_reorder_few_kernel, grid, dim3(sip::kReorderThreads), 0, stream, a);
+  } else {
+    const dim3 grid(groups, sip::kReorderTableBlocks + tiles(L_max, sip::kReorderWords));
+    hipLaunchKernelGGL(sip::state_reorder_kernel, grid, dim3(tiles(width, sip::kReorderEach) * 64), 0, stream, a);
+  }
   hipLaunchKernelGGL(sip::state_reorder_append_kernel, dim3(groups), dim3(64), 0, stream, a);
   return launched();
 }

@@ -189,12 +189,12 @@ sip_status sip_embed_backward(const void* grad_out, int64_t grad_out_stride, sip
   if (N <= 8192) hipLaunchKernelGGL(sip::embed_sort_kernel<8192>, sort_grid, dim3(sip::kSortThreads), 0, stream, a);
   else hipLaunchKernelGGL(sip::embed_sort_kernel<16384>, sort_grid, dim3(sip::kSortThreads), 0, stream, a);
   if (N > 0) {
-    const dim3 sum_grid(tiles((long long)pl.pieces * (D / 8), 256)), join_grid(tiles(pl.pieces, sip::kJoinPieces), tiles(D, 512));
+    const dim3 sum_grid(tiles((long long)pl.pieces * (D / 8), 256)), join_grid(tiles(pl.pieces, sip::kJoinPieces), tiles(D, sip::kJoinLanes * 8));
     auto launch = [&](auto in_add) {
       constexpr bool kAdd = decltype(in_add)::value;
       if (grad_out_dtype == SIP_BF16) hipLaunchKernelGGL((sip::embed_sum_kernel<true, kAdd>), sum_grid, dim3(256), 0, stream, a);
       else hipLaunchKernelGGL((sip::embed_sum_kernel<false, kAdd>), sum_grid, dim3(256), 0, stream, a);
-      hipLaunchKernelGGL(sip::embed_join_kernel<kAdd>, join_grid, dim3(1024), 0, stream, a);
+      hipLaunchKernelGGL(sip::embed_join_kernel<kAdd>, join_grid, dim3(sip::kJoinThreads), 0, stream, a);
     };
     if (accumulate) launch(std::true_type{});
     else launch(std::false_type{});
