@@ -31,10 +31,23 @@ struct BeamArgs {
   double scale;                                          // logit_scale
   const float* scores; const uint8_t* finished; const float* rank_scale;
   int end_token;
+  uint32_t wanted, wanted_last;                          // see beam_wanted()
   int* tokens; int* parents; float* out_scores;
   BeamPart* part;                                        // [rows][chunks]
   unsigned long long* cand;                              // [rows][chunks][n] keys in descending order, 0 = none
 };
+
+// How many of a wave's lanes' maxima have to reach the bound that it gives, a byte a wave: n of all, by how many of its lanes have logits among
+// the chunk's `lanes`.  (0: any bound will do.)
+inline uint32_t beam_wanted(int n, int lanes) {
+  uint32_t wanted = 0;
+  for (int w = 0; w < kBeamWaves; ++w) {
+    const int live = lanes > w * 64 ? lanes - w * 64 < 64 ? lanes - w * 64 : 64 : 0;
+    wanted |= (uint32_t)((n * live + lanes - 1) / lanes) << 8 * w;
+  }
+  return wanted;
+}
+static_assert(SIP_MAX_CONTINUATIONS < 256, "a byte");
 
 // Floats as whole numbers that order alike (one zero; -inf is 0x007fffff), and back.
 __device__ inline uint32_t ordered(float z) {
@@ -191,7 +204,7 @@ __device__ __forceinline__ int select_apart(u32x4 (&raw)[kBeamLoads], double* li
 // The chunk stays in registers: its maxima give the bound from which on logits can be among the n best -- n of the 256 lanes' maxima reach it,
 // and few logits more --, its sum follows, and what reaches the bound is ranked in LDS.
 // fp32 is bound by reading: 256 rows of V = 152064, a tenth of them finished, n = 8 28.8 us, 4.9 TB/s.  bf16 by vector instructions: 224 rows of
-// 151643 20 us for n = 1 (floor 13), 26 for n = 64, of which they are busy for 17.5: unpacking, an exponential's four passes, the ranks.
+// 151643 20 us for n = 1 (floor 13), 27 for n = 64, of which they are busy for 17.5: unpacking, an exponential's four passes, the ranks.
 template <bool BF16>
 __global__ __launch_bounds__(kBeamThreads) void beam_chunk_kernel(BeamArgs a) {
   constexpr int kGroup = BF16 ? 8 : 4, kEach = kBeamLoads * kGroup;      // logits of a 16-byte load, of a lane
@@ -259,12 +272,11 @@ __global__ __launch_bounds__(kBeamThreads) void beam_chunk_kernel(BeamArgs a) {
     }
     m = i ? fmaxf(m, best[i]) : best[i];
   }
-  // The wave's n/4-th largest maximum of a lane, by its leading bits: of four waves, the smallest is at most the n-th largest logit.
+  // The wave's n/4-th largest maximum of a lane (beam_wanted() in a short chunk), by its leading bits: of four waves, the smallest is at most the n-th
+  // largest logit.
   const uint32_t lane_max = ordered(m);
   uint32_t least_of_wave = 0;
-  int wanted = (a.n + kBeamWaves - 1) / kBeamWaves;
-  const int lanes = (a.V - chunk * a.chunk + kGroup - 1) / kGroup, live = min(max(lanes - w * 64, 0), 64);
-  if (lanes < kBeamThreads) wanted = (a.n * live + lanes - 1) / lanes;  // (a short chunk: of each wave by the lanes that have logits)
+  const int wanted = (chunk == a.chunks - 1 ? a.wanted_last : a.wanted) >> 8 * w & 255;
   for (int bit = 31; bit >= 16; --bit) {
     const uint32_t up = least_of_wave | 1u << bit;
     if (__popcll(__ballot(lane_max >= up)) >= wanted) least_of_wave = up;
@@ -272,7 +284,7 @@ __global__ __launch_bounds__(kBeamThreads) void beam_chunk_kernel(BeamArgs a) {
   const uint32_t largest = dpp_scan_max_u32(lane_max);
   if (lane == 63) {
     wave_max[w] = unordered(largest);
-    wave_least[w] = live > 0 ? least_of_wave : 0xffffffffu;
+    wave_least[w] = least_of_wave;
   }
   if (t == 0) count = 0;
   __syncthreads();
@@ -432,14 +444,19 @@ __device__ inline uint32_t nth_largest(const uint32_t (&x)[EACH], int n, int eno
   return from;
 }
 
-// The same bound from the lists' heads alone, one a thread, compared with one another (their last bits make them differ), four a read: 16
+// Where n of a group's entries can be told by one of each list alone: if n / d lists have d entries from a bound on, n entries reach it.  Of so many
+// lists a quarter decides; where there are few, by entries further down.
+__device__ inline int beam_depth(int lists, int n) { return min(n, max(1, (4 * n + lists - 1) / lists)); }
+
+// The same bound from one entry of each list, one a thread, compared with one another (their last bits make them differ), four a read: 16
 // waves' reads of LDS are what it costs.  0 if there are fewer than n.
 constexpr int kHeadsMost = 256;
-template <int THREADS>
-__device__ inline uint32_t nth_head(uint32_t lead, int lists, int n, uint32_t (&heads)[kHeadsMost], int (&ranks)[THREADS], uint32_t& bound) {
-  constexpr uint32_t kLast = kHeadsMost - 1;
+template <int THREADS, int MOST>
+__device__ inline uint32_t nth_head(uint32_t lead, int lists, int n, uint32_t (&heads)[MOST], int (&ranks)[THREADS], uint32_t& bound) {
+  static_assert(MOST <= THREADS, "a thread a head");
+  constexpr uint32_t kLast = MOST - 1;
   const int t = threadIdx.x;
-  if (t < kHeadsMost) heads[t] = t < lists ? (lead & ~kLast) | (kLast - t) : 0;
+  if (t < MOST) heads[t] = t < lists ? (lead & ~kLast) | (kLast - t) : 0;
   ranks[t] = 0;
   if (t == 0) bound = 0;
   __syncthreads();
@@ -589,13 +606,14 @@ __global__ __launch_bounds__(256) void beam_merge_few_kernel(BeamArgs a) {
   const int lists = a.width * a.chunks;
   uint32_t from = 0;
   if (entries <= 64) from = 0;                           // (so few are compared with one another at once)
-  else if (lists >= a.n && lists <= kHeadsMost) {
-    // entry 0 of list t is entry t * n of all
+  else if (lists <= kHeadsMost) {
+    // entry d - 1 of list t is entry t * n + d - 1 of all
+    const int depth = beam_depth(lists, a.n);
 #pragma unroll
     for (int i = 0; i < kEach; ++i)
-      if (t + i * 256 < entries && (t + i * 256) % a.n == 0) first[(t + i * 256) / a.n] = lead[i];
+      if (t + i * 256 < entries && (t + i * 256) % a.n == depth - 1) first[(t + i * 256) / a.n] = lead[i];
     __syncthreads();
-    from = nth_head<256>(t < lists ? first[t] : 0, lists, a.n, heads, ranks, bound);
+    from = nth_head<256, kHeadsMost>(t < lists ? first[t] : 0, lists, (a.n + depth - 1) / depth, heads, ranks, bound);
   } else {
     int reach = entries;
     from = nth_largest(lead, a.n, max(a.n, 64), reach, votes);
@@ -611,9 +629,9 @@ __global__ __launch_bounds__(256) void beam_merge_few_kernel(BeamArgs a) {
   store_missing(a, kept);
 }
 
-// Any group.  The lists are in order, so the n-th best of their heads bounds what can be selected, and a list whose head is the
-// r-th best can give its n - r first entries at most.  7 groups of 32 beams, 320 lists of 64 each: 15.7 us, latency too.
-constexpr int kMergeThreads = 1024, kRankMost = 256;
+// Any group.  The lists are in order, so one entry of each bounds what can be selected, and a list whose head is the r-th best
+// can give its n - r first entries at most.  7 groups of 32 beams, 320 lists of 64 each: 14.8 us, latency too.
+constexpr int kMergeThreads = 1024, kRankMost = 256, kHeadsMany = 512;
 constexpr int kMergeLists = SIP_MAX_BEAMS * 64;
 constexpr int kMergeRoom = SIP_MAX_CONTINUATIONS * (SIP_MAX_CONTINUATIONS + 1) / 2;
 static_assert(kMergeRoom >= kMergeLists, "room for all heads");
@@ -623,14 +641,16 @@ __global__ __launch_bounds__(kMergeThreads) void beam_merge_kernel(BeamArgs a) {
   __shared__ BeamRank found[kMergeRoom];
   __shared__ int ranks[kMergeThreads], chosen[SIP_MAX_CONTINUATIONS], count;
   __shared__ uint32_t bound;
-  __shared__ __align__(16) uint32_t leads[kHeadsMost];
+  __shared__ __align__(16) uint32_t leads[kHeadsMany];
   __shared__ __align__(16) BeamVotes votes;
   const int t = threadIdx.x, S = a.chunks, n = a.n, lists = a.width * S;
   const unsigned long long* cand = a.cand + (long long)blockIdx.x * lists * n;
   static_assert(kHeads == 4, "and as many entries at once");
-  unsigned long long key[kHeads];
+  unsigned long long key[kHeads], deep = 0;
+  const int depth = beam_depth(lists, n);
 #pragma unroll
   for (int i = 0; i < kHeads; ++i) key[i] = t + i * kMergeThreads < lists ? cand[(long long)(t + i * kMergeThreads) * n] : 0;
+  if (t < lists && depth > 1) deep = cand[(long long)t * n + depth - 1];
   if (t == 0) count = 0;
   if (t < kVoteTurns * 4) votes[t / 4][t % 4] = 0;
   load_group<kMergeThreads>(a, rows);
@@ -641,8 +661,15 @@ __global__ __launch_bounds__(kMergeThreads) void beam_merge_kernel(BeamArgs a) {
     const int l = t + i * kMergeThreads;
     lead[i] = l < lists ? (uint32_t)(rank_of(a, rows, l, 0, key[i]).total >> 32) : 0;
   }
-  int reach = lists;
-  const uint32_t from = max(lists < n ? 0 : lists <= kHeadsMost ? nth_head<kMergeThreads>(lead[0], lists, n, leads, ranks, bound) : nth_largest(lead, n, n, reach, votes), 1u);
+  uint32_t from;
+  if (lists <= kHeadsMany) {
+    const uint32_t mine = depth > 1 && t < lists ? (uint32_t)(rank_of(a, rows, t, depth - 1, deep).total >> 32) : lead[0];
+    from = nth_head<kMergeThreads, kHeadsMany>(mine, lists, (n + depth - 1) / depth, leads, ranks, bound);
+  } else {
+    int reach = lists;
+    from = nth_largest(lead, n, n + n / 4, reach, votes);
+  }
+  from = max(from, 1u);
 #pragma unroll
   for (int i = 0; i < kHeads; ++i)
     if (lead[i] >= from) found[atomicAdd(&count, 1)] = rank_of(a, rows, t + i * kMergeThreads, 0, key[i]);

@@ -1,5 +1,7 @@
 // Host side of the entry points declared in include/sip_beam.h: argument checks, workspace carving, launches.
 #pragma once
+#include <algorithm>
+
 #include "../../include/sip_beam.h"
 #include "sip_beam.h"
 #include "sip_host.h"
@@ -44,6 +46,9 @@ sip_status sip_beam_select(const void* logits, int32_t groups, int32_t width, in
   a.width = width; a.V = V; a.n = n;
   a.chunks = beam_chunks(V, dtype == SIP_BF16);
   a.chunk = sip::beam_chunk(dtype == SIP_BF16);
+  const int group = dtype == SIP_BF16 ? 8 : 4;
+  a.wanted = sip::beam_wanted(n, sip::kBeamThreads);
+  a.wanted_last = sip::beam_wanted(n, std::min(tiles(V - (a.chunks - 1) * a.chunk, group), sip::kBeamThreads));
   a.scale = (double)logit_scale;
   a.c = (float)(a.scale * 1.4426950408889634074);
   a.scores = scores; a.finished = finished; a.rank_scale = rank_scale; a.end_token = end_token;
