@@ -204,7 +204,7 @@ __device__ __forceinline__ int select_apart(u32x4 (&raw)[kBeamLoads], double* li
 // The chunk stays in registers: its maxima give the bound from which on logits can be among the n best -- n of the 256 lanes' maxima reach it,
 // and few logits more --, its sum follows, and what reaches the bound is ranked in LDS.
 // fp32 is bound by reading: 256 rows of V = 152064, a tenth of them finished, n = 8 28.8 us, 4.9 TB/s.  bf16 by vector instructions: 224 rows of
-// 151643 20 us for n = 1 (floor 13), 27 for n = 64, of which they are busy for 17.5: unpacking, an exponential's four passes, the ranks.
+// 151643 19 us for n = 1 (floor 13), 24 for n = 64: unpacking, an exponential's four passes, the ranks.
 template <bool BF16>
 __global__ __launch_bounds__(kBeamThreads) void beam_chunk_kernel(BeamArgs a) {
   constexpr int kGroup = BF16 ? 8 : 4, kEach = kBeamLoads * kGroup;      // logits of a 16-byte load, of a lane
@@ -291,14 +291,20 @@ __global__ __launch_bounds__(kBeamThreads) void beam_chunk_kernel(BeamArgs a) {
   m = fmaxf(fmaxf(wave_max[0], wave_max[1]), fmaxf(wave_max[2], wave_max[3]));
   const uint32_t least = min(min(wave_least[0], wave_least[1]), min(wave_least[2], wave_least[3]));
   const float from = least < 0x00800000u ? -3.402823466e38f : unordered(least);          // (-inf is no continuation)
-  // My logits from the bound on go to the list: counted first, so that nothing waits for a place.
-  int mine = 0;
+  // My logits from the bound on go to the list: marked and counted first, so that nothing waits for a place, and read once more then, since there
+  // are few: 64 tests and places of all were a third of this kernel's instructions.
+  uint32_t hits[kEach == 64 ? 2 : 1] = {};               // a load's bits from the last logit's on
 #pragma unroll
   for (int i = 0; i < kBeamLoads; ++i)
     if (best[i] >= from) {
+      uint32_t of_load = 0;
 #pragma unroll
-      for (int j = 0; j < kGroup; ++j) mine += value(i * kGroup + j) >= from;
+      for (int j = 0; j < kGroup; ++j) of_load = of_load + of_load + (value(i * kGroup + j) >= from);
+      hits[i * kGroup / 32] |= of_load << i * kGroup % 32;
     }
+  unsigned long long marked = hits[0];
+  if constexpr (kEach == 64) marked |= (unsigned long long)hits[1] << 32;
+  const int mine = __popcll(marked);
   const int upto = (int)dpp_scan_add_u32((uint32_t)mine);
   int place = 0;
   if (lane == 63) place = atomicAdd(&count, upto);
@@ -323,18 +329,12 @@ __global__ __launch_bounds__(kBeamThreads) void beam_chunk_kernel(BeamArgs a) {
   }
   hide();
   place = __builtin_amdgcn_readlane(place, 63) + upto - mine;
-#pragma unroll
-  for (int i = 0; i < kBeamLoads; ++i)
-    if (best[i] >= from) {
-#pragma unroll
-      for (int j = 0; j < kGroup; ++j) {
-        const int e = i * kGroup + j;
-        if (value(e) >= from) {
-          if (place < kBeamList) list[place] = list_entry(value(e), t * kGroup + beam_place<kGroup>(e));
-          ++place;
-        }
-      }
-    }
+  for (; marked && place < kBeamList; marked &= marked - 1, ++place) {
+    const int b = __builtin_ctzll(marked), i = b / kGroup, j = kGroup - 1 - b % kGroup;
+    const char* at = z0 + i * kBeamThreads * 16 + j * (BF16 ? 2 : 4);
+    const float z = BF16 ? (float)*reinterpret_cast<const __bf16*>(at) : *reinterpret_cast<const float*>(at);
+    list[place] = list_entry(z, (i * kBeamThreads + t) * kGroup + j);
+  }
   const double sum = wave_total(((double)s[0] + (double)s[1]) + ((double)s[2] + (double)s[3]));
   if (lane == 63) wave_sum[w] = sum;
   __syncthreads();
