@@ -204,7 +204,7 @@ __device__ __forceinline__ int select_apart(u32x4 (&raw)[kBeamLoads], double* li
 // The chunk stays in registers: its maxima give the bound from which on logits can be among the n best -- n of the 256 lanes' maxima reach it,
 // and few logits more --, its sum follows, and what reaches the bound is ranked in LDS.
 // fp32 is bound by reading: 256 rows of V = 152064, a tenth of them finished, n = 8 28.8 us, 4.9 TB/s.  bf16 by vector instructions: 224 rows of
-// 151643 19 us for n = 1 (floor 13), 24 for n = 64: unpacking, an exponential's four passes, the ranks.
+// 151643 20 us for n = 1 (floor 13), 24 for n = 64: unpacking, an exponential's four passes, the ranks.
 template <bool BF16>
 __global__ __launch_bounds__(kBeamThreads) void beam_chunk_kernel(BeamArgs a) {
   constexpr int kGroup = BF16 ? 8 : 4, kEach = kBeamLoads * kGroup;      // logits of a 16-byte load, of a lane
@@ -329,6 +329,7 @@ __global__ __launch_bounds__(kBeamThreads) void beam_chunk_kernel(BeamArgs a) {
   }
   hide();
   place = __builtin_amdgcn_readlane(place, 63) + upto - mine;
+  if (__builtin_amdgcn_readlane(upto, 63) > kBeamList) marked = 0;       // (the list will not be used)
   for (; marked && place < kBeamList; marked &= marked - 1, ++place) {
     const int b = __builtin_ctzll(marked), i = b / kGroup, j = kGroup - 1 - b % kGroup;
     const char* at = z0 + i * kBeamThreads * 16 + j * (BF16 ? 2 : 4);
