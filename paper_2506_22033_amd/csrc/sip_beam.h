@@ -203,7 +203,7 @@ __device__ __forceinline__ int select_apart(u32x4 (&raw)[kBeamLoads], double* li
 
 // The chunk stays in registers: its maxima give the bound from which on logits can be among the n best -- n of the 256 lanes' maxima reach it,
 // and few logits more --, its sum follows, and what reaches the bound is ranked in LDS.
-// fp32 is bound by reading: 256 rows of V = 152064, a tenth of them finished, n = 8 28.8 us, 4.9 TB/s.  bf16 by vector instructions: 224 rows of
+// fp32 is bound by reading: 256 rows of V = 152064, a tenth of them finished, n = 8 28.2 us, 5 TB/s.  bf16 by vector instructions: 224 rows of
 // 151643 20 us for n = 1 (floor 13), 24 for n = 64: unpacking, an exponential's four passes, the ranks.
 template <bool BF16>
 __global__ __launch_bounds__(kBeamThreads) void beam_chunk_kernel(BeamArgs a) {
