@@ -228,7 +228,7 @@ __device__ inline Bucket list_bucket(const EmbedGradArgs& a, int bucket, BucketS
   const int t = threadIdx.x, lane = t & 63, w = t >> 6;
   // A wave's run of ids, four neighbours a lane, kQuads loads under way at once.
   constexpr int kQuads = 4;
-  const int run = (a.N + kSortThreads * 4 - 1) / (kSortThreads * 4) * 256, first = w * run, last = min(a.N, first + run);
+  const int run = (a.N + kSortThreads * 4 - 1) / (kSortThreads * 4) * 256, first = __builtin_amdgcn_readfirstlane(w) * run, last = min(a.N, first + run);
   Bucket b;
   b.low = (uint32_t)bucket << a.shift;
   b.size = min((uint32_t)a.V - b.low, 1u << a.shift);
@@ -249,10 +249,12 @@ __device__ inline Bucket list_bucket(const EmbedGradArgs& a, int bucket, BucketS
     load(i0);
 #pragma unroll
     for (int j = 0; j < kQuads; ++j)
+      if (i0 + j * 256 < last) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        n += __popcll(__ballot(id[j].x[e] - b.low < b.size));
-        before += __popcll(__ballot(id[j].x[e] < b.low));
+        for (int e = 0; e < 4; ++e) {
+          n += __popcll(__ballot(id[j].x[e] - b.low < b.size));
+          before += __popcll(__ballot(id[j].x[e] < b.low));
+        }
       }
   }
   if (lane == 0) { s.wave_total[w] = n; s.wave_before[w] = before; }
@@ -271,6 +273,7 @@ __device__ inline Bucket list_bucket(const EmbedGradArgs& a, int bucket, BucketS
     if (run > kQuads * 256) load(i0);
 #pragma unroll
     for (int j = 0; j < kQuads; ++j) {
+      if (i0 + j * 256 >= last) continue;
       unsigned long long mine[4];
 #pragma unroll
       for (int e = 0; e < 4; ++e) mine[e] = __ballot(id[j].x[e] - b.low < b.size);
