@@ -419,25 +419,49 @@ __device__ inline BeamRank rank_of(const BeamArgs& a, const BeamGroup& rows, int
   return {0, 0};
 }
 
-// The leading bits of the n-th largest of the workgroup's values, EACH a lane: two bits a turn, of which votes[turn] counts the values
-// that reach the three possibilities (zeros before; a barrier a turn).  `reach` says how many reach it, before: of how many; no more than `enough` end
-// the search.  0 if there are fewer than n.
+// The leading bits of the n-th largest of the workgroup's values, EACH a lane: two bits a turn from the first one on in which any two of them
+// differ, of which votes.at[turn] counts the values that reach the three possibilities (zeros before; a barrier a turn).  `reach` says how many
+// reach it, before: of how many; no more than `enough` end the search.  0 is no value, unless ZEROS.
 constexpr int kVoteTurns = 16;
-typedef int BeamVotes[kVoteTurns][4];
+struct __align__(16) BeamVotes { int at[kVoteTurns][4]; uint32_t high, low; };       // low: its complement
+__device__ inline void clear(BeamVotes& votes) {
+  const int t = threadIdx.x;
+  if (t < kVoteTurns * 4) votes.at[t / 4][t % 4] = 0;
+  if (t == 0) votes.high = votes.low = 0;
+}
 template <int EACH>
-__device__ inline uint32_t nth_largest(const uint32_t (&x)[EACH], int n, int enough, int& reach, BeamVotes& votes) {
+__device__ inline uint32_t nth_largest(const uint32_t (&x)[EACH], int n, int enough, int& reach, BeamVotes& votes, bool zeros) {
   const int lane = threadIdx.x & 63;
   uint32_t from = 0;
-  for (int turn = 0; turn < kVoteTurns && reach > enough; ++turn) {
-    const int bit = 30 - 2 * turn;
+  int bit = 30;
+  if (!zeros) {
+    uint32_t high = 0, low = 0;
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+      high = max(high, x[i]);
+      low = max(low, x[i] ? ~x[i] : 0);
+    }
+    high = dpp_scan_max_u32(high);
+    low = dpp_scan_max_u32(low);
+    if (lane == 63 && high) {
+      atomicMax(&votes.high, high);
+      atomicMax(&votes.low, low);
+    }
+    __syncthreads();
+    const uint32_t least = ~votes.low, differ = votes.high ^ least;
+    if (votes.high == 0) return 0;
+    bit = differ ? 31 - __builtin_clz(differ) & ~1 : -2;
+    from = differ ? least & ~((4u << bit) - 1) : least;
+  }
+  for (int turn = 0; bit >= 0 && reach > enough; ++turn, bit -= 2) {
     int mine[3] = {0, 0, 0};
 #pragma unroll
     for (int i = 0; i < EACH; ++i)
 #pragma unroll
       for (int j = 0; j < 3; ++j) mine[j] += __popcll(__ballot(x[i] >= (from | (uint32_t)(j + 1) << bit)));
-    if (lane < 3 && mine[0]) atomicAdd(&votes[turn][lane], lane == 0 ? mine[0] : lane == 1 ? mine[1] : mine[2]);
+    if (lane < 3 && mine[0]) atomicAdd(&votes.at[turn][lane], lane == 0 ? mine[0] : lane == 1 ? mine[1] : mine[2]);
     __syncthreads();
-    const int4 all = *reinterpret_cast<const int4*>(votes[turn]);
+    const int4 all = *reinterpret_cast<const int4*>(votes.at[turn]);
     const int step = (all.x >= n) + (all.y >= n) + (all.z >= n);
     from |= (uint32_t)step << bit;
     if (step) reach = step == 1 ? all.x : step == 2 ? all.y : all.z;
@@ -499,10 +523,10 @@ __device__ inline int keep_largest(BeamRank* found, int m, int n, int enough, Be
     uint32_t word[kEach];
 #pragma unroll
     for (int i = 0; i < kEach; ++i) word[i] = open[i] ? (uint32_t)((w < 2 ? x[i].total : x[i].rest) >> (w & 1 ? 0 : 32)) : 0;
-    if (t < kVoteTurns * 4) votes[t / 4][t % 4] = 0;
+    clear(votes);
     if (t == 0) count = 0;
     __syncthreads();
-    const uint32_t from = nth_largest(word, n - above, enough - above, reach, votes);
+    const uint32_t from = nth_largest(word, n - above, enough - above, reach, votes, w > 0);
     const bool last = above + reach <= enough;           // (else `from` is the n-th largest word, all of it)
     int mine = 0;
 #pragma unroll
@@ -585,14 +609,14 @@ __global__ __launch_bounds__(256) void beam_merge_few_kernel(BeamArgs a) {
   __shared__ int ranks[256], count;
   __shared__ uint32_t first[kHeadsMost], bound;
   __shared__ __align__(16) uint32_t heads[kHeadsMost];
-  __shared__ __align__(16) BeamVotes votes;
+  __shared__ BeamVotes votes;
   const int t = threadIdx.x, entries = a.width * a.chunks * a.n;
   const unsigned long long* cand = a.cand + (long long)blockIdx.x * entries;
   unsigned long long key[kEach];
 #pragma unroll
   for (int i = 0; i < kEach; ++i) key[i] = t + i * 256 < entries ? cand[t + i * 256] : 0;
   if (t == 0) count = 0;
-  if (t < kVoteTurns * 4) votes[t / 4][t % 4] = 0;
+  clear(votes);
   load_group<256>(a, rows);
   __syncthreads();
   BeamRank x[kEach];
@@ -617,7 +641,7 @@ __global__ __launch_bounds__(256) void beam_merge_few_kernel(BeamArgs a) {
     from = nth_head<256, kHeadsMost>(t < lists ? first[t] : 0, lists, (a.n + depth - 1) / depth, heads, ranks, bound);
   } else {
     int reach = entries;
-    from = nth_largest(lead, a.n, max(a.n, 64), reach, votes);
+    from = nth_largest(lead, a.n, max(a.n, 64), reach, votes, false);
   }
   from = max(from, 1u);                                  // (0: there is none)
 #pragma unroll
@@ -643,7 +667,7 @@ __global__ __launch_bounds__(kMergeThreads) void beam_merge_kernel(BeamArgs a) {
   __shared__ int ranks[kMergeThreads], chosen[SIP_MAX_CONTINUATIONS], count;
   __shared__ uint32_t bound;
   __shared__ __align__(16) uint32_t leads[kHeadsMany];
-  __shared__ __align__(16) BeamVotes votes;
+  __shared__ BeamVotes votes;
   const int t = threadIdx.x, S = a.chunks, n = a.n, lists = a.width * S;
   const unsigned long long* cand = a.cand + (long long)blockIdx.x * lists * n;
   static_assert(kHeads == 4, "and as many entries at once");
@@ -653,7 +677,7 @@ __global__ __launch_bounds__(kMergeThreads) void beam_merge_kernel(BeamArgs a) {
   for (int i = 0; i < kHeads; ++i) key[i] = t + i * kMergeThreads < lists ? cand[(long long)(t + i * kMergeThreads) * n] : 0;
   if (t < lists && depth > 1) deep = cand[(long long)t * n + depth - 1];
   if (t == 0) count = 0;
-  if (t < kVoteTurns * 4) votes[t / 4][t % 4] = 0;
+  clear(votes);
   load_group<kMergeThreads>(a, rows);
   __syncthreads();
   uint32_t lead[kHeads];
@@ -668,7 +692,7 @@ __global__ __launch_bounds__(kMergeThreads) void beam_merge_kernel(BeamArgs a) {
     from = nth_head<kMergeThreads, kHeadsMany>(mine, lists, (n + depth - 1) / depth, leads, ranks, bound);
   } else {
     int reach = lists;
-    from = nth_largest(lead, n, n + n / 4, reach, votes);
+    from = nth_largest(lead, n, n + n / 4, reach, votes, false);
   }
   from = max(from, 1u);
 #pragma unroll
