@@ -421,7 +421,7 @@ __device__ inline BeamRank rank_of(const BeamArgs& a, const BeamGroup& rows, int
 
 // The leading bits of the n-th largest of the workgroup's values, EACH a lane: two bits a turn from the first one on in which any two of them
 // differ, of which votes.at[turn] counts the values that reach the three possibilities (zeros before; a barrier a turn).  `reach` says how many
-// reach it, before: of how many; no more than `enough` end the search.  0 is no value, unless ZEROS.
+// reach it, before: of how many; no more than `enough` end the search.  0 is no value, unless `zeros`.
 constexpr int kVoteTurns = 16;
 struct __align__(16) BeamVotes { int at[kVoteTurns][4]; uint32_t high, low; };       // low: its complement
 __device__ inline void clear(BeamVotes& votes) {

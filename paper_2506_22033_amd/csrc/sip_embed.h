@@ -310,7 +310,7 @@ __device__ inline LdsEntries sort_bucket(const EmbedGradArgs& a, LdsEntries from
 // A workgroup a bucket, up to 128 of them, each of which reads all tokens: no counts are exchanged, and none waits for another.  The
 // workgroups behind fill grad_weight with zeros meanwhile, unless it is added to.  ROOM: entries of a bucket that LDS holds, twice; larger buckets
 // are sorted in the workspace.
-// 8192 tokens 10 us, 65536 21, and 41 where one token is an eighth of them: reading, and the largest bucket.  Beside 1.24 GB of zeros
+// 8192 tokens 9.4 us, 65536 21, and 41 where one token is an eighth of them: reading, and the largest bucket.  Beside 1.24 GB of zeros
 // that is hidden: 211 us, 5.9 TB/s.
 template <int ROOM>
 __global__ __launch_bounds__(kSortThreads) void embed_sort_kernel(EmbedGradArgs a) {
@@ -428,7 +428,7 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(EmbedGradArgs a) {
 
 // A small gradient in one launch: a workgroup a bucket, which sums its tokens' rows itself and clears the bucket's others.  The sorted
 // entries go to groups of waves that cover a row each, a run of entries a group; what crosses the end of a run goes through LDS.
-// 384 tokens, 4096 x 512 fp32: 8.9 us instead of the three kernels' 16.
+// 384 tokens, 4096 x 512 fp32: 8.4 us instead of the three kernels' 16.
 constexpr int kSmallTokens = 1024, kSmallWidth = kSortWaves * 512;
 template <bool BF16, bool ADD>
 __global__ __launch_bounds__(kSortThreads) void embed_small_kernel(EmbedGradArgs a) {
