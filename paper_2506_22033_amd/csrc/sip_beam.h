@@ -421,13 +421,14 @@ __device__ inline BeamRank rank_of(const BeamArgs& a, const BeamGroup& rows, int
 
 // The leading bits of the n-th largest of the workgroup's values, EACH a lane: two bits a turn from the first one on in which any two of them
 // differ, of which votes.at[turn] counts the values that reach the three possibilities (zeros before; a barrier a turn).  `reach` says how many
-// reach it, before: of how many; no more than `enough` end the search.  0 is no value, unless `zeros`.
+// reach it; no more than `enough` end the search.  0 is no value, unless `zeros`: then `reach` is the number of values before.  0 if there are
+// fewer than n.
 constexpr int kVoteTurns = 16;
-struct __align__(16) BeamVotes { int at[kVoteTurns][4]; uint32_t high, low; };       // low: its complement
+struct __align__(16) BeamVotes { int at[kVoteTurns][4]; uint32_t high, low; int some; };       // low: its complement
 __device__ inline void clear(BeamVotes& votes) {
   const int t = threadIdx.x;
   if (t < kVoteTurns * 4) votes.at[t / 4][t % 4] = 0;
-  if (t == 0) votes.high = votes.low = 0;
+  if (t == 0) votes.high = votes.low = votes.some = 0;
 }
 template <int EACH>
 __device__ inline uint32_t nth_largest(const uint32_t (&x)[EACH], int n, int enough, int& reach, BeamVotes& votes, bool zeros) {
@@ -436,20 +437,24 @@ __device__ inline uint32_t nth_largest(const uint32_t (&x)[EACH], int n, int eno
   int bit = 30;
   if (!zeros) {
     uint32_t high = 0, low = 0;
+    int some = 0;
 #pragma unroll
     for (int i = 0; i < EACH; ++i) {
       high = max(high, x[i]);
       low = max(low, x[i] ? ~x[i] : 0);
+      some += __popcll(__ballot(x[i] != 0));
     }
     high = dpp_scan_max_u32(high);
     low = dpp_scan_max_u32(low);
     if (lane == 63 && high) {
       atomicMax(&votes.high, high);
       atomicMax(&votes.low, low);
+      atomicAdd(&votes.some, some);
     }
     __syncthreads();
+    reach = votes.some;
+    if (reach < n) return 0;
     const uint32_t least = ~votes.low, differ = votes.high ^ least;
-    if (votes.high == 0) return 0;
     bit = differ ? 31 - __builtin_clz(differ) & ~1 : -2;
     from = differ ? least & ~((4u << bit) - 1) : least;
   }
@@ -640,7 +645,7 @@ __global__ __launch_bounds__(256) void beam_merge_few_kernel(BeamArgs a) {
     __syncthreads();
     from = nth_head<256, kHeadsMost>(t < lists ? first[t] : 0, lists, (a.n + depth - 1) / depth, heads, ranks, bound);
   } else {
-    int reach = entries;
+    int reach;
     from = nth_largest(lead, a.n, max(a.n, 64), reach, votes, false);
   }
   from = max(from, 1u);                                  // (0: there is none)
@@ -691,7 +696,7 @@ __global__ __launch_bounds__(kMergeThreads) void beam_merge_kernel(BeamArgs a) {
     const uint32_t mine = depth > 1 && t < lists ? (uint32_t)(rank_of(a, rows, t, depth - 1, deep).total >> 32) : lead[0];
     from = nth_head<kMergeThreads, kHeadsMany>(mine, lists, (n + depth - 1) / depth, leads, ranks, bound);
   } else {
-    int reach = lists;
+    int reach;
     from = nth_largest(lead, n, n + n / 4, reach, votes, false);
   }
   from = max(from, 1u);

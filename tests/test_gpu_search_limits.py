@@ -42,6 +42,23 @@ def test_wide_groups_of_few_lists_and_short_chunks(groups, width, V, n, dtype):
     _check(logits, scores, width, n, sip.sip_beam_select(logits, scores, width, n))
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("finished", [False, True])
+@pytest.mark.parametrize("live", [1, 3, 60])
+@pytest.mark.parametrize("width,V,n", [(60, 88820, 120), (64, 150000, 128), (30, 3000, 1), (64, 524288, 2), (30, 170000, 33), (60, 20000, 7)])
+def test_many_lists_of_which_few_hold_anything(width, V, n, live, finished, dtype):
+    # As before the first step of a search, or near its end.
+    logits, g = _rows(width, V, dtype, V + n)
+    scores = -torch.rand(width, generator=g, device=DEV) * 9.0
+    done = None
+    if finished:
+        done = torch.ones(width, dtype=torch.uint8, device=DEV)
+        done[:live] = 0
+    else:
+        scores[live:] = -float("inf")
+    _check(logits, scores, width, n, sip.sip_beam_select(logits, scores, width, n, finished=done, end_token=2), done, end_token=2)
+
+
 @pytest.mark.parametrize("width,V,n", [(64, 9000, 128), (64, 40000, 100), (8, 3000, 16), (64, 100, 3), (1, 50000, 128)])
 def test_equal_rows_of_equal_logits_by_beam_and_token(width, V, n):
     # Every continuation of every beam has the same total: the first beam's lowest tokens, then the next one's.
