@@ -779,43 +779,51 @@ __device__ inline Move move_of(const ReorderArgs& a, int group, bool lengths) {
 struct __attribute__((packed, aligned(4))) StateLine { uint32_t w[4]; };
 
 // A lane takes the same 16 bytes of every slot of a group of up to kGroupWidth, of the tables or of the tokens: it reads them all before it writes any,
-// and nobody else touches them, so that the slots change places without room beside them.  The moves come from the wave's lanes, as scalars.
+// and nobody else touches them, so that the slots change places without room beside them.  The moves come from the wave's lanes, as scalars, and are
+// fetched where all lanes are active (fetch_moves(); fetch_lengths() where these are wanted, since they arrive later): what a lane's register
+// holds that has left a loop is not defined.
 constexpr int kGroupWidth = 8;
-__device__ inline void move_table(const ReorderArgs& a, const Move& m, int column) {
+struct Moves { int from[kGroupWidth], to[kGroupWidth], length[kGroupWidth]; };       // to < 0: nothing moves
+__device__ inline void fetch_moves(Moves& all, const Move& m) {
   const int to = m.to == m.from ? -1 : m.to;
-  StateLine x[kGroupWidth];
 #pragma unroll
   for (int k = 0; k < kGroupWidth; ++k) {
-    const int from = __builtin_amdgcn_readlane(m.from, k);
-    if (__builtin_amdgcn_readlane(to, k) < 0) continue;
-    const uint32_t empty = column < kTableSlots ? kTableEmpty : 0u;
-    x[k] = StateLine{{empty, empty, empty, empty}};
-    if (from >= 0) x[k] = *reinterpret_cast<const StateLine*>(a.table + (long long)from * (2 * kTableSlots) + column);
-  }
-#pragma unroll
-  for (int k = 0; k < kGroupWidth; ++k) {
-    const int slot = __builtin_amdgcn_readlane(to, k);
-    if (slot >= 0) *reinterpret_cast<StateLine*>(a.table + (long long)slot * (2 * kTableSlots) + column) = x[k];
+    all.from[k] = __builtin_amdgcn_readlane(m.from, k);
+    all.to[k] = __builtin_amdgcn_readlane(to, k);
   }
 }
-__device__ inline void move_tokens(const ReorderArgs& a, const Move& m, int column) {
-  const int to = m.to == m.from ? -1 : m.to;
+__device__ inline void fetch_lengths(Moves& all, const Move& m) {
+#pragma unroll
+  for (int k = 0; k < kGroupWidth; ++k) all.length[k] = __builtin_amdgcn_readlane(m.length, k);
+}
+__device__ inline void move_table(const ReorderArgs& a, const Moves& m, int column) {
   StateLine x[kGroupWidth];
 #pragma unroll
   for (int k = 0; k < kGroupWidth; ++k) {
-    const int from = __builtin_amdgcn_readlane(m.from, k), length = __builtin_amdgcn_readlane(m.length, k);
-    if (__builtin_amdgcn_readlane(to, k) < 0 || column >= length) continue;
-    x[k] = *reinterpret_cast<const StateLine*>(a.tokens + (long long)from * a.L_max + column);
+    if (m.to[k] < 0) continue;
+    const uint32_t empty = column < kTableSlots ? kTableEmpty : 0u;
+    x[k] = StateLine{{empty, empty, empty, empty}};
+    if (m.from[k] >= 0) x[k] = *reinterpret_cast<const StateLine*>(a.table + (long long)m.from[k] * (2 * kTableSlots) + column);
+  }
+#pragma unroll
+  for (int k = 0; k < kGroupWidth; ++k)
+    if (m.to[k] >= 0) *reinterpret_cast<StateLine*>(a.table + (long long)m.to[k] * (2 * kTableSlots) + column) = x[k];
+}
+__device__ inline void move_tokens(const ReorderArgs& a, const Moves& m, int column) {
+  StateLine x[kGroupWidth];
+#pragma unroll
+  for (int k = 0; k < kGroupWidth; ++k) {
+    if (m.to[k] < 0 || column >= m.length[k]) continue;
+    x[k] = *reinterpret_cast<const StateLine*>(a.tokens + (long long)m.from[k] * a.L_max + column);
   }
 #pragma unroll
   for (int k = 0; k < kGroupWidth; ++k) {
-    const int slot = __builtin_amdgcn_readlane(to, k), length = __builtin_amdgcn_readlane(m.length, k);
-    if (slot < 0 || column >= length) continue;
-    int* out = a.tokens + (long long)slot * a.L_max + column;
-    if (column + 4 <= length) *reinterpret_cast<StateLine*>(out) = x[k];
+    if (m.to[k] < 0 || column >= m.length[k]) continue;
+    int* out = a.tokens + (long long)m.to[k] * a.L_max + column;
+    if (column + 4 <= m.length[k]) *reinterpret_cast<StateLine*>(out) = x[k];
     else
       for (int j = 0; j < 3; ++j)
-        if (column + j < length) out[j] = (int)x[k].w[j];
+        if (column + j < m.length[k]) out[j] = (int)x[k].w[j];
   }
 }
 // A row's length and number of distinct tokens (`n`, `nd` as its parent had them), and its new token, once the copies are there.
@@ -853,9 +861,12 @@ __global__ __launch_bounds__(kGroupThreads) void state_reorder_group_kernel(Reor
   const int t = threadIdx.x;
   const Move m = move_of(a, blockIdx.x, true);
   const Appended x = appended_of(a, blockIdx.x, m);
-  move_table(a, m, t * 4);
-  move_table(a, m, kTableSlots + t * 4);
-  for (int column = t * 4; column < a.L_max; column += kGroupThreads * 4) move_tokens(a, m, column);
+  Moves all;
+  fetch_moves(all, m);
+  move_table(a, all, t * 4);
+  move_table(a, all, kTableSlots + t * 4);
+  fetch_lengths(all, m);
+  for (int column = t * 4; column < a.L_max; column += kGroupThreads * 4) move_tokens(a, all, column);
   __syncthreads();                                       // (everybody has read, and written)
   if (t < a.width && m.to >= 0) append_token(a, m.to, m.length, x.nd, x.token);
 }
@@ -867,8 +878,14 @@ __global__ __launch_bounds__(kReorderThreads) void state_reorder_few_kernel(Reor
   const int block = blockIdx.y - kReorderTables;         // (below 0: of the tables)
   const Move m = move_of(a, blockIdx.x, block >= 0);
   const int column = ((block < 0 ? blockIdx.y : block) * kReorderThreads + threadIdx.x) * 4;
-  if (block < 0) move_table(a, m, column);
-  else move_tokens(a, m, column);
+  Moves all;
+  fetch_moves(all, m);
+  if (block < 0) {
+    move_table(a, all, column);
+  } else {
+    fetch_lengths(all, m);
+    move_tokens(a, all, column);
+  }
 }
 
 // Wider groups: a workgroup takes 1 KB of a group's slots, a wave that of kReorderEach of them, and all are read before any is written.  2 groups
@@ -884,14 +901,18 @@ __global__ __launch_bounds__(SIP_MAX_BEAMS / kReorderEach * 64) void state_reord
   const long long pitch = table ? 2 * kTableSlots : a.L_max;
   const uint32_t empty = column < kTableSlots ? kTableEmpty : 0u;
   StateLine x[kReorderEach];
-  int to[kReorderEach], left[kReorderEach];              // words from mine on that move
+  int from[kReorderEach], to[kReorderEach], left[kReorderEach];          // words from mine on that move
+#pragma unroll
+  for (int j = 0; j < kReorderEach; ++j) {               // (with all lanes active, before any load of some)
+    const int k = w * kReorderEach + j, length = __builtin_amdgcn_readlane(m.length, k);
+    from[j] = __builtin_amdgcn_readlane(m.from, k);
+    to[j] = __builtin_amdgcn_readlane(m.to, k);
+    left[j] = to[j] < 0 || to[j] == from[j] ? 0 : table ? 4 : length - column;
+  }
 #pragma unroll
   for (int j = 0; j < kReorderEach; ++j) {
-    const int k = w * kReorderEach + j, from = __builtin_amdgcn_readlane(m.from, k);
-    to[j] = __builtin_amdgcn_readlane(m.to, k);
-    left[j] = to[j] < 0 || to[j] == from ? 0 : table ? 4 : __builtin_amdgcn_readlane(m.length, k) - column;
     x[j] = StateLine{{empty, empty, empty, empty}};
-    if (left[j] > 0 && from >= 0) x[j] = *reinterpret_cast<const StateLine*>(rows + from * pitch + column);
+    if (left[j] > 0 && from[j] >= 0) x[j] = *reinterpret_cast<const StateLine*>(rows + from[j] * pitch + column);
   }
 #pragma unroll
   for (int j = 0; j < kReorderEach; ++j) asm volatile("" : "+v"(x[j].w[0]), "+v"(x[j].w[1]), "+v"(x[j].w[2]), "+v"(x[j].w[3]) :: "memory");      // (they are here)
