@@ -137,6 +137,14 @@ struct EmbedGradArgs {
   float* part;                                           // [pieces][2][D] sums of what crosses a border: on the left, on the right
 };
 
+// What the wave's lanes did to its own part of LDS comes before what they do next.  (LDS takes a wave's accesses in order: no instruction, only
+// the compiler's order.)
+__device__ inline void wave_order() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
 // Stable sort of n entries by `bits` of the token, a digit after the other; from and to are LDS or global memory.  Returns where the
 // result is.  A wave has a run of entries, and counters of its own (their rows in LDS a bank apart).
 typedef uint32_t SortCounters[kSortWaves][kSortBins + 1];
@@ -165,6 +173,7 @@ __device__ inline P sort_entries(P from, P to, int n, int bits, SortCounters& at
       const bool mine = i0 + lane < last;
       const uint32_t digit = (mine ? from[i0 + lane] : 0) >> shift & mask;
       const unsigned long long same = match(digit, mine);
+      wave_order();                                      // (another lane's zero, or its count of the turn before)
       if (mine && !(same & below)) at[w][digit] += __popcll(same);
     }
     __syncthreads();
@@ -187,7 +196,9 @@ __device__ inline P sort_entries(P from, P to, int n, int bits, SortCounters& at
       const uint32_t entry = mine ? from[i0 + lane] : 0, digit = entry >> shift & mask;
       const unsigned long long same = match(digit, mine);
       uint32_t base = 0;
+      wave_order();                                      // (the first lane's place of the turn before)
       if (mine) base = at[w][digit];
+      wave_order();                                      // (all have read it)
       if (mine && !(same & below)) at[w][digit] = base + __popcll(same);
       if (mine) to[base + __popcll(same & below)] = entry;
     }

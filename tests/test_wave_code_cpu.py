@@ -27,3 +27,14 @@ def test_moves_come_from_active_lanes():
     for name, first in (("state_reorder_group_kernel", "move_tokens("), ("state_reorder_kernel", "reinterpret_cast<const StateLine*>")):
         body = _function("sip_beam.h", name)
         assert first in body and not CROSS_LANE.search(body[body.index(first):]), name
+
+
+def test_a_wave_s_counters_are_ordered():
+    # Every access of sort_entries() to the wave's counters is one lane's of what another wrote: behind a wave's or the workgroup's barrier since the last.
+    body = _function("sip_embed.h", "sort_entries")
+    order = re.compile(r"wave_order\(\)|__syncthreads\(\)")
+    accesses = [m.start() for m in re.finditer(r"\bat\[w\]\[digit\]", body)]
+    assert len(accesses) == 3
+    cleared = body.index("at[w][lane] = 0")
+    for before, at in zip([cleared] + accesses, accesses):
+        assert order.search(body, before, at), body[before:at]
