@@ -40,14 +40,16 @@ def sip_beam_workspace_bytes(groups: int, width: int, V: int, n: int) -> int:
 
 
 def sip_beam_select(logits: torch.Tensor, scores: torch.Tensor, width: int, n: Optional[int] = None, *,
-                    finished: Optional[torch.Tensor] = None, rank_scale: Optional[torch.Tensor] = None, end_token: int = 0,
-                    logit_scale: float = 1.0, tokens: Optional[torch.Tensor] = None, parents: Optional[torch.Tensor] = None,
-                    out_scores: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
-                    stream: Optional[torch.cuda.Stream] = None) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
+                    finished: Optional[torch.Tensor] = None, rank_scale: Optional[torch.Tensor] = None,
+                    end_token: Optional[int] = None, logit_scale: float = 1.0, tokens: Optional[torch.Tensor] = None,
+                    parents: Optional[torch.Tensor] = None, out_scores: Optional[torch.Tensor] = None,
+                    workspace: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None
+                    ) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
     """(tokens, parents, scores), each [groups, n] in descending order: the ``n`` (default: ``width``) best continuations of every
     group of ``width`` beams, from ``logits`` [groups * width, V] (float32 or bfloat16) and the beams' ``scores`` so far (float32,
-    -inf = no such beam).  ``finished`` (uint8 or bool): those beams go on at no cost with ``end_token`` alone.  ``rank_scale``
-    (float32, > 0): what totals are multiplied with for comparison.  Missing continuations are token -1, parent -1, score -inf."""
+    -inf = no such beam).  ``finished`` (uint8 or bool): those beams go on at no cost with ``end_token`` alone, which has to be given
+    then.  ``rank_scale`` (float32, > 0): what totals are multiplied with for comparison.  Missing continuations are token -1, parent -1,
+    score -inf."""
     lib = _load()
     _matrix(logits, "logits", (torch.bfloat16, torch.float32))
     (R, V), dev = logits.shape, logits.device
@@ -56,6 +58,8 @@ def sip_beam_select(logits: torch.Tensor, scores: torch.Tensor, width: int, n: O
     groups, n = R // width, width if n is None else n
     _vector(scores, "scores", torch.float32, R)
     if finished is not None:
+        if end_token is None:
+            raise TypeError("finished beams go on with end_token: it has to be given")
         _vector(finished, "finished", torch.bool if finished.dtype == torch.bool else torch.uint8, R)
     if rank_scale is not None:
         _vector(rank_scale, "rank_scale", torch.float32, R)
@@ -73,8 +77,8 @@ def sip_beam_select(logits: torch.Tensor, scores: torch.Tensor, width: int, n: O
     ws = _scratch(workspace, 0 if workspace is not None else lib.sip_beam_workspace_bytes(groups, width, V, n), dev, stream)
     stride = logits.stride(0) if R > 1 else (V + 7) // 8 * 8                 # (that of a single row says nothing)
     _call("sip_beam_select", dev, stream, _ptr(logits), groups, width, V, stride, _DTYPES[logits.dtype], logit_scale,
-          _ptr(scores), _ptr(finished), end_token, _ptr(rank_scale), n, _ptr(tokens), _ptr(parents), _ptr(out_scores), _ptr(ws),
-          _nbytes(ws))
+          _ptr(scores), _ptr(finished), 0 if end_token is None else end_token, _ptr(rank_scale), n, _ptr(tokens), _ptr(parents),
+          _ptr(out_scores), _ptr(ws), _nbytes(ws))
     return tokens, parents, out_scores
 
 
