@@ -199,8 +199,9 @@ sip_status sip_embed_codes(const uint8_t* codes, int64_t codes_stride, const voi
 /*
  *   grad_weight[v] = scale * sum_{i: ids[i] = v} grad_out[i]   (+ grad_weight[v] if accumulate)
  *
- * Tokens are sorted, and a row of grad_weight is the fp32 sum of its tokens' rows in an order that depends on the
- * tokens alone, scaled, added to what was there if asked for, and rounded once.  A token outside [0, V) takes no part, whatever
+ * Tokens are sorted, and a row of grad_weight is the fp32 sum of its tokens' rows, scaled, added to what was there if asked for, and
+ * rounded once.  The same call gives the same bits every time; calls that differ in sizes, types or `accumulate` may add up the same
+ * rows in another order.  A token outside [0, V) takes no part, whatever
  * its row of grad_out holds.  With accumulate != 0 rows of grad_weight that no token names are not touched; without, they
  * become zeros.  (A matrix that is head and embedding at once: sip_xent_backward() first, then this call with accumulate.)
  *
