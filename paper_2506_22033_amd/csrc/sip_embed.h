@@ -131,7 +131,7 @@ struct EmbedGradArgs {
   int pieces, piece, whole;                              // entries of a piece, and of a token that is not cut: powers of two
   // workspace
   int* live;                                             // entries that take part
-  uint32_t* key; uint32_t* pos;                          // [N + 8] tokens and their positions, sorted
+  uint32_t* key; uint32_t* pos;                          // [N + 2 kSumAhead] tokens and their positions, sorted; the last are looked at, and may be anything
   int* cut;                                              // [pieces + 1] where a piece begins
   uint32_t* spare[2];                                    // [N] for buckets that LDS does not hold
   float* part;                                           // [pieces][2][D] sums of what crosses a border: on the left, on the right
@@ -377,7 +377,7 @@ __device__ inline void embed_store(const EmbedGradArgs& a, long long at, f32x8 s
 constexpr int kSumAhead = 8;
 template <bool BF16, bool ADD>
 __global__ __launch_bounds__(256) void embed_sum_kernel(EmbedGradArgs a) {
-  const uint32_t per_row = a.D / 8, u = blockIdx.x * 256 + threadIdx.x;                     // (up to 2^28)
+  const uint32_t per_row = a.D / 8, u = blockIdx.x * 256 + threadIdx.x;                     // (up to 2^21)
   const int n = *a.live, piece = (int)(u / per_row), c = (int)(u - piece * per_row) * 8;
   if (piece >= a.pieces) return;
   const int first = a.cut[piece], end = a.cut[piece + 1];               // (from the last entry on: anything)
