@@ -35,7 +35,7 @@ extern "C" {
  *  logits      [groups * width, row_stride] fp32 or bf16, as sip_sample() takes them: base pointer and row stride
  *              multiples of 16 bytes.  Only the first V entries of a row are read; never written.  A logit of -inf is no
  *              continuation; a row that holds a NaN or +inf has none.
- *  logit_scale finite and > 0: 1, or the reciprocal of a temperature.
+ *  logit_scale 1e-30 to 1e30: 1, or the reciprocal of a temperature.
  *  scores      [groups * width] fp32: the beams' log-probabilities so far.  A beam whose score is not finite
  *              (-inf: one that does not exist, as all but the first before the first step) has no
  *              continuation, and its logits are not looked at.
@@ -48,7 +48,8 @@ extern "C" {
  *  n           1 .. SIP_MAX_CONTINUATIONS, normally width, or 2 * width where the caller takes out those that end.
  *  tokens,     [groups, n] int32: the continuation's token, and the beam (0 .. width - 1) that it continues.
  *  parents
- *  out_scores  [groups, n] fp32: total.  May be `scores` itself where n = width.
+ *  out_scores  [groups, n] fp32: total, -inf below fp32's range (a mask's lowest value times a logit_scale above 1).  May be `scores`
+ *              itself where n = width.
  *  Where a group has fewer than n continuations, the rest is token -1, parent -1, score -inf.
  *  workspace   256-byte aligned, at least sip_beam_workspace_bytes(groups, width, V, n) bytes; contents need not be kept.  What
  *              is enough is enough for fewer groups, fewer beams, a smaller vocabulary or a smaller n too.

@@ -168,8 +168,9 @@ sip_status sip_head_logits(const void* hidden, int32_t B, int32_t D, int64_t hid
  *  logits    [B, logits_stride] fp32 or bf16, aligned to its element; only the first V entries of a row are read or written.
  *  workspace 256-byte aligned, at least sip_head_adapt_workspace_bytes(B, adapters, rank, D) bytes.  What is enough for B
  *            rows is enough for fewer.
- * Products and sums are fp32, t is kept in fp32; the new logit is rounded once.  A row with an entry of t that is not finite (or beyond the
- * largest bf16), or with such an entry in an fp32 hidden state, has logits of NaN; other rows are not affected.
+ * Products and sums are fp32, scales[a] * t is kept in fp32; the new logit is rounded once.  A row with an entry of t (or of scales[a] * t)
+ * that is not finite or beyond the largest bf16, or with such an entry in an fp32 hidden state, has logits of NaN; other rows are not
+ * affected.  An entry of `up` that is not finite makes its own logit NaN or infinite, of either sign.
  */
 size_t sip_head_adapt_workspace_bytes(int32_t B, int32_t adapters, int32_t rank, int32_t D);
 sip_status sip_head_adapt(const void* hidden, int32_t B, int32_t D, int64_t hidden_stride, sip_dtype hidden_dtype,
@@ -201,9 +202,8 @@ sip_status sip_embed_codes(const uint8_t* codes, int64_t codes_stride, const voi
  *
  * Tokens are sorted, and a row of grad_weight is the fp32 sum of its tokens' rows, scaled, added to what was there if asked for, and
  * rounded once.  The same call gives the same bits every time; calls that differ in sizes, types or `accumulate` may add up the same
- * rows in another order.  A token outside [0, V) takes no part, whatever
- * its row of grad_out holds.  With accumulate != 0 rows of grad_weight that no token names are not touched; without, they
- * become zeros.  (A matrix that is head and embedding at once: sip_xent_backward() first, then this call with accumulate.)
+ * rows in another order.  A token outside [0, V) takes no part, whatever its row of grad_out holds.  With accumulate != 0 rows of
+ * grad_weight that no token names are not touched; without, they become zeros.  (A matrix that is head and embedding at once: sip_xent_backward() first, then this call with accumulate.)
  *
  *  grad_out    [N, grad_out_stride] bf16 or fp32, grad_weight [V, grad_weight_stride] bf16 or fp32; rows aligned to 16 bytes.
  *  N           0 .. SIP_MAX_TOKENS; D a multiple of 8.
