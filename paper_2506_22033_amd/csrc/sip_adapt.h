@@ -11,7 +11,9 @@ namespace sip {
 // Rows that share an adapter are served sixteen at a time, a batch: the sixteen columns of a matrix instruction, whose rows are an
 // adapter's.  Both products read their adapter from memory straight into the instruction's registers.
 constexpr int kAdaptRows = 16;
-constexpr int kAdaptDirect = 64;                         // up to so many rows a wave finds its batch by itself
+// Up to so many rows a wave finds its batch by itself.  One row, rank 16, V = 128256: 4.3 + 5.5 us, instead of 2.9 + 4.2 + 5.3 with a kernel that lists
+// the rows.  (Near the limit listing is shorter: 59 rows of 57 adapters of rank 8, V = 125990, 10.7 + 47.2 and 4.6 + 7.4 + 36.8.)
+constexpr int kAdaptDirect = 64;
 
 struct AdaptArgs {
   const void* hidden; long long hidden_stride;
@@ -27,7 +29,7 @@ struct AdaptArgs {
   int parts, batches;
 };
 
-// One workgroup lists the rows by adapter, in batches.  (The order of an adapter's rows changes no result.)  Latency: 256 rows 4.7 us.
+// One workgroup lists the rows by adapter, in batches.  (The order of an adapter's rows changes no result.)  Latency: 256 rows 4.8 us.
 __global__ __launch_bounds__(1024) void adapt_rows_kernel(AdaptArgs p) {
   __shared__ int first[SIP_MAX_ADAPTERS], wave_n[16], wave_m[16];
   const int t = threadIdx.x, lane = t & 63, w = t >> 6, A = p.adapters;
@@ -109,7 +111,7 @@ __device__ inline Split split_of(f32x8 x) {
 }
 
 // t of a batch, sixteen entries a workgroup: its waves share a part of the sum over D and join what they have in order.  Bound by reading:
-// 32 adapters of rank 64, D = 4096, 16.8 MB, 10.5 us; one of rank 16 4.2 us in four parts, 6.8 in one.
+// 32 adapters of rank 64, D = 4096, 16.8 MB, 10.3 us; one of rank 16 4.4 us in four parts, 6.9 in one.
 constexpr int kDownWaves = 16, kDownParts = 4;
 template <bool BF16, bool DIRECT>
 __global__ __launch_bounds__(kDownWaves * 64) void adapt_down_kernel(AdaptArgs p) {
@@ -158,9 +160,9 @@ __global__ __launch_bounds__(kDownWaves * 64) void adapt_down_kernel(AdaptArgs p
 
 // The additions of one batch to `tiles` of kUpWaves * 32 logits each.  A wave's share of a tile is 32 entries of the vocabulary, of
 // which a lane has eight neighbours of one row, loaded and stored wherever they lie: two matrix products, one for the first four of every
-// eight, one for the others (four a lane are 32 bytes of a bf16 row at once: 219 rows, 40 adapters of rank 8, V = 214517 140 us in all instead of 92).  ONE: tiles = 1, and t may be in parts.
+// eight, one for the others (four a lane are 32 bytes of a bf16 row at once: 219 rows, 40 adapters of rank 8, V = 214517 130 us instead of 82).  ONE: tiles = 1, and t may be in parts.
 // t enters as three bf16 parts, which hold its 24 bits: the products are exact, the matrix cores hardly busy.  Bound by memory: 224 rows, 32
-// adapters of rank 64, V = 128256, 760 MB, 162 us, 4.7 TB/s (558 us with a lane an entry of the vocabulary and fp32 products).
+// adapters of rank 64, V = 128256, 760 MB, 161 us, 4.7 TB/s (555 us with a lane an entry of the vocabulary and fp32 products).
 constexpr int kUpWaves = 4, kUpEntries = kUpWaves * 32;
 struct __attribute__((packed, aligned(4))) FourF32 { f32x4 x; };        // four logits as they may lie: aligned to one
 struct __attribute__((packed, aligned(2))) EightBf16 { u32x4 x; };
@@ -200,7 +202,8 @@ __global__ __launch_bounds__(kUpWaves * 64) void adapt_up_kernel(AdaptArgs p, in
   const uint16_t* up = p.up + (long long)x.adapter * p.V * p.rank;
   const bf16x8 none = {};
   // Tiles whose loads are under way at once, kEarly while as many others are multiplied.  More waves do better where their loads are short: rank
-  // 8 as above 92 us, kEarly 98, and with two tiles 119, four 170; rank 64 as above 1 % less with two, rank 112 2 % less kEarly.
+  // 8 as above 82 us, two tiles the same, kEarly 91, four tiles 96; rank 64 as above 161 with two, 164 with one and 163 not kEarly; 220 rows of 10
+  // adapters of rank 112, V = 213705, 170, 176 not kEarly and 179 with two.
   constexpr bool kEarly = ONE || STEPS > 1;
   constexpr int kAhead = ONE || STEPS != 2 ? 1 : 2;
   constexpr int kParts = ONE ? kDownParts : 1;

@@ -204,7 +204,7 @@ __device__ __forceinline__ int select_apart(u32x4 (&raw)[kBeamLoads], double* li
 // The chunk stays in registers: its maxima give the bound from which on logits can be among the n best -- n of the 256 lanes' maxima reach it,
 // and few logits more --, its sum follows, and what reaches the bound is ranked in LDS.
 // fp32 is bound by reading: 256 rows of V = 152064, a tenth of them finished, n = 8 28.2 us, 5 TB/s.  bf16 by vector instructions: 224 rows of
-// 151643 20 us for n = 1 (floor 13), 24 for n = 64: unpacking, an exponential's four passes, the ranks.
+// 151643 19 us for n = 1 (floor 13), 24 for n = 64: unpacking, an exponential's four passes, the ranks.
 template <bool BF16>
 __global__ __launch_bounds__(kBeamThreads) void beam_chunk_kernel(BeamArgs a) {
   constexpr int kGroup = BF16 ? 8 : 4, kEach = kBeamLoads * kGroup;      // logits of a 16-byte load, of a lane
@@ -509,7 +509,7 @@ __device__ inline uint32_t nth_head(uint32_t lead, int lists, int n, uint32_t (&
 }
 
 // Of m entries the n largest and few more, up to `enough` in all; m > enough >= n.  By the leading word of their ranks, and where that is equal
-// by the next.  What it saves: ranking 8000 entries among one another takes 2 ms.
+// by the next.  What it saves: two groups of 62 beams of one chunk each, n = 124, are merged in 17.5 us, in 1.2 ms with all entries ranked among one another.
 template <int THREADS, int ROOM>
 __device__ inline int keep_largest(BeamRank* found, int m, int n, int enough, BeamVotes& votes, int& count) {
   constexpr int kEach = (ROOM + THREADS - 1) / THREADS;
@@ -604,7 +604,7 @@ __device__ inline void store_missing(const BeamArgs& a, int kept) {
 }
 
 // A group whose lists have up to kMergeFew entries together: all of them in registers.  Latency, of the loads and a dozen barriers: 64 groups
-// with 608 entries 6.5 us, one with 64 4.1.
+// with 608 entries 6.8 us, one with 64 4.2 (with the kernel for any group 8.0 and 5.8).
 constexpr int kMergeFew = 1024, kRankFew = 192;           // (entries that are ranked among one another at most)
 static_assert(kRankFew >= SIP_MAX_CONTINUATIONS, "all that are selected");
 __global__ __launch_bounds__(256) void beam_merge_few_kernel(BeamArgs a) {
@@ -660,7 +660,7 @@ __global__ __launch_bounds__(256) void beam_merge_few_kernel(BeamArgs a) {
 }
 
 // Any group.  The lists are in order, so one entry of each bounds what can be selected, and a list whose head is the r-th best
-// can give its n - r first entries at most.  7 groups of 32 beams, 320 lists of 64 each: 14.8 us, latency too.
+// can give its n - r first entries at most.  7 groups of 32 beams, 320 lists of 64 each: 14.6 us, latency too.
 constexpr int kMergeThreads = 1024, kRankMost = 256, kHeadsMany = 512;
 constexpr int kMergeLists = SIP_MAX_BEAMS * 64;
 constexpr int kMergeRoom = SIP_MAX_CONTINUATIONS * (SIP_MAX_CONTINUATIONS + 1) / 2;
@@ -872,7 +872,7 @@ __global__ __launch_bounds__(kGroupThreads) void state_reorder_group_kernel(Reor
 }
 
 // The same in many workgroups, 4 KB of a group's slots each, without the new tokens.  Latency: slots, then lengths, then the loads, then the stores.  64
-// groups of 8 slots with 3000 tokens each: 9.2 us for 33 MB read and written.
+// groups of 8 slots with 3000 tokens each: 9.5 us for 33 MB read and written.
 constexpr int kReorderThreads = 256, kReorderTables = 2 * kTableSlots / (kReorderThreads * 4);
 __global__ __launch_bounds__(kReorderThreads) void state_reorder_few_kernel(ReorderArgs a) {
   const int block = blockIdx.y - kReorderTables;         // (below 0: of the tables)
@@ -889,7 +889,7 @@ __global__ __launch_bounds__(kReorderThreads) void state_reorder_few_kernel(Reor
 }
 
 // Wider groups: a workgroup takes 1 KB of a group's slots, a wave that of kReorderEach of them, and all are read before any is written.  2 groups
-// of 64 slots 6.6 us; 20 with all slots in every lane's registers: the instructions of so many are what costs.  64 groups of 8 11 us.
+// of 64 slots, L_max = 2097, 6.7 us; 24 with all slots in every lane's registers: the instructions of so many are what costs.  64 groups of 8 10.8 us.
 constexpr int kReorderEach = 4, kReorderWords = 64 * 4;
 constexpr int kReorderTableBlocks = 2 * kTableSlots / kReorderWords;
 __global__ __launch_bounds__(SIP_MAX_BEAMS / kReorderEach * 64) void state_reorder_kernel(ReorderArgs a) {

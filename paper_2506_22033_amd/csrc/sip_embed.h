@@ -58,7 +58,7 @@ struct EmbedArgs {
 };
 
 // A lane takes eight neighbours of a row, or of kEmbedAhead rows, all under way at once.  Bound by memory: 16000 tokens of 4096 bf16 40 us, 4.5 TB/s
-// of the distinct rows and what is written; a few tokens by a launch and two reads, 2.9 us.
+// of the distinct rows and what is written; a few tokens by a launch and two reads, 2.8 us.
 template <bool CODES, int kEmbedAhead>
 __global__ __launch_bounds__(256) void embed_kernel(EmbedArgs a) {
   const uint32_t per_row = a.D / 8, total = per_row * (uint32_t)a.N;                        // (up to 2^31)
@@ -321,8 +321,8 @@ __device__ inline LdsEntries sort_bucket(const EmbedGradArgs& a, LdsEntries from
 // A workgroup a bucket, up to 128 of them, each of which reads all tokens: no counts are exchanged, and none waits for another.  The
 // workgroups behind fill grad_weight with zeros meanwhile, unless it is added to.  ROOM: entries of a bucket that LDS holds, twice; larger buckets
 // are sorted in the workspace.
-// 8192 tokens 9.4 us, 65536 21, and 41 where one token is an eighth of them: reading, and the largest bucket.  Beside 1.24 GB of zeros
-// that is hidden: 211 us, 5.9 TB/s.
+// 8192 tokens 7 to 9 us, 65536 22, and 39 where one token is an eighth of them: reading, and the largest bucket.  Beside 1.24 GB of zeros
+// that is hidden: 215 us, 5.8 TB/s.
 template <int ROOM>
 __global__ __launch_bounds__(kSortThreads) void embed_sort_kernel(EmbedGradArgs a) {
   __shared__ uint32_t room[2][ROOM];
@@ -372,8 +372,8 @@ __device__ inline void embed_store(const EmbedGradArgs& a, long long at, f32x8 s
 }
 
 // A lane: eight columns of one piece, eight rows under way at once, and where they are added to the rows of grad_weight that end there.
-// Bound by memory: 8192 rows of 4096 bf16, a tenth masked, added to 3500 rows of bf16 26.5 us, 4.4 TB/s; 65536 of 2048 to as many rows of fp32 275 us,
-// 4.9 TB/s.
+// Bound by memory: 8192 rows of 4096 bf16, a tenth masked, added to 3500 rows of bf16 26 us, 4.5 TB/s; 65536 of 2048 to 53000 rows of fp32 240 us,
+// 4.7 TB/s.
 constexpr int kSumAhead = 8;
 template <bool BF16, bool ADD>
 __global__ __launch_bounds__(256) void embed_sum_kernel(EmbedGradArgs a) {
@@ -439,7 +439,7 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(EmbedGradArgs a) {
 
 // A small gradient in one launch: a workgroup a bucket, which sums its tokens' rows itself and clears the bucket's others.  The sorted
 // entries go to groups of waves that cover a row each, a run of entries a group; what crosses the end of a run goes through LDS.
-// 384 tokens, 4096 x 512 fp32: 8.4 us instead of the three kernels' 16.
+// 384 tokens, 4096 x 512 fp32: 8.5 us instead of the three kernels' 16.
 constexpr int kSmallTokens = 1024, kSmallWidth = kSortWaves * 512;
 template <bool BF16, bool ADD>
 __global__ __launch_bounds__(kSortThreads) void embed_small_kernel(EmbedGradArgs a) {
@@ -515,7 +515,7 @@ __global__ __launch_bounds__(kSortThreads) void embed_small_kernel(EmbedGradArgs
 
 // The tokens that begin in a piece and go on behind its right border.  A workgroup looks at kJoinPieces of them, kJoinLanes lanes of eight
 // columns, of which each has kJoinWorkers workers that take every sixteenth of the token's pieces: one that is a fifth of all tokens has a thousand.
-// Latency, 4 us where there is nothing to join, 8 for the 18 most frequent tokens of 8192, and 24 where 50000 tokens of 568 columns are drawn with
+// Latency, 2 to 5 us where there is nothing to join, 8 for the 18 most frequent tokens of 8192, and 23 where 50000 tokens of 568 columns are drawn with
 // 1 / rank^1.2 (64 lanes, 1024 threads: 8.5 and 54; 8 lanes: 13 and 26).
 constexpr int kJoinPieces = 4, kJoinThreads = 256, kJoinLanes = 16, kJoinWorkers = kJoinThreads / kJoinLanes;
 template <bool ADD>

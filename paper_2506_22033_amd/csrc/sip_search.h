@@ -17,7 +17,7 @@ static_assert(SIP_MAX_V <= 64 * sip::kBeamThreads * sip::kBeamLoads * 4, "the me
 size_t beam_part_bytes(int64_t lists) { return head_align((size_t)lists * sizeof(sip::BeamPart)); }
 
 // Up to so many words a group's slots are moved by one workgroup, in one launch instead of two.  Kernels in us, one and two: a group of 4 beams,
-// L_max = 512, 5.3 and 3.4 + 2.6; 128 groups of 4, 2048, 9.5 and 6.5 + 3.6; but 64 of 8, 4096, 14.8 and 9.4 + 4.0.
+// L_max = 512, 4.8 and 3.3 + 2.7; 128 groups of 4, 2048, 10.0 and 7.5 + 4.0; but 64 of 8, 4096, 16.6 and 9.5 + 4.4.
 constexpr long long kGroupWords = 48 << 10;
 static_assert(kGroupWords < (sip::kGroupWidth + 1) * 2 * sip::kTableSlots, "no wider groups");
 
